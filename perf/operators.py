@@ -187,7 +187,7 @@ def _stored(rows):
     """E4M3 codes and scales of rows [...,128]."""
     x = rows.float()
     amax = x.abs().amax(-1, keepdim=True)
-    inv = torch.where(amax == 0, torch.zeros_like(amax), LARGEST / amax)
+    inv = torch.where(amax == 0, torch.zeros_like(amax), torch.full_like(amax, LARGEST) / amax)      # (one rounding)
     return (x * inv).clamp(-LARGEST, LARGEST).to(E4M3).view(torch.uint8), (amax / LARGEST).squeeze(-1)
 
 
@@ -314,7 +314,7 @@ def _exact_codes(x):
     """The E4M3 values nearest to x * 448 / (largest of the row), ties to even, and the scale.  What is rounded to 8 bits is
     the product of 32-bit factors, as the codes are defined: those beside a tie would else go by the last bit of it."""
     top = x.abs().amax(-1, keepdim=True)
-    y = torch.where(top > 0, x.float() * (LARGEST / top.float()), 0.0).double()
+    y = torch.where(top > 0, x.float() * torch.full_like(top, LARGEST).float().div(top.float()), 0.0).double()
     step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
     return torch.round(y / step) * step, (top / LARGEST)[..., 0]
 
