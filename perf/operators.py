@@ -187,8 +187,9 @@ def _stored(rows):
     """E4M3 codes and scales of rows [...,128]."""
     x = rows.float()
     amax = x.abs().amax(-1, keepdim=True)
-    inv = torch.where(amax == 0, torch.zeros_like(amax), torch.full_like(amax, LARGEST) / amax)      # (one rounding)
-    return (x * inv).clamp(-LARGEST, LARGEST).to(E4M3).view(torch.uint8), (amax / LARGEST).squeeze(-1)
+    largest = torch.full_like(amax, LARGEST)               # (a quotient with a number would be a product with its inverse)
+    inv = torch.where(amax == 0, torch.zeros_like(amax), largest / amax)
+    return (x * inv).clamp(-LARGEST, LARGEST).to(E4M3).view(torch.uint8), (amax / largest).squeeze(-1)
 
 
 def _write(pages, scales, rows, at, slot, there):
