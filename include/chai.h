@@ -59,7 +59,7 @@ enum {
 /* Size of the scratch array built into the library for chai_decode_attention_static. */
 #define CHAI_STATIC_SCRATCH_BYTES (32u << 20)
 
-enum { CHAI_F32 = 0, CHAI_BF16 = 1 };
+enum { CHAI_F32 = 0, CHAI_BF16 = 1, CHAI_E4M3 = 2 /* only where an argument is called cache_dtype */ };
 
 /* Library version, major * 100 + minor. */
 int chai_version(void);
@@ -504,6 +504,84 @@ int chai_project_qk(const void *x, const void *w_q, const void *w_k, const int32
 int chai_project_qk_timed(const void *x, const void *w_q, const void *w_k, const int32_t *rep_heads, int B, int H,
                           int k, int Tn, int D, int d, int dtype, void *q_out, void *k_compact, int pos0,
                           int Tc_cap, void *stream, void *start_event, void *stop_event);
+
+/*
+ * Caches in pages.  A server's requests have lengths of their own and come
+ * and go; their keys and values then live in one pool of pages, and a table
+ * names the pages of every row in order.  The method is unchanged (Sections 2
+ * and 3.4-3.5); only where a cached row lies, and how many a request has, is.
+ *
+ *   k_pages     [n_pages,k,page,d]   a page holds `page` consecutive positions
+ *   v_pages     [n_pages,H,page,d]   of all streams of one row; cache_dtype is
+ *               `dtype` (CHAI_F32 or CHAI_BF16, as q and new rows are) or
+ *               CHAI_E4M3: uint8 codes as chai_quantize_rows makes them, with
+ *   k_scales    [n_pages,k,page]     fp32, one scale per cached row (NULL and
+ *   v_scales    [n_pages,H,page]     not read in the other cases)
+ *   block_table [B,max_blocks] int32, on the device: position t of row b lies
+ *               in page block_table[b][t / page], at place t % page.  An entry
+ *               outside [0,n_pages) is an absent page: attention leaves its
+ *               positions out, nothing is written to it, zeros are read back.
+ *               Entries beyond a row's positions are not used (they may hold
+ *               anything); pages may stand in several rows (a shared prefix)
+ *               as long as no call writes to them.
+ *   seq_lens, start, count  [B] int32, on the device: nothing is read back, so
+ *               the calls can be captured and replayed with other lengths.
+ *
+ * Layers without clusters: k = H with rep_heads and head_to_cluster both NULL.
+ * page is a multiple of 8, at least 8.  Limits (CHAI_ERR_UNSUPPORTED): d = 128,
+ * B <= 4096, H + k <= 65535, T_max and Tn <= 2^24, n_pages * H * page < 2^32
+ * rows, B * H * T_max < 2^35.
+ *
+ * chai_paged_append_kv: rows i < count[b] (count NULL: all Tn) of a block of
+ *   new tokens go to positions start[b] + i: keys of the representatives,
+ *   values of all heads, copied or quantised on the way.
+ *     k_new  element (b,h,i,c) at (b*H+h)*k_head_stride + i*d + c
+ *     v_new  element (b,h,i,c) at (b*H+h)*v_head_stride + i*d + c
+ *     (strides in elements, >= Tn*d, multiples of 8: a prompt's keys and values
+ *     are read in place from contiguous caches).  Counts are taken into
+ *     [0,Tn]; positions below 0 or past the table are not written, nor are
+ *     slots without a cluster (rep_heads < 0).  Two rows must not be given
+ *     the same place in one call.
+ * chai_paged_gather_kv: reads back; row i < count[b] of k_out [B,k,Tn,d] and
+ *   v_out [B,H,Tn,d] (dtype) is position start[b] + i, codes times their
+ *   scale in fp32, rounded once where dtype is CHAI_BF16; absent positions
+ *   give 0, rows i >= count[b] are not written.  What it leaves are contiguous
+ *   caches as chai_prefill_attention and the others take them.
+ * chai_paged_decode_attention: one new token of every row attends to
+ *   positions t < seq_lens[b] of its row (taken into [0,T_max]) that are in a
+ *   page, as chai_decode_attention does:
+ *     q [B,H,d] dtype;  out [B,H,d] fp32, written;  maps as there
+ *   Rows without such a position, and heads whose scores are all -inf, get 0.
+ *   T_max (1 <= T_max <= max_blocks * page) bounds the rows' lengths; what the
+ *   masked places hold (infinities, NaN) does not matter.
+ * chai_paged_decode_step: position seq_lens[b]-1 of every row (if seq_lens[b]
+ *   is in [1,T_max]) is the token being decoded: its rows k_new, v_new [B,H,d]
+ *   are written to the pages as by chai_paged_append_kv, then attention as
+ *   above; an 8-bit cache is attended to as it was quantised.
+ * workspace: chai_paged_workspace_bytes (0 on invalid sizes; never decreases
+ *   when B, H, k or T_max grows), 256-byte aligned, contents as for
+ *   chai_decode_attention.
+ */
+size_t chai_paged_workspace_bytes(int B, int H, int k, int T_max, int d);
+int chai_paged_append_kv(const void *k_new, const void *v_new, int64_t k_head_stride, int64_t v_head_stride,
+                         const int32_t *rep_heads, const int32_t *block_table, const int32_t *start,
+                         const int32_t *count, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int B,
+                         int H, int k, int Tn, int n_pages, int page, int max_blocks, int d, int dtype,
+                         int cache_dtype, void *stream);
+int chai_paged_gather_kv(const void *k_pages, const void *v_pages, const float *k_scales, const float *v_scales,
+                         const int32_t *block_table, const int32_t *start, const int32_t *count, void *k_out,
+                         void *v_out, int B, int H, int k, int Tn, int n_pages, int page, int max_blocks, int d,
+                         int dtype, int cache_dtype, void *stream);
+int chai_paged_decode_attention(const void *q, const void *k_pages, const void *v_pages, const float *k_scales,
+                                const float *v_scales, const int32_t *head_to_cluster, const int32_t *rep_heads,
+                                const int32_t *block_table, const int32_t *seq_lens, int B, int H, int k, int T_max,
+                                int n_pages, int page, int max_blocks, int d, int dtype, int cache_dtype, float scale,
+                                float *out, void *workspace, size_t workspace_bytes, void *stream);
+int chai_paged_decode_step(const void *q, const void *k_new, const void *v_new, void *k_pages, void *v_pages,
+                           float *k_scales, float *v_scales, const int32_t *head_to_cluster, const int32_t *rep_heads,
+                           const int32_t *block_table, const int32_t *seq_lens, int B, int H, int k, int T_max,
+                           int n_pages, int page, int max_blocks, int d, int dtype, int cache_dtype, float scale,
+                           float *out, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -6,7 +6,8 @@ any entry point without a built library raises ImportError.
 """
 import importlib
 
-_BINDING_NAMES = ("CHAI_BF16", "CHAI_F32", "CHAI_OK", "EXPORTS", "LIB_PATH", "ChaiError", "alloc_workspace", "lib")
+_BINDING_NAMES = ("CHAI_BF16", "CHAI_E4M3", "CHAI_F32", "CHAI_OK", "EXPORTS", "LIB_PATH", "ChaiError", "alloc_paged_workspace",
+                  "alloc_workspace", "lib")
 
 
 def __getattr__(name):

@@ -19,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libchai.so")
 
 CHAI_OK = 0
-CHAI_F32, CHAI_BF16 = 0, 1
+CHAI_F32, CHAI_BF16, CHAI_E4M3 = 0, 1, 2
 STATUS_NAMES = {0: "CHAI_OK", 1: "CHAI_ERR_NULL", 2: "CHAI_ERR_SHAPE", 3: "CHAI_ERR_DTYPE", 4: "CHAI_ERR_WORKSPACE",
                 5: "CHAI_ERR_UNSUPPORTED", 6: "CHAI_ERR_HIP", 7: "CHAI_ERR_ALIGN", 8: "CHAI_ERR_STATIC_LIMIT"}
 CHAI_STATIC_SCRATCH_BYTES = 32 << 20
@@ -32,7 +32,9 @@ EXPORTS = ["chai_version", "chai_status_string", "chai_score_features", "chai_as
            "chai_decode_attention_q8", "chai_decode_attention_q8_timed",
            "chai_decode_scores", "chai_decode_values", "chai_decode_scores_timed", "chai_decode_values_timed",
            "chai_dense_decode_attention", "chai_prefill_workspace_bytes", "chai_prefill_attention",
-           "chai_prefill_attention_timed", "chai_dense_prefill_attention", "chai_project_qk", "chai_project_qk_timed", "chai_stream_read_probe", "chai_mfma_rate_probe"]
+           "chai_prefill_attention_timed", "chai_dense_prefill_attention", "chai_project_qk", "chai_project_qk_timed", "chai_stream_read_probe", "chai_mfma_rate_probe",
+           "chai_paged_workspace_bytes", "chai_paged_append_kv", "chai_paged_gather_kv", "chai_paged_decode_attention",
+           "chai_paged_decode_step"]
 
 
 class ChaiError(RuntimeError):
@@ -85,8 +87,14 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.chai_prefill_attention.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, cf, vp, vp, sz, vp]
     L.chai_prefill_attention_timed.argtypes = L.chai_prefill_attention.argtypes + [vp, vp]
     L.chai_dense_prefill_attention.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, cf, vp, vp, sz, vp]
+    L.chai_paged_workspace_bytes.restype = sz
+    L.chai_paged_workspace_bytes.argtypes = [ci] * 5
+    L.chai_paged_append_kv.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp] + [ci] * 10 + [vp]
+    L.chai_paged_gather_kv.argtypes = [vp] * 9 + [ci] * 10 + [vp]
+    L.chai_paged_decode_attention.argtypes = [vp] * 9 + [ci] * 10 + [cf, vp, vp, sz, vp]
+    L.chai_paged_decode_step.argtypes = [vp] * 11 + [ci] * 10 + [cf, vp, vp, sz, vp]
     for fn in EXPORTS:
-        if fn not in ("chai_status_string", "chai_decode_workspace_bytes", "chai_prefill_workspace_bytes",
+        if fn not in ("chai_paged_workspace_bytes", "chai_status_string", "chai_decode_workspace_bytes", "chai_prefill_workspace_bytes",
                       "chai_decode_q8_workspace_bytes"):
             getattr(L, fn).restype = ci
     return L
@@ -489,6 +497,117 @@ def alloc_workspace(B: int, H: int, k: int, T: int, d: int, dtype: int, device="
     """Device scratch of the size the decode calls ask for (torch allocations are 512-byte aligned)."""
     n = max(chai_decode_workspace_bytes(B, H, k, T, d, dtype), 256)
     return torch.empty((n,), dtype=torch.uint8, device=device)
+
+
+def _paged_shapes(fn, k_pages, v_pages, k_scales, v_scales, block_table, dtype, maps):
+    """(B, H, k, n_pages, page, max_blocks, d, cache dtype code) of a call on pages; what does not fit together is refused here:
+    the library is given sizes once and cannot see the tensors."""
+    n_pages, k, page, d = k_pages.shape
+    H = v_pages.shape[1]
+    if v_pages.shape != (n_pages, H, page, d) or v_pages.dtype != k_pages.dtype:
+        raise ValueError(f"{fn}: k_pages {tuple(k_pages.shape)} {k_pages.dtype} and v_pages {tuple(v_pages.shape)} "
+                         f"{v_pages.dtype} do not fit together")
+    if k_pages.dtype == torch.uint8:
+        if k_scales is None or v_scales is None or k_scales.shape != (n_pages, k, page) or v_scales.shape != (n_pages, H, page) \
+                or k_scales.dtype != torch.float32 or v_scales.dtype != torch.float32:
+            raise ValueError(f"{fn}: pages of codes need fp32 scales of shape [n_pages, streams, page]")
+        code = CHAI_E4M3
+    elif k_pages.dtype != dtype:
+        raise TypeError(f"{fn}: pages of {k_pages.dtype} beside tensors of {dtype}")
+    else:
+        code = CHAI_BF16 if dtype == torch.bfloat16 else CHAI_F32
+    B, max_blocks = block_table.shape
+    for t, shape in ((block_table, (B, max_blocks)), *maps):
+        if t is not None and (t.shape != (shape if isinstance(shape, tuple) else (B, shape)) or t.dtype != torch.int32):
+            raise ValueError(f"{fn}: int32 [{B}, ...] expected, got {t.dtype} {tuple(t.shape)}")
+    return B, H, k, n_pages, page, max_blocks, d, code
+
+
+def _same(fn, shape, dtype, *tensors):
+    for t in tensors:
+        if t.shape != shape or t.dtype != dtype:
+            raise ValueError(f"{fn}: {dtype} {tuple(shape)} expected, got {t.dtype} {tuple(t.shape)}")
+
+
+def chai_paged_workspace_bytes(B: int, H: int, k: int, T_max: int, d: int = 128) -> int:
+    return int(_lib.chai_paged_workspace_bytes(B, H, k, T_max, d))
+
+
+def alloc_paged_workspace(B: int, H: int, k: int, T_max: int, device="cuda") -> torch.Tensor:
+    """Device scratch for the decode calls on pages; one of the largest sizes serves all smaller calls."""
+    return torch.empty((max(chai_paged_workspace_bytes(B, H, k, T_max), 256),), dtype=torch.uint8, device=device)
+
+
+def chai_paged_append_kv(k_new, v_new, rep_heads, block_table, start, count, k_pages, v_pages, Tn: Optional[int] = None,
+                         k_scales=None, v_scales=None, stream=None):
+    """The first count[b] (None: Tn) of the Tn new tokens k_new, v_new [B,H,>= Tn,d] of every row go to positions start[b]..
+    of its pages k_pages [n_pages,k,page,d], v_pages [n_pages,H,page,d] (uint8: quantised, beside scales
+    [n_pages,streams,page]).  rep_heads [B,k], or None for every head (k = H)."""
+    fn = "chai_paged_append_kv"
+    B, H, k, n_pages, page, max_blocks, d, code = _paged_shapes(
+        fn, k_pages, v_pages, k_scales, v_scales, block_table, k_new.dtype,
+        ((rep_heads, k_pages.shape[1]), (start, start.shape[:1]), (count, start.shape[:1])))
+    nk, nv = k_new.shape[2], v_new.shape[2]
+    Tn = min(nk, nv) if Tn is None else Tn
+    _same(fn, (B, H, nk, d), k_new.dtype, k_new)
+    _same(fn, (B, H, nv, d), k_new.dtype, v_new)
+    _same(fn, (B,), torch.int32, start)
+    _check(fn, _lib.chai_paged_append_kv(_ptr(k_new), _ptr(v_new), nk * d, nv * d, _ptr(rep_heads), _ptr(block_table),
+                                         _ptr(start), _ptr(count), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales),
+                                         _ptr(v_scales), B, H, k, Tn, n_pages, page, max_blocks, d, dtype_code(k_new), code,
+                                         _stream(stream)))
+
+
+def chai_paged_gather_kv(k_pages, v_pages, block_table, start, count, k_out, v_out, k_scales=None, v_scales=None, stream=None):
+    """Positions start[b] .. start[b]+count[b]-1 (None: all Tn) of every row's pages -> the first rows of k_out [B,k,Tn,d] and
+    v_out [B,H,Tn,d] (fp32 or bf16; codes times their scales)."""
+    fn = "chai_paged_gather_kv"
+    B, H, k, n_pages, page, max_blocks, d, code = _paged_shapes(
+        fn, k_pages, v_pages, k_scales, v_scales, block_table, k_out.dtype,
+        ((start, start.shape[:1]), (count, start.shape[:1])))
+    Tn = k_out.shape[2]
+    _same(fn, (B, k, Tn, d), k_out.dtype, k_out)
+    _same(fn, (B, H, Tn, d), k_out.dtype, v_out)
+    _same(fn, (B,), torch.int32, start)
+    _check(fn, _lib.chai_paged_gather_kv(_ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(block_table),
+                                         _ptr(start), _ptr(count), _ptr(k_out), _ptr(v_out), B, H, k, Tn, n_pages, page,
+                                         max_blocks, d, dtype_code(k_out), code, _stream(stream)))
+    return k_out, v_out
+
+
+def chai_paged_decode_attention(q, k_pages, v_pages, head_to_cluster, rep_heads, block_table, seq_lens, T_max: int, scale: float,
+                                out, workspace, k_scales=None, v_scales=None, stream=None):
+    """One clustered decode step of one layer over pages: row b attends to its first seq_lens[b] positions.  Maps as for
+    chai_decode_attention, or both None for a layer without clusters (k = H)."""
+    fn = "chai_paged_decode_attention"
+    B, H, k, n_pages, page, max_blocks, d, code = _paged_shapes(
+        fn, k_pages, v_pages, k_scales, v_scales, block_table, q.dtype,
+        ((head_to_cluster, v_pages.shape[1]), (rep_heads, k_pages.shape[1]), (seq_lens, seq_lens.shape[:1])))
+    _same(fn, (B, H, d), q.dtype, q)
+    _same(fn, (B, H, d), torch.float32, out)
+    _same(fn, (B,), torch.int32, seq_lens)
+    _check(fn, _lib.chai_paged_decode_attention(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales),
+                                                _ptr(head_to_cluster), _ptr(rep_heads), _ptr(block_table), _ptr(seq_lens), B,
+                                                H, k, T_max, n_pages, page, max_blocks, d, dtype_code(q), code, scale,
+                                                _ptr(out), _ptr(workspace), workspace.nbytes, _stream(stream)))
+    return out
+
+
+def chai_paged_decode_step(q, k_new, v_new, k_pages, v_pages, head_to_cluster, rep_heads, block_table, seq_lens, T_max: int,
+                           scale: float, out, workspace, k_scales=None, v_scales=None, stream=None):
+    """Cache growth + attention in one call: position seq_lens[b]-1 of every row is taken from k_new / v_new [B,H,d]."""
+    fn = "chai_paged_decode_step"
+    B, H, k, n_pages, page, max_blocks, d, code = _paged_shapes(
+        fn, k_pages, v_pages, k_scales, v_scales, block_table, q.dtype,
+        ((head_to_cluster, v_pages.shape[1]), (rep_heads, k_pages.shape[1]), (seq_lens, seq_lens.shape[:1])))
+    _same(fn, (B, H, d), q.dtype, q, k_new, v_new)
+    _same(fn, (B, H, d), torch.float32, out)
+    _same(fn, (B,), torch.int32, seq_lens)
+    _check(fn, _lib.chai_paged_decode_step(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales),
+                                           _ptr(v_scales), _ptr(head_to_cluster), _ptr(rep_heads), _ptr(block_table),
+                                           _ptr(seq_lens), B, H, k, T_max, n_pages, page, max_blocks, d, dtype_code(q), code,
+                                           scale, _ptr(out), _ptr(workspace), workspace.nbytes, _stream(stream)))
+    return out
 
 
 class _Binding(types.ModuleType):

@@ -21,6 +21,7 @@ SOURCES = {
     "api.hip": [],
     "decode.hip": [],
     "cache.hip": [],
+    "paged.hip": [],
     # the softmax bookkeeping never sees NaNs (masked scores are -inf): drop the NaN-quieting copies around max.
     # Matrix results in ordinary registers: the accumulation half belongs to the accumulators the source names.
     # Uniform branches stay branches: as flags they make the count of outstanding loads a guess.

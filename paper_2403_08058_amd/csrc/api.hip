@@ -557,4 +557,135 @@ int chai_dense_prefill_attention(const void *q, const void *k_cache, const void 
                                      out, workspace, true, KernelEvents{}, static_cast<hipStream_t>(stream)));
 }
 
+// Checks common to the calls on pages, and what the kernels are told of them.
+static int check_pages(const void *k_pages, const void *v_pages, const float *k_scales, const float *v_scales, const int32_t *table, int B,
+                       int H, int k, bool maps, int n_pages, int page, int max_blocks, int d, int dtype, int cache_dtype, PagedShape *sh,
+                       PagedPages *pg)
+{
+    if (!k_pages || !v_pages || !table) return CHAI_ERR_NULL;
+    if (bad_dtype(dtype) || (cache_dtype != dtype && cache_dtype != CHAI_E4M3)) return CHAI_ERR_DTYPE;
+    if (cache_dtype == CHAI_E4M3 && (!k_scales || !v_scales)) return CHAI_ERR_NULL;
+    if (B < 0 || H < 1 || k < 1 || k > H || (!maps && k != H) || n_pages < 1 || page < 8 || page % 8 != 0 || max_blocks < 1 || d < 1)
+        return CHAI_ERR_SHAPE;
+    if (d != kHeadDim || B > kMaxPagedBatch || (long long)H + k > kMaxGridYZ || page > kMaxPagedTokens ||
+        (unsigned long long)n_pages * (unsigned long long)H >= (1ull << 32) / (unsigned int)page)
+        return CHAI_ERR_UNSUPPORTED;
+    if (!aligned16(k_pages) || !aligned16(v_pages)) return CHAI_ERR_ALIGN;
+    sh->table = table;
+    sh->B = B;
+    sh->H = H;
+    sh->k = k;
+    sh->n_pages = n_pages;
+    sh->page = page;
+    sh->max_blocks = max_blocks;
+    set_page_division(sh);
+    pg->k = static_cast<const char *>(k_pages);
+    pg->v = static_cast<const char *>(v_pages);
+    pg->k_scales = k_scales;
+    pg->v_scales = v_scales;
+    return CHAI_OK;
+}
+
+static int check_paged_decode(const void *q, const int32_t *h2c, const int32_t *rep, const int32_t *lens, int T_max, const float *out,
+                              const void *workspace, size_t workspace_bytes, PagedShape *sh, PagedPlan *plan)
+{
+    if (!q || !lens || !out || !h2c != !rep) return CHAI_ERR_NULL;
+    if (T_max < 1 || (long long)sh->max_blocks * sh->page < T_max) return CHAI_ERR_SHAPE;
+    if (T_max > kMaxPagedTokens || (long long)sh->B * sh->H * T_max >= (1ll << 35)) return CHAI_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(out)) return CHAI_ERR_ALIGN;
+    sh->lens = lens;
+    sh->T_max = T_max;
+    *plan = make_paged_plan(sh->B, sh->H, sh->k, T_max);
+    if (sh->B > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < plan->bytes))
+        return CHAI_ERR_WORKSPACE;
+    return CHAI_OK;
+}
+
+size_t chai_paged_workspace_bytes(int B, int H, int k, int T_max, int d)
+{
+    if (B < 0 || B > kMaxPagedBatch || H < 1 || k < 1 || k > H || (long long)H + k > kMaxGridYZ || T_max < 1 || T_max > kMaxPagedTokens ||
+        d != kHeadDim || (long long)B * H * T_max >= (1ll << 35))
+        return 0;
+    return B == 0 ? 256 : make_paged_plan(B, H, k, T_max).bytes;
+}
+
+int chai_paged_append_kv(const void *k_new, const void *v_new, int64_t k_head_stride, int64_t v_head_stride,
+                         const int32_t *rep_heads, const int32_t *block_table, const int32_t *start, const int32_t *count,
+                         void *k_pages, void *v_pages, float *k_scales, float *v_scales, int B, int H, int k, int Tn,
+                         int n_pages, int page, int max_blocks, int d, int dtype, int cache_dtype, void *stream)
+{
+    if (!k_new || !v_new || !start) return CHAI_ERR_NULL;
+    PagedShape sh;
+    PagedPages pg;
+    const int st = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, B, H, k, rep_heads != nullptr, n_pages, page,
+                               max_blocks, d, dtype, cache_dtype, &sh, &pg);
+    if (st != CHAI_OK) return st;
+    if (Tn < 0 || k_head_stride < (int64_t)Tn * d || v_head_stride < (int64_t)Tn * d || (k_head_stride & 7) || (v_head_stride & 7))
+        return CHAI_ERR_SHAPE;
+    if (Tn > kMaxPagedTokens) return CHAI_ERR_UNSUPPORTED;
+    if (!aligned16(k_new) || !aligned16(v_new)) return CHAI_ERR_ALIGN;
+    if (B == 0 || Tn == 0) return CHAI_OK;
+    return hip_status(launch_paged_append(sh, pg, k_new, v_new, k_head_stride, v_head_stride, rep_heads, start, count, Tn, dtype,
+                                          cache_dtype, static_cast<hipStream_t>(stream)));
+}
+
+int chai_paged_gather_kv(const void *k_pages, const void *v_pages, const float *k_scales, const float *v_scales,
+                         const int32_t *block_table, const int32_t *start, const int32_t *count, void *k_out, void *v_out,
+                         int B, int H, int k, int Tn, int n_pages, int page, int max_blocks, int d, int dtype,
+                         int cache_dtype, void *stream)
+{
+    if (!start || !k_out || !v_out) return CHAI_ERR_NULL;
+    PagedShape sh;
+    PagedPages pg;
+    const int st = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, B, H, k, true, n_pages, page, max_blocks, d, dtype,
+                               cache_dtype, &sh, &pg);
+    if (st != CHAI_OK) return st;
+    if (Tn < 0) return CHAI_ERR_SHAPE;
+    if (Tn > kMaxPagedTokens) return CHAI_ERR_UNSUPPORTED;
+    if (!aligned16(k_out) || !aligned16(v_out)) return CHAI_ERR_ALIGN;
+    if (B == 0 || Tn == 0) return CHAI_OK;
+    return hip_status(launch_paged_gather(sh, pg, start, count, k_out, v_out, Tn, dtype, cache_dtype, static_cast<hipStream_t>(stream)));
+}
+
+int chai_paged_decode_attention(const void *q, const void *k_pages, const void *v_pages, const float *k_scales,
+                                const float *v_scales, const int32_t *head_to_cluster, const int32_t *rep_heads,
+                                const int32_t *block_table, const int32_t *seq_lens, int B, int H, int k, int T_max, int n_pages,
+                                int page, int max_blocks, int d, int dtype, int cache_dtype, float scale, float *out,
+                                void *workspace, size_t workspace_bytes, void *stream)
+{
+    PagedShape sh;
+    PagedPages pg;
+    PagedPlan plan;
+    int st = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, B, H, k, head_to_cluster || rep_heads, n_pages, page, max_blocks,
+                         d, dtype, cache_dtype, &sh, &pg);
+    if (st == CHAI_OK)
+        st = check_paged_decode(q, head_to_cluster, rep_heads, seq_lens, T_max, out, workspace, workspace_bytes, &sh, &plan);
+    if (st != CHAI_OK || B == 0) return st;
+    return hip_status(launch_paged_attention(sh, pg, q, dtype, cache_dtype, head_to_cluster, rep_heads, scale, out, workspace, plan,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+int chai_paged_decode_step(const void *q, const void *k_new, const void *v_new, void *k_pages, void *v_pages, float *k_scales,
+                           float *v_scales, const int32_t *head_to_cluster, const int32_t *rep_heads,
+                           const int32_t *block_table, const int32_t *seq_lens, int B, int H, int k, int T_max, int n_pages,
+                           int page, int max_blocks, int d, int dtype, int cache_dtype, float scale, float *out,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!k_new || !v_new) return CHAI_ERR_NULL;
+    PagedShape sh;
+    PagedPages pg;
+    PagedPlan plan;
+    int st = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, B, H, k, head_to_cluster || rep_heads, n_pages, page, max_blocks,
+                         d, dtype, cache_dtype, &sh, &pg);
+    if (st == CHAI_OK)
+        st = check_paged_decode(q, head_to_cluster, rep_heads, seq_lens, T_max, out, workspace, workspace_bytes, &sh, &plan);
+    if (st != CHAI_OK) return st;
+    if (!aligned16(k_new) || !aligned16(v_new)) return CHAI_ERR_ALIGN;
+    if (B == 0) return CHAI_OK;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const int e = launch_paged_append(sh, pg, k_new, v_new, kHeadDim, kHeadDim, rep_heads, nullptr, nullptr, 1, dtype, cache_dtype, s);
+    if (e != (int)hipSuccess) return CHAI_ERR_HIP;
+    return hip_status(launch_paged_attention(sh, pg, q, dtype, cache_dtype, head_to_cluster, rep_heads, scale, out, workspace, plan, s));
+}
+
 }  // extern "C"

@@ -1,6 +1,6 @@
 // K-cache pruning and cache growth (Section 3.5: after membership is fixed only the representatives' keys are
 // kept; all values are kept).  Pure 16-byte copies: bit-exact by construction, bound by HBM bandwidth.
-#include "chai_internal.h"
+#include "chai_rows.h"
 
 #include <hip/hip_ext.h>
 
@@ -71,68 +71,6 @@ __global__ __launch_bounds__(64) void append_kernel(const uint4 *__restrict__ k_
 // subnormals, largest finite value 448) with one fp32 scale per row: scale = amax / 448, code = nearest E4M3
 // value (ties to even) of x * (448 / amax), all in fp32; an all-zero row gets scale 0 and codes 0.
 // ---------------------------------------------------------------------------------------------------------
-
-// E4M3 codes of four values of at most 448 (the clamp leaves no NaN): the hardware's conversion (nearest, ties to even, subnormals
-// kept), two at a time.  It gives the code that integer arithmetic on the bits gave for all 2 277 507 074 fp32 numbers of that size.
-// Those, some fifteen instructions each, were what the kernel waited for.
-__device__ __forceinline__ unsigned int e4m3_codes(float a, float b, float c, float d)
-{
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (unsigned int)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
-}
-
-// max over the sixteen lanes of a DPP row, in every one of them
-template <int CTRL>
-__device__ __forceinline__ float dpp_max(float x)
-{
-    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false)));
-}
-
-// Sixteen lanes quantise one row, eight elements each (x): returns the eight codes of this lane (two words) and the
-// row's scale.  All sixteen lanes of the group must call it together.
-struct Piece {
-    float x[8];
-};
-template <bool BF16>
-__device__ __forceinline__ Piece load_piece(const char *row, int piece)
-{
-    Piece p;
-    if (BF16) {
-        const uint4 raw = *reinterpret_cast<const uint4 *>(row + piece * 16);
-        const unsigned int w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p.x[2 * i] = __uint_as_float(w[i] << 16);
-            p.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    } else {
-        const float4 lo = *reinterpret_cast<const float4 *>(row + piece * 32);
-        const float4 hi = *reinterpret_cast<const float4 *>(row + piece * 32 + 16);
-        p.x[0] = lo.x; p.x[1] = lo.y; p.x[2] = lo.z; p.x[3] = lo.w;
-        p.x[4] = hi.x; p.x[5] = hi.y; p.x[6] = hi.z; p.x[7] = hi.w;
-    }
-    return p;
-}
-__device__ __forceinline__ uint2 quantize_piece(const Piece &p, float &scale)
-{
-    float amax = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(p.x[i]));
-    amax = dpp_max<0xB1>(amax);                      // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
-    amax = dpp_max<0x4E>(amax);
-    amax = dpp_max<0x141>(amax);
-    amax = dpp_max<0x140>(amax);
-    if (amax == 0.f) {
-        scale = 0.f;
-        return make_uint2(0u, 0u);
-    }
-    scale = amax / 448.0f;
-    const float inv = 448.0f / amax;
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(p.x[i] * inv, -448.0f), 448.0f);
-    return make_uint2(e4m3_codes(y[0], y[1], y[2], y[3]), e4m3_codes(y[4], y[5], y[6], y[7]));
-}
 
 // grid ceil(n_rows / (16 rows)), 256 threads: sixteen lanes per row, sixteen rows at a time, four times (once for fp32, whose rows
 // are twice as long), all requested at once.

@@ -135,6 +135,36 @@ int launch_project_qk(const void *x, const void *w_q, const void *w_k, const int
                       int D, void *q_out, void *k_compact, int pos0, int Tc_cap, const KernelEvents &ev,
                       hipStream_t stream);
 
+// Caches in pages.  rows of either kind: [n_pages, streams, page, 128], streams = k for keys and H for values.
+struct PagedShape {
+    const int32_t *table = nullptr;      // [B, max_blocks]: page of positions [i * page, (i + 1) * page) of a row
+    const int32_t *lens = nullptr;       // [B]
+    int B = 0, H = 0, k = 0, T_max = 0, n_pages = 0, page = 0, max_blocks = 0;
+    int div_shift = 0;                   // n / page without a division (set_page_division)
+    unsigned int div_mul = 0;
+};
+struct PagedPages {
+    const char *k = nullptr, *v = nullptr;
+    const float *k_scales = nullptr, *v_scales = nullptr;
+};
+// Regions of the workspace, upper bounds over the types.
+struct PagedPlan {
+    size_t off_recs, off_partial, bytes;
+};
+constexpr int kMaxPagedBatch = 4096;     // rows: two levels of 64 lanes add up their lengths
+constexpr int kMaxPagedTokens = 1 << 24;
+PagedPlan make_paged_plan(int B, int H, int k, int T_max);
+void set_page_division(PagedShape *sh);
+// h2c = rep = NULL: every head its own cluster (k = H)
+int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const void *q, int dtype, int cache_dtype, const int32_t *h2c,
+                           const int32_t *rep, float scale, float *out, void *workspace, const PagedPlan &plan, hipStream_t stream);
+// start = NULL: the one new token of every row, at its last position (sh.lens)
+int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *k_new, const void *v_new, int64_t k_stride,
+                        int64_t v_stride, const int32_t *rep, const int32_t *start, const int32_t *count, int Tn, int dtype,
+                        int cache_dtype, hipStream_t stream);
+int launch_paged_gather(const PagedShape &sh, const PagedPages &pg, const int32_t *start, const int32_t *count, void *k_out, void *v_out,
+                        int Tn, int dtype, int cache_dtype, hipStream_t stream);
+
 // 32 x 32 x 16 products alone: `rounds` rounds of 8 of them per wave on operands taken from buf; flops of one launch
 int launch_mfma_probe(const void *buf, size_t bytes, int rounds, float *sink, const KernelEvents &ev, hipStream_t stream);
 double mfma_probe_flops(int rounds);

@@ -8,7 +8,7 @@
 //
 // Method: attention definition of Section 2; one score computation per cluster with the representative's
 // query and keys, shared by the member heads, each applying it to its own values (Sections 3.4-3.5, Fig. 3).
-#include "chai_internal.h"
+#include "chai_rows.h"
 
 #include <hip/hip_ext.h>
 
@@ -18,26 +18,8 @@ namespace chai {
 
 namespace {
 
-constexpr int kUnroll = 8;        // 16-byte loads per lane in one batch
 constexpr int kScoreWaves = 4;    // waves per workgroup of the score kernel ...
 constexpr int kScoreBatches = 2;  // ... each with this many batches in flight
-
-// storage types of the caches inside this file: CHAI_F32, CHAI_BF16, and 8-bit E4M3 codes with per-row scales
-constexpr int DT_F32 = CHAI_F32, DT_BF16 = CHAI_BF16, DT_E4M3 = 2;
-template <int DT>
-struct Elem {
-    static constexpr int BYTES = DT == DT_F32 ? 4 : (DT == DT_BF16 ? 2 : 1);
-    static constexpr int EPL = 16 / BYTES;                 // elements per lane per load (16 bytes)
-};
-
-template <int DT>
-struct Tile {
-    static constexpr int EPL = Elem<DT>::EPL;
-    static constexpr int LPR = kHeadDim / EPL;             // lanes per row: 32 (fp32) / 16 (bf16) / 8 (codes)
-    static constexpr int RPW = 64 / LPR;                   // rows per wave load: 2 / 4 / 8
-    static constexpr int BATCH = RPW * kUnroll;            // rows per wave batch: 16 / 32 / 64
-    static constexpr int ROW_BYTES = kHeadDim * Elem<DT>::BYTES;
-};
 
 // Value kernel: a workgroup may take only one of DS column parts of its head's rows (DS = 1: whole rows).
 template <int DT, int DS>
@@ -51,77 +33,6 @@ struct VTile {
     static constexpr int PART_BYTES = ROW_BYTES / DS;
     static_assert(BATCH <= 64, "one lane per row of a batch turns its score into a probability");
 };
-
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ void unpack(const u32x4 &raw, float (&f)[8])
-{
-    // bf16 pairs: the low half-word is the even element; a bf16 is the top half of an fp32
-    f[0] = __uint_as_float(raw.x << 16); f[1] = __uint_as_float(raw.x & 0xffff0000u);
-    f[2] = __uint_as_float(raw.y << 16); f[3] = __uint_as_float(raw.y & 0xffff0000u);
-    f[4] = __uint_as_float(raw.z << 16); f[5] = __uint_as_float(raw.z & 0xffff0000u);
-    f[6] = __uint_as_float(raw.w << 16); f[7] = __uint_as_float(raw.w & 0xffff0000u);
-}
-
-// sixteen E4M3 codes: the hardware conversion widens two bytes of a word at a time (exact)
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void unpack(const u32x4 &raw, float (&f)[16])
-{
-    const unsigned int w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false);
-        const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-        f[4 * i + 0] = lo.x; f[4 * i + 1] = lo.y; f[4 * i + 2] = hi.x; f[4 * i + 3] = hi.y;
-    }
-}
-
-__device__ __forceinline__ void unpack(const u32x4 &raw, float (&f)[4])
-{
-    f[0] = __uint_as_float(raw.x); f[1] = __uint_as_float(raw.y);
-    f[2] = __uint_as_float(raw.z); f[3] = __uint_as_float(raw.w);
-}
-
-// The caches are read exactly once per call: non-temporal loads keep them from displacing the small,
-// re-read score and statistics buffers in L2 (and measure ~10% faster than plain loads on a pure stream).
-__device__ __forceinline__ u32x4 stream16(const char *p)
-{
-    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
-}
-
-// x + (x of the lane selected by a DPP control) -- cross-lane adds inside a 16-lane DPP row
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x)
-{
-    int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false);
-    return x + __int_as_float(y);
-}
-
-// Sum over the lanes that share a row; every one of them ends up with the total.
-template <int DT>
-__device__ __forceinline__ float row_sum(float x)
-{
-    x = dpp_add<0xB1>(x);    // quad_perm [1,0,3,2]: lane ^ 1
-    x = dpp_add<0x4E>(x);    // quad_perm [2,3,0,1]: lane ^ 2
-    x = dpp_add<0x141>(x);   // row_half_mirror: other quad of the same 8 lanes (rows of 8-bit codes end here)
-    if (DT != DT_E4M3) x = dpp_add<0x140>(x);   // row_mirror: other half of the same 16 lanes
-    if (DT == DT_F32) x += __shfl_xor(x, 16);   // fp32 rows span 32 lanes
-    return x;
-}
-
-__device__ __forceinline__ float wave_max(float x)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-    return x;
-}
-
-__device__ __forceinline__ float wave_sum(float x)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    return x;
-}
 
 // ---------------------------------------------------------------------------------------------------------
 // Value kernel: out[b][h] = sum_t p_c[t] * V[b][h][t], c = cluster of h.  grid = (n_cp, H, B).

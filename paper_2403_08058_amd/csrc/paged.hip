@@ -1,0 +1,607 @@
+// Caches in pages: requests of different lengths share one pool of pages, a table names every row's pages in order.  Writing new
+// rows into pages (as they are, or as 8-bit codes), attention of one new token per request over its pages, reading pages back.
+//
+// Method: Sections 2 and 3.4-3.5 as in the contiguous kernels (one score computation per cluster, shared by the members); only
+// where a cached row lies is different.  A page holds `page` consecutive positions of every stream: rows [n_pages, streams, page].
+#include "chai_rows.h"
+
+#include <hip/hip_ext.h>
+
+namespace chai {
+
+namespace {
+
+constexpr int kWaves = kBlock / 64;
+
+// `workers` waves take at least `least` units each
+struct PagedSplit {
+    unsigned int workers, least;
+};
+
+__device__ __forceinline__ int block_of(const PagedShape &sh, int pos)
+{
+    return (int)((__umulhi((unsigned int)pos, sh.div_mul) + (unsigned int)pos) >> sh.div_shift);
+}
+
+// positions of row b that are attended to
+__device__ __forceinline__ int row_len(const PagedShape &sh, int b) { return min(max(sh.lens[b], 0), sh.T_max); }
+
+// ---------------------------------------------------------------------------------------------------------
+// How the work of a ragged batch is dealt out.  A unit is one batch of a wave's loads (16 rows of fp32, 32 of bf16, 64 of codes);
+// the units of all streams of all rows are laid end to end, (row, stream, unit), and worker w, one wave, takes the quota units from
+// w * quota on: every wave streams the same number of bytes whatever the lengths are, which only the device knows.  Each wave adds up
+// the rows' units for itself (64 rows per load and six steps of a scan).
+// ---------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ unsigned int wave_scan(unsigned int x, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned int y = (unsigned int)__shfl_up((int)x, o);
+        x += lane >= o ? y : 0u;
+    }
+    return x;
+}
+
+template <int U>
+struct Deal {
+    unsigned int incl, mine;                 // lane l: units of one stream over rows up to and with its own, and of its own rows
+    int span;                                // rows per lane
+    unsigned int total;                      // units of one stream over all rows
+
+    __device__ __forceinline__ static unsigned int units(const PagedShape &sh, int b) { return (unsigned int)(row_len(sh, b) + U - 1) / U; }
+
+    __device__ __forceinline__ Deal(const PagedShape &sh, int lane)
+    {
+        span = (sh.B + 63) / 64;
+        mine = 0u;
+        for (int i = 0; i < span; ++i) {
+            const int b = lane * span + i;
+            mine += b < sh.B ? units(sh, min(b, sh.B - 1)) : 0u;
+        }
+        incl = wave_scan(mine, lane);
+        total = (unsigned int)__builtin_amdgcn_readlane((int)incl, 63);
+    }
+
+    __device__ __forceinline__ unsigned int quota(int streams, const PagedSplit &sp) const
+    {
+        const unsigned int n = total * (unsigned int)streams;
+        return max((n + sp.workers - 1) / sp.workers, sp.least);
+    }
+
+    // units of one stream before row b
+    __device__ __forceinline__ unsigned int before(const PagedShape &sh, int b, int lane) const
+    {
+        const int l = b / span;
+        unsigned int p = (unsigned int)__builtin_amdgcn_readlane((int)(incl - mine), l);
+        if (span > 1) {
+            const int r = l * span + lane;
+            const unsigned int u = lane < span && r < b ? units(sh, min(r, sh.B - 1)) : 0u;
+            p += (unsigned int)__builtin_amdgcn_readlane((int)wave_scan(u, lane), 63);
+        }
+        return p;
+    }
+
+    // the row that unit y of one stream falls into (y < total), and the units before it
+    __device__ __forceinline__ int row_at(const PagedShape &sh, unsigned int y, int lane, unsigned int *first) const
+    {
+        const int l = __ffsll((long long)__ballot(incl > y)) - 1;
+        unsigned int p = (unsigned int)__builtin_amdgcn_readlane((int)(incl - mine), l);
+        int b = l * span;
+        if (span > 1) {
+            const int r = b + lane;
+            const unsigned int u = lane < span && r < sh.B ? units(sh, min(r, sh.B - 1)) : 0u;
+            const unsigned int in = wave_scan(u, lane);
+            const int i = __ffsll((long long)__ballot(p + in > y)) - 1;
+            p += (unsigned int)__builtin_amdgcn_readlane((int)(in - u), i);
+            b += i;
+        }
+        *first = p;
+        return b;
+    }
+};
+
+// the query as the lane multiplies it: elements cg * EPL .. of its representative's row (beside codes q has a type of its own)
+template <int DT>
+__device__ __forceinline__ void load_query(const char *q, size_t row, int cg, int q_dtype, float (&qf)[Tile<DT>::EPL])
+{
+    if constexpr (DT == DT_E4M3) {
+        const char *p = q + row * (size_t)(kHeadDim * (q_dtype == CHAI_BF16 ? 2 : 4));
+        if (q_dtype == CHAI_BF16) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                float f[8];
+                unpack(*reinterpret_cast<const u32x4 *>(p + cg * 32 + part * 16), f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) qf[part * 8 + e] = f[e];
+            }
+        } else {
+#pragma unroll
+            for (int part = 0; part < 4; ++part) {
+                float f[4];
+                unpack(*reinterpret_cast<const u32x4 *>(p + cg * 64 + part * 16), f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[part * 4 + e] = f[e];
+            }
+        }
+    } else {
+        unpack(*reinterpret_cast<const u32x4 *>(q + row * Tile<DT>::ROW_BYTES + cg * 16), qf);
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void store_floats(float *p, const float (&f)[N])
+{
+#pragma unroll
+    for (int e = 0; e < N; e += 4) *reinterpret_cast<float4 *>(p + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+}
+
+constexpr float kPagedDown = 0x1p-24f;       // times kMaxPagedTokens weights of at most 1: at most 1
+constexpr float kPagedLarge = 0x1p120f;
+
+// ---------------------------------------------------------------------------------------------------------
+// Attention: one wave streams keys and values of its units together.  With a running reference m (the largest score so far; it moves
+// only when a batch exceeds it, then what has been added up is scaled by exp(old - new)):
+//     s[t] = scale * q . K[t],   acc += exp(s[t] - m) V[t],   l += exp(s[t] - m)
+// A stream that ends inside the wave's units and began there goes to `out` as acc / l; of others acc / l goes to `partial` and (m, l)
+// to `recs` of the wave, two of each (its first units, its last ones), and paged_join_kernel puts them together.
+// A load covers RPW consecutive rows and pages hold multiples of 8, so every load lies in one page: lane i looks up the page of load
+// i % 8 and the loads' bases are uniform.  Rows past the end and of absent pages: the pool's first rows are loaded in their place,
+// their scores are -inf and their values zeroed.
+// ---------------------------------------------------------------------------------------------------------
+template <int DT, bool IDENT>
+__global__ __launch_bounds__(kBlock, 4) void paged_attend_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q,
+                                                                 int q_dtype, const int32_t *__restrict__ h2c,
+                                                                 const int32_t *__restrict__ rep, float scale,
+                                                                 float *__restrict__ partial, float2 *__restrict__ recs,
+                                                                 float *__restrict__ out)
+{
+    using TL = Tile<DT>;
+    constexpr int U = TL::BATCH;
+    __shared__ float p_lds[kWaves][64];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned int worker = blockIdx.x * kWaves + w;
+    const int cg = lane % TL::LPR, rg = lane / TL::LPR;
+    const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
+
+    const Deal<U> deal(sh, lane);
+    const unsigned int quota = deal.quota(sh.H, sp), n_units = deal.total * (unsigned int)sh.H;
+    const unsigned long long x0l = (unsigned long long)worker * quota;
+    if (worker >= sp.workers || x0l >= n_units) return;
+    const unsigned int x0 = (unsigned int)x0l, x1 = min(x0 + quota, n_units);
+    unsigned int first;
+    int b = deal.row_at(sh, x0 / (unsigned int)sh.H, lane, &first);
+    unsigned int n_row = Deal<U>::units(sh, b);
+    int h = (int)((x0 - first * (unsigned int)sh.H) / n_row);
+    unsigned int ua = x0 - first * (unsigned int)sh.H - (unsigned int)h * n_row;
+
+    for (unsigned int x = x0; x < x1;) {
+        const unsigned int ue = min(n_row, ua + (x1 - x));
+        const int len = row_len(sh, b);
+        const int c = IDENT ? h : min(max(h2c[(size_t)b * sh.H + h], 0), sh.k - 1);
+        const int r = IDENT ? h : min(max(rep[(size_t)b * sh.k + c], 0), sh.H - 1);
+        const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
+        float qf[TL::EPL];
+        load_query<DT>(q, (size_t)b * sh.H + r, cg, q_dtype, qf);
+
+        float acc[TL::EPL], m_ref, l_run, down = 1.f;
+        for (;;) {
+            // page of load (lane % 8) of unit u, -1 past the end of the row and of the units
+            auto look = [&](unsigned int u) {
+                const int row = (int)(u * U) + (lane & 7) * TL::RPW;
+                const int at = table[min(block_of(sh, min(row, sh.T_max - 1)), sh.max_blocks - 1)];
+                return u < ue && row < len && (unsigned int)at < (unsigned int)sh.n_pages ? at : -1;
+            };
+            auto row_of = [&](int at, unsigned int u, int streams, int s) {
+                const int row = (int)(u * U) + (lane & 7) * TL::RPW;
+                return at < 0 ? 0u : (unsigned int)(at * streams + s) * (unsigned int)sh.page + (unsigned int)(row - block_of(sh, row) * sh.page);
+            };
+            auto request = [&](u32x4 (&buf)[kUnroll], const char *rows, unsigned int row) {
+#pragma unroll
+                for (int i = 0; i < kUnroll; ++i) {
+                    const char *base = rows + (size_t)(unsigned int)__builtin_amdgcn_readlane((int)row, i) * TL::ROW_BYTES;
+                    buf[i] = stream16(base + lane_off);
+                }
+            };
+            u32x4 kb[kUnroll], vb[kUnroll];
+            float ks = 1.f, vs = 1.f;
+            int at = look(ua), at1 = look(ua + 1);
+            unsigned int krow = row_of(at, ua, sh.k, c), vrow = row_of(at, ua, sh.H, h);
+            request(kb, pg.k, krow);
+            if (DT == DT_E4M3) ks = pg.k_scales[krow + (at < 0 ? 0 : rg)];
+            request(vb, pg.v, vrow);
+            if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at < 0 ? 0 : rg)];
+#pragma unroll
+            for (int e = 0; e < TL::EPL; ++e) acc[e] = 0.f;
+            m_ref = -INFINITY;
+            l_run = 0.f;
+            for (unsigned int u = ua; u < ue; ++u) {
+                const int at2 = look(u + 2);
+                float mine = 0.f;
+#pragma unroll
+                for (int i = 0; i < kUnroll; ++i) {
+                    float f[TL::EPL];
+                    unpack(kb[i], f);
+                    float dot = 0.f;
+#pragma unroll
+                    for (int e = 0; e < TL::EPL; ++e) dot = fmaf(qf[e], f[e], dot);
+                    dot = row_sum<DT>(dot);
+                    mine = cg == i ? dot : mine;
+                }
+                // lane cg < 8 of a lane group owns the row of load cg: row rg + cg * RPW of the unit
+                const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
+                const float sv = there ? (DT == DT_E4M3 ? (scale * ks) * mine : scale * mine) : -INFINITY;
+                krow = row_of(at1, u + 1, sh.k, c);
+                request(kb, pg.k, krow);
+                if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
+                if (__any(sv > m_ref)) {
+                    const float m_new = fmaxf(m_ref, wave_max(sv));
+                    const float f = __expf(m_ref - m_new);
+#pragma unroll
+                    for (int e = 0; e < TL::EPL; ++e) acc[e] *= f;
+                    l_run *= f;
+                    m_ref = m_new;
+                }
+                const float p = __expf(sv - (m_ref == -INFINITY ? 0.f : m_ref)) * down;
+                l_run += p;
+                if (cg < kUnroll) p_lds[w][rg * kUnroll + cg] = DT == DT_E4M3 ? (there ? p * vs : 0.f) : p;
+                __builtin_amdgcn_wave_barrier();
+                float pv[kUnroll];
+#pragma unroll
+                for (int i = 0; i < kUnroll; ++i) pv[i] = p_lds[w][rg * kUnroll + i];
+                __builtin_amdgcn_wave_barrier();
+                if (!__all(there || cg >= kUnroll)) {
+                    const unsigned long long have = __ballot(there) >> (rg * TL::LPR);
+#pragma unroll
+                    for (int i = 0; i < kUnroll; ++i)
+                        if (!((have >> i) & 1ull)) vb[i] = u32x4{0u, 0u, 0u, 0u};
+                }
+#pragma unroll
+                for (int i = 0; i < kUnroll; ++i) {
+                    float f[TL::EPL];
+                    unpack(vb[i], f);
+#pragma unroll
+                    for (int e = 0; e < TL::EPL; ++e) acc[e] = fmaf(pv[i], f[e], acc[e]);
+                }
+                vrow = row_of(at1, u + 1, sh.H, h);
+                request(vb, pg.v, vrow);
+                if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
+                at = at1;
+                at1 = at2;
+            }
+            // lane groups; sums beyond the largest float (the quotient is not) are taken again with smaller weights
+            bool large = false;
+#pragma unroll
+            for (int e = 0; e < TL::EPL; ++e) {
+#pragma unroll
+                for (int o = TL::LPR; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
+                large = large || !(fabsf(acc[e]) <= kPagedLarge);
+            }
+            if (!__any(large) || down != 1.f) break;
+            down = kPagedDown;
+        }
+        const float l = wave_sum(l_run);
+#pragma unroll
+        for (int e = 0; e < TL::EPL; ++e) acc[e] = l == 0.f ? 0.f : acc[e] / l;
+        if (ua == 0 && ue == n_row) {
+            if (rg == 0) store_floats(out + ((size_t)b * sh.H + h) * kHeadDim + cg * TL::EPL, acc);
+        } else {
+            const size_t slot = 2 * (size_t)worker + (x == x0 ? 0 : 1);
+            if (rg == 0) store_floats(partial + slot * kHeadDim + cg * TL::EPL, acc);
+            if (lane == 0) recs[slot] = make_float2(m_ref, l / down);
+        }
+        x += ue - ua;
+        ua = 0;
+        if (++h == sh.H) {
+            h = 0;
+            do ++b;
+            while (b < sh.B && (n_row = Deal<U>::units(sh, b)) == 0u);
+        }
+    }
+}
+
+// Streams that several waves took: out = mean of their parts, each weighed by its sum of exponentials times exp(its reference - the
+// largest).  A wave per (row, head), two columns per lane; streams that one wave took are left alone, rows without a position get 0.
+template <int U>
+__global__ __launch_bounds__(kBlock) void paged_join_kernel(PagedShape sh, PagedSplit sp, const float *__restrict__ partial,
+                                                            const float2 *__restrict__ recs, float *__restrict__ out)
+{
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = blockIdx.x * kWaves + w, b = blockIdx.y;
+    if (h >= sh.H) return;
+    float2 *o = reinterpret_cast<float2 *>(out + ((size_t)b * sh.H + h) * kHeadDim) + lane;
+    const unsigned int n_row = Deal<U>::units(sh, b);
+    if (n_row == 0u) {
+        *o = make_float2(0.f, 0.f);
+        return;
+    }
+    const Deal<U> deal(sh, lane);
+    const unsigned int quota = deal.quota(sh.H, sp);
+    const unsigned int a = deal.before(sh, b, lane) * (unsigned int)sh.H + (unsigned int)h * n_row;
+    const unsigned int wa = a / quota, n = (a + n_row - 1) / quota - wa + 1;
+    if (n == 1) return;
+    auto slot = [&](unsigned int i) { return 2 * (size_t)(wa + i) + (i == 0 && a != wa * quota ? 1 : 0); };
+    float M = -INFINITY;
+    for (unsigned int i = lane; i < n; i += 64) M = fmaxf(M, recs[slot(i)].x);
+    M = wave_max(M);
+    // (a part whose scores are all -inf has the sum 0, one with NaN among them NaN)
+    auto weight = [&](const float2 &rc) { return rc.x == -INFINITY ? rc.y : __expf(rc.x - M) * rc.y; };
+    float l = 0.f;
+    for (unsigned int i = lane; i < n; i += 64) l += weight(recs[slot(i)]);
+    l = wave_sum(l);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    float2 sum = make_float2(0.f, 0.f);
+    for (unsigned int i0 = 0; i0 < n; i0 += 64) {
+        const float wt = i0 + lane < n ? weight(recs[slot(i0 + lane)]) * inv : 0.f;
+        const unsigned int here = min(n - i0, 64u);
+        for (unsigned int i = 0; i < here; i += 8) {
+            float2 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[j] = reinterpret_cast<const float2 *>(partial + slot(i0 + min(i + j, here - 1)) * kHeadDim)[lane];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float wj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), (int)min(i + j, 63u)));
+                if (i + j < here) {
+                    sum.x = fmaf(wj, v[j].x, sum.x);
+                    sum.y = fmaf(wj, v[j].y, sum.y);
+                }
+            }
+        }
+    }
+    *o = sum;
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// New rows into pages, and pages into contiguous rows.  A workgroup takes kMoveRows rows of one request: TB consecutive tokens (a
+// power of two, so that one new token of many streams fills a workgroup as well) of kMoveRows / TB streams; streams are the k key
+// slots, then the H value heads.  Sixteen lanes per row, eight elements each, all rows requested at once.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kMoveUnroll = 4, kMoveRows = kBlock / 16 * kMoveUnroll;
+
+struct MovedRow {
+    bool there, zero;                        // in a page; wanted but in none
+    unsigned int at;                         // row among the pool's rows of its kind
+    int stream, token;
+};
+
+__device__ __forceinline__ MovedRow moved_row(const PagedShape &sh, const int32_t *start, const int32_t *count, int Tn, int shift, int local, int b)
+{
+    MovedRow m;
+    m.token = (int)(blockIdx.x << shift) + (local & ((1 << shift) - 1));
+    m.stream = blockIdx.y * (kMoveRows >> shift) + (local >> shift);
+    int n = Tn, first;
+    if (start == nullptr) {                  // the last position of every row
+        first = sh.lens[b] - 1;
+        n = first >= 0 && first < sh.T_max ? 1 : 0;
+    } else {
+        first = start[b];
+        if (count != nullptr) n = min(max(count[b], 0), Tn);
+    }
+    const bool wanted = m.token < n && m.stream < sh.k + sh.H;
+    const int pos = (int)((unsigned int)first + (unsigned int)m.token);
+    const int block = block_of(sh, max(pos, 0));
+    int at = -1;
+    if (wanted && pos >= 0 && block < sh.max_blocks) at = sh.table[(size_t)b * sh.max_blocks + block];
+    m.there = (unsigned int)at < (unsigned int)sh.n_pages;
+    m.zero = wanted && !m.there;
+    const int streams = m.stream < sh.k ? sh.k : sh.H, s = m.stream < sh.k ? m.stream : m.stream - sh.k;
+    m.at = m.there ? (unsigned int)(at * streams + s) * (unsigned int)sh.page + (unsigned int)(pos - block * sh.page) : 0u;
+    return m;
+}
+
+// eight bf16 values as they were before they were widened
+__device__ __forceinline__ uint4 packed(const Piece &p)
+{
+    unsigned int x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (__float_as_uint(p.x[2 * e]) >> 16) | (__float_as_uint(p.x[2 * e + 1]) & 0xffff0000u);
+    return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+template <int DT, bool BF16>
+__global__ __launch_bounds__(kBlock) void paged_append_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ k_new,
+                                                              const char *__restrict__ v_new, long long k_stride, long long v_stride,
+                                                              const int32_t *__restrict__ rep, const int32_t *__restrict__ start,
+                                                              const int32_t *__restrict__ count, int Tn, int shift)
+{
+    const int b = blockIdx.z, piece = threadIdx.x & 15, local = threadIdx.x >> 4;
+    constexpr int kBytes = BF16 ? 2 : 4;
+    MovedRow m[kMoveUnroll];
+    Piece p[kMoveUnroll];
+#pragma unroll
+    for (int i = 0; i < kMoveUnroll; ++i) {
+        m[i] = moved_row(sh, start, count, Tn, shift, local + i * (kBlock / 16), b);
+        if (!m[i].there) continue;
+        const bool key = m[i].stream < sh.k;
+        int h = key ? m[i].stream : m[i].stream - sh.k;
+        if (key && rep != nullptr) h = min(rep[(size_t)b * sh.k + h], sh.H - 1);
+        m[i].there = h >= 0;                 // (a slot without a cluster keeps what it holds)
+        if (m[i].there)
+            p[i] = load_piece<BF16>((key ? k_new : v_new) + (((size_t)b * sh.H + h) * (key ? k_stride : v_stride) + (size_t)m[i].token * kHeadDim) * kBytes, piece);
+    }
+#pragma unroll
+    for (int i = 0; i < kMoveUnroll; ++i) {
+        if (!m[i].there) continue;           // (the same for the sixteen lanes of a row)
+        const bool key = m[i].stream < sh.k;
+        char *rows = const_cast<char *>(key ? pg.k : pg.v);
+        if constexpr (DT == DT_E4M3) {
+            float scale;
+            const uint2 codes = quantize_piece(p[i], scale);
+            reinterpret_cast<uint2 *>(rows)[(size_t)m[i].at * 16 + piece] = codes;
+            if (piece == 0) const_cast<float *>(key ? pg.k_scales : pg.v_scales)[m[i].at] = scale;
+        } else if constexpr (BF16) {
+            reinterpret_cast<uint4 *>(rows)[(size_t)m[i].at * 16 + piece] = packed(p[i]);
+        } else {
+            store_floats(reinterpret_cast<float *>(rows) + (size_t)m[i].at * kHeadDim + piece * 8, p[i].x);
+        }
+    }
+}
+
+__device__ __forceinline__ unsigned int bf16_pair(float lo, float hi)
+{
+    // nearest, ties to even; NaN stays NaN
+    auto bits = [](float x) {
+        const unsigned int u = __float_as_uint(x);
+        return x != x ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+    };
+    return bits(lo) | (bits(hi) << 16);
+}
+
+template <int DT, bool BF16>
+__global__ __launch_bounds__(kBlock) void paged_gather_kernel(PagedShape sh, PagedPages pg, const int32_t *__restrict__ start,
+                                                              const int32_t *__restrict__ count, char *__restrict__ k_out,
+                                                              char *__restrict__ v_out, int Tn, int shift)
+{
+    const int b = blockIdx.z, piece = threadIdx.x & 15, local = threadIdx.x >> 4;
+    constexpr int kBytes = BF16 ? 2 : 4;
+    MovedRow m[kMoveUnroll];
+    Piece p[kMoveUnroll];
+#pragma unroll
+    for (int i = 0; i < kMoveUnroll; ++i) {
+        m[i] = moved_row(sh, start, count, Tn, shift, local + i * (kBlock / 16), b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[i].x[e] = 0.f;
+        if (!m[i].there) continue;
+        const bool key = m[i].stream < sh.k;
+        const char *rows = key ? pg.k : pg.v;
+        if constexpr (DT == DT_E4M3) {
+            const uint2 codes = reinterpret_cast<const uint2 *>(rows)[(size_t)m[i].at * 16 + piece];
+            const float scale = (key ? pg.k_scales : pg.v_scales)[m[i].at];
+            const unsigned int x[2] = {codes.x, codes.y};
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[e], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[e], true);
+                p[i].x[4 * e] = lo.x * scale;
+                p[i].x[4 * e + 1] = lo.y * scale;
+                p[i].x[4 * e + 2] = hi.x * scale;
+                p[i].x[4 * e + 3] = hi.y * scale;
+            }
+        } else {
+            p[i] = load_piece<BF16>(rows + (size_t)m[i].at * (kHeadDim * kBytes), piece);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kMoveUnroll; ++i) {
+        if (!m[i].there && !m[i].zero) continue;
+        const bool key = m[i].stream < sh.k;
+        const int streams = key ? sh.k : sh.H, s = key ? m[i].stream : m[i].stream - sh.k;
+        const size_t row = ((size_t)b * streams + s) * Tn + m[i].token;
+        char *o = key ? k_out : v_out;
+        if constexpr (DT == DT_BF16) {
+            reinterpret_cast<uint4 *>(o)[row * 16 + piece] = packed(p[i]);
+        } else if constexpr (BF16) {
+            const float *x = p[i].x;
+            reinterpret_cast<uint4 *>(o)[row * 16 + piece] = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+        } else {
+            store_floats(reinterpret_cast<float *>(o) + row * kHeadDim + piece * 8, p[i].x);
+        }
+    }
+}
+
+// tokens per workgroup, as a power of two: all of them up to kMoveRows
+int move_shift(int Tn)
+{
+    int shift = 0;
+    while ((1 << shift) < Tn && (1 << shift) < kMoveRows) ++shift;
+    return shift;
+}
+
+dim3 move_grid(const PagedShape &sh, int Tn, int shift)
+{
+    const int streams = kMoveRows >> shift;
+    return dim3((unsigned int)((Tn + (1 << shift) - 1) >> shift), (unsigned int)((sh.k + sh.H + streams - 1) / streams), (unsigned int)sh.B);
+}
+
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+int unit_rows(int cache_dtype) { return cache_dtype == CHAI_F32 ? Tile<DT_F32>::BATCH : (cache_dtype == CHAI_BF16 ? Tile<DT_BF16>::BATCH : Tile<DT_E4M3>::BATCH); }
+
+}  // namespace
+
+constexpr unsigned int kPagedWorkers = 256 * 16;       // waves that fit the CUs beside each other
+constexpr unsigned int kPagedParts = 64;               // most waves of one stream
+
+PagedPlan make_paged_plan(int, int, int, int)
+{
+    PagedPlan pl;
+    pl.off_recs = 0;
+    pl.off_partial = align_up(2 * (size_t)kPagedWorkers * sizeof(float2), 256);
+    pl.bytes = pl.off_partial + 2 * (size_t)kPagedWorkers * kHeadDim * sizeof(float);
+    return pl;
+}
+
+static PagedSplit make_paged_split(int B, int streams, int T_max, int cache_dtype)
+{
+    PagedSplit sp;
+    const int u = unit_rows(cache_dtype);
+    const long long row_units = ((long long)T_max + u - 1) / u, units = row_units * B * streams;
+    sp.workers = (unsigned int)(units < (long long)kPagedWorkers ? units : kPagedWorkers);
+    sp.least = (unsigned int)((row_units + kPagedParts - 1) / kPagedParts);
+    if (sp.least < 2u) sp.least = 2u;
+    return sp;
+}
+
+void set_page_division(PagedShape *sh)
+{
+    // floor(n / page) = (mulhi(n, mul) + n) >> shift for every 0 <= n < 2^31
+    int s = 0;
+    while ((1ll << s) < sh->page) ++s;
+    sh->div_shift = s;
+    sh->div_mul = (unsigned int)((((1ull << s) - (unsigned long long)sh->page) << 32) / (unsigned long long)sh->page + 1ull);
+}
+
+int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const void *q, int dtype, int cache_dtype, const int32_t *h2c,
+                           const int32_t *rep, float scale, float *out, void *workspace, const PagedPlan &plan, hipStream_t stream)
+{
+    float2 *recs = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + plan.off_recs);
+    float *partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.off_partial);
+    const PagedSplit sp = make_paged_split(sh.B, sh.H, sh.T_max, cache_dtype);
+    const dim3 grid((sp.workers + kWaves - 1) / kWaves), block(kBlock);
+    const char *qc = static_cast<const char *>(q);
+    auto go = [&](auto *attend, auto *join) {
+        const hipError_t e = launch_kernel(attend, grid, block, 0, stream, KernelEvents(), sh, pg, sp, qc, dtype, h2c, rep, scale,
+                                           partial, recs, out);
+        if (e != hipSuccess) return (int)e;
+        return (int)launch_kernel(join, dim3((unsigned int)(sh.H + kWaves - 1) / kWaves, (unsigned int)sh.B), block, 0, stream, KernelEvents(), sh,
+                                  sp, partial, recs, out);
+    };
+    const bool ident = h2c == nullptr;
+    if (cache_dtype == CHAI_F32)
+        return ident ? go(paged_attend_kernel<DT_F32, true>, paged_join_kernel<Tile<DT_F32>::BATCH>)
+                     : go(paged_attend_kernel<DT_F32, false>, paged_join_kernel<Tile<DT_F32>::BATCH>);
+    if (cache_dtype == CHAI_BF16)
+        return ident ? go(paged_attend_kernel<DT_BF16, true>, paged_join_kernel<Tile<DT_BF16>::BATCH>)
+                     : go(paged_attend_kernel<DT_BF16, false>, paged_join_kernel<Tile<DT_BF16>::BATCH>);
+    return ident ? go(paged_attend_kernel<DT_E4M3, true>, paged_join_kernel<Tile<DT_E4M3>::BATCH>)
+                 : go(paged_attend_kernel<DT_E4M3, false>, paged_join_kernel<Tile<DT_E4M3>::BATCH>);
+}
+
+int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *k_new, const void *v_new, int64_t k_stride,
+                        int64_t v_stride, const int32_t *rep, const int32_t *start, const int32_t *count, int Tn, int dtype,
+                        int cache_dtype, hipStream_t stream)
+{
+    const int shift = move_shift(Tn);
+    const char *kc = static_cast<const char *>(k_new), *vc = static_cast<const char *>(v_new);
+    auto go = [&](auto *kernel) {
+        return (int)launch_kernel(kernel, move_grid(sh, Tn, shift), dim3(kBlock), 0, stream, KernelEvents(), sh, pg, kc, vc, k_stride, v_stride,
+                                  rep, start, count, Tn, shift);
+    };
+    if (cache_dtype == CHAI_E4M3) return dtype == CHAI_BF16 ? go(paged_append_kernel<DT_E4M3, true>) : go(paged_append_kernel<DT_E4M3, false>);
+    return dtype == CHAI_BF16 ? go(paged_append_kernel<DT_BF16, true>) : go(paged_append_kernel<DT_F32, false>);
+}
+
+int launch_paged_gather(const PagedShape &sh, const PagedPages &pg, const int32_t *start, const int32_t *count, void *k_out, void *v_out,
+                        int Tn, int dtype, int cache_dtype, hipStream_t stream)
+{
+    const int shift = move_shift(Tn);
+    char *ko = static_cast<char *>(k_out), *vo = static_cast<char *>(v_out);
+    auto go = [&](auto *kernel) {
+        return (int)launch_kernel(kernel, move_grid(sh, Tn, shift), dim3(kBlock), 0, stream, KernelEvents(), sh, pg, start, count, ko, vo, Tn,
+                                  shift);
+    };
+    if (cache_dtype == CHAI_E4M3) return dtype == CHAI_BF16 ? go(paged_gather_kernel<DT_E4M3, true>) : go(paged_gather_kernel<DT_E4M3, false>);
+    return dtype == CHAI_BF16 ? go(paged_gather_kernel<DT_BF16, true>) : go(paged_gather_kernel<DT_F32, false>);
+}
+
+}  // namespace chai
