@@ -149,7 +149,7 @@ struct PagedPages {
 };
 // Regions of the workspace, upper bounds over the types.
 struct PagedPlan {
-    size_t off_recs, off_partial, bytes;
+    size_t off_recs, off_partial, off_whole, off_scores, bytes;
 };
 constexpr int kMaxPagedBatch = 4096;     // rows: two levels of 64 lanes add up their lengths
 constexpr int kMaxPagedTokens = 1 << 24;

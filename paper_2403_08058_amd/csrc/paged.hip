@@ -32,7 +32,6 @@ __device__ __forceinline__ int row_len(const PagedShape &sh, int b) { return min
 // w * quota on: every wave streams the same number of bytes whatever the lengths are, which only the device knows.  Each wave adds up
 // the rows' units for itself (64 rows per load and six steps of a scan).
 // ---------------------------------------------------------------------------------------------------------
-
 __device__ __forceinline__ unsigned int wave_scan(unsigned int x, int lane)
 {
 #pragma unroll
@@ -46,22 +45,27 @@ __device__ __forceinline__ unsigned int wave_scan(unsigned int x, int lane)
 template <int U>
 struct Deal {
     unsigned int incl, mine;                 // lane l: units of one stream over rows up to and with its own, and of its own rows
+    int len;                                 // (up to 64 rows) of the lane's row
     int span;                                // rows per lane
     unsigned int total;                      // units of one stream over all rows
 
-    __device__ __forceinline__ static unsigned int units(const PagedShape &sh, int b) { return (unsigned int)(row_len(sh, b) + U - 1) / U; }
+    __device__ __forceinline__ static unsigned int units(int len) { return (unsigned int)(len + U - 1) / U; }
 
     __device__ __forceinline__ Deal(const PagedShape &sh, int lane)
     {
         span = (sh.B + 63) / 64;
+        len = 0;
         mine = 0u;
         for (int i = 0; i < span; ++i) {
             const int b = lane * span + i;
-            mine += b < sh.B ? units(sh, min(b, sh.B - 1)) : 0u;
+            len = b < sh.B ? row_len(sh, min(b, sh.B - 1)) : 0;
+            mine += units(len);
         }
         incl = wave_scan(mine, lane);
         total = (unsigned int)__builtin_amdgcn_readlane((int)incl, 63);
     }
+
+    __device__ __forceinline__ int len_of(const PagedShape &sh, int b) const { return span == 1 ? __builtin_amdgcn_readlane(len, b) : row_len(sh, b); }
 
     __device__ __forceinline__ unsigned int quota(int streams, const PagedSplit &sp) const
     {
@@ -76,7 +80,7 @@ struct Deal {
         unsigned int p = (unsigned int)__builtin_amdgcn_readlane((int)(incl - mine), l);
         if (span > 1) {
             const int r = l * span + lane;
-            const unsigned int u = lane < span && r < b ? units(sh, min(r, sh.B - 1)) : 0u;
+            const unsigned int u = lane < span && r < b ? units(row_len(sh, min(r, sh.B - 1))) : 0u;
             p += (unsigned int)__builtin_amdgcn_readlane((int)wave_scan(u, lane), 63);
         }
         return p;
@@ -90,7 +94,7 @@ struct Deal {
         int b = l * span;
         if (span > 1) {
             const int r = b + lane;
-            const unsigned int u = lane < span && r < sh.B ? units(sh, min(r, sh.B - 1)) : 0u;
+            const unsigned int u = lane < span && r < sh.B ? units(row_len(sh, min(r, sh.B - 1))) : 0u;
             const unsigned int in = wave_scan(u, lane);
             const int i = __ffsll((long long)__ballot(p + in > y)) - 1;
             p += (unsigned int)__builtin_amdgcn_readlane((int)(in - u), i);
@@ -100,6 +104,131 @@ struct Deal {
         return b;
     }
 };
+
+// The stretches of one stream that a worker's units fall into, one after the other: units ua .. ue-1 of stream s of row b.
+template <int U>
+struct Walk {
+    unsigned int x, x0, x1, ua, ue, n_row, first;        // n_row: units of the stream; first: units of one stream before row b
+    int b, s, len;
+    __device__ __forceinline__ bool begin(const PagedShape &sh, const Deal<U> &deal, unsigned int worker, int streams, const PagedSplit &sp, int lane)
+    {
+        const unsigned int quota = deal.quota(streams, sp), n = deal.total * (unsigned int)streams;
+        if (worker >= sp.workers || (unsigned long long)worker * quota >= n) return false;
+        x = x0 = worker * quota;
+        x1 = min(x0 + quota, n);
+        b = deal.row_at(sh, x / (unsigned int)streams, lane, &first);
+        len = deal.len_of(sh, b);
+        n_row = Deal<U>::units(len);
+        const unsigned int at = x - first * (unsigned int)streams;
+        s = (int)(at / n_row);
+        ua = at - (unsigned int)s * n_row;
+        ue = min(n_row, ua + (x1 - x));
+        return true;
+    }
+    __device__ __forceinline__ bool next(const PagedShape &sh, const Deal<U> &deal, int streams)
+    {
+        x += ue - ua;
+        if (x >= x1) return false;
+        if (++s == streams) {
+            s = 0;
+            first += n_row;
+            do {
+                len = deal.len_of(sh, ++b);              // (units are left, so a row is)
+                n_row = Deal<U>::units(len);
+            } while (n_row == 0u);
+        }
+        ua = 0;
+        ue = min(n_row, x1 - x);
+        return true;
+    }
+    __device__ __forceinline__ bool whole() const { return ua == 0 && ue == n_row; }
+    // a worker's parts of streams: the first stretch's, and the last one's where that is another
+    __device__ __forceinline__ size_t slot(unsigned int worker) const { return 2 * (size_t)worker + (x == x0 ? 0 : 1); }
+};
+
+// Who took a stream of n_row units of which `at` stand before it: `n` workers from `from` on; slot of the i-th one's part.
+struct Takers {
+    unsigned int from, n, late;
+    __device__ __forceinline__ Takers(unsigned int at, unsigned int n_row, unsigned int quota)
+    {
+        from = at / quota;
+        n = (at + n_row - 1) / quota - from + 1;
+        late = at != from * quota ? 1u : 0u;
+    }
+    __device__ __forceinline__ size_t slot(unsigned int i) const { return 2 * (size_t)(from + i) + (i == 0 ? late : 0u); }
+};
+
+// ---------------------------------------------------------------------------------------------------------
+// Loads of one unit.  A load covers RPW consecutive rows and pages hold multiples of 8, so every load lies in one page: lane i looks up
+// the page of load i % 8 and the loads' bases are uniform.  Rows past the end and of absent pages: the pool's first rows are loaded in
+// their place, and masked where they are used.
+// ---------------------------------------------------------------------------------------------------------
+template <int DT>
+__device__ __forceinline__ int look_up(const PagedShape &sh, const int32_t *table, unsigned int u, unsigned int ue, int len, int lane)
+{
+    const int row = (int)(u * Tile<DT>::BATCH) + (lane & 7) * Tile<DT>::RPW;
+    const int at = table[min(block_of(sh, min(row, sh.T_max - 1)), sh.max_blocks - 1)];
+    return u < ue && row < len && (unsigned int)at < (unsigned int)sh.n_pages ? at : -1;
+}
+
+// the first row of the lane's load among the pool's rows (0 where there is none)
+template <int DT>
+__device__ __forceinline__ unsigned int pool_row(const PagedShape &sh, int at, unsigned int u, int streams, int s, int lane)
+{
+    const int row = (int)(u * Tile<DT>::BATCH) + (lane & 7) * Tile<DT>::RPW;
+    return at < 0 ? 0u : (unsigned int)(at * streams + s) * (unsigned int)sh.page + (unsigned int)(row - block_of(sh, row) * sh.page);
+}
+
+template <int DT>
+__device__ __forceinline__ void request(u32x4 (&buf)[kUnroll], const char *rows, unsigned int row, unsigned int lane_off)
+{
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i)
+        buf[i] = stream16(rows + (size_t)(unsigned int)__builtin_amdgcn_readlane((int)row, i) * Tile<DT>::ROW_BYTES + lane_off);
+}
+
+// scores of a unit: lane cg < 8 of a lane group gets that of load cg, row rg + cg * RPW of the unit
+template <int DT>
+__device__ __forceinline__ float dots(const u32x4 (&kb)[kUnroll], const float (&qf)[Tile<DT>::EPL], int cg)
+{
+    float mine = 0.f;
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+        float f[Tile<DT>::EPL];
+        unpack(kb[i], f);
+        float dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < Tile<DT>::EPL; ++e) dot = fmaf(qf[e], f[e], dot);
+        dot = row_sum<DT>(dot);
+        mine = cg == i ? dot : mine;
+    }
+    return mine;
+}
+
+// acc += weight * row over a unit's rows; `weight` lies with the lane that owns the row (as in dots), `there` says whether it counts
+template <int DT>
+__device__ __forceinline__ void weigh(float (&acc)[Tile<DT>::EPL], u32x4 (&vb)[kUnroll], float weight, bool there, float *strip, int cg, int rg)
+{
+    if (cg < kUnroll) strip[rg * kUnroll + cg] = weight;
+    __builtin_amdgcn_wave_barrier();
+    float pv[kUnroll];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) pv[i] = strip[rg * kUnroll + i];
+    __builtin_amdgcn_wave_barrier();
+    if (!__all(there || cg >= kUnroll)) {
+        const unsigned long long have = __ballot(there) >> (rg * Tile<DT>::LPR);
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i)
+            if (!((have >> i) & 1ull)) vb[i] = u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i) {
+        float f[Tile<DT>::EPL];
+        unpack(vb[i], f);
+#pragma unroll
+        for (int e = 0; e < Tile<DT>::EPL; ++e) acc[e] = fmaf(pv[i], f[e], acc[e]);
+    }
+}
 
 // the query as the lane multiplies it: elements cg * EPL .. of its representative's row (beside codes q has a type of its own)
 template <int DT>
@@ -136,48 +265,42 @@ __device__ __forceinline__ void store_floats(float *p, const float (&f)[N])
     for (int e = 0; e < N; e += 4) *reinterpret_cast<float4 *>(p + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
 }
 
+// the stored score is the rounded product: statistics and probabilities both start from it
+template <int DT>
+__device__ __forceinline__ float scaled(float dot, float scale, float row_scale)
+{
+#pragma clang fp contract(off)
+    return DT == DT_E4M3 ? (scale * row_scale) * dot : scale * dot;
+}
+
 constexpr float kPagedDown = 0x1p-24f;       // times kMaxPagedTokens weights of at most 1: at most 1
 constexpr float kPagedLarge = 0x1p120f;
 
 // ---------------------------------------------------------------------------------------------------------
-// Attention: one wave streams keys and values of its units together.  With a running reference m (the largest score so far; it moves
-// only when a batch exceeds it, then what has been added up is scaled by exp(old - new)):
+// Attention in one pass: one wave streams keys and values of its units together.  With a running reference m (the largest score so
+// far; it moves only when a unit exceeds it, then what has been added up is scaled by exp(old - new)):
 //     s[t] = scale * q . K[t],   acc += exp(s[t] - m) V[t],   l += exp(s[t] - m)
 // A stream that ends inside the wave's units and began there goes to `out` as acc / l; of others acc / l goes to `partial` and (m, l)
 // to `recs` of the wave, two of each (its first units, its last ones), and paged_join_kernel puts them together.
-// A load covers RPW consecutive rows and pages hold multiples of 8, so every load lies in one page: lane i looks up the page of load
-// i % 8 and the loads' bases are uniform.  Rows past the end and of absent pages: the pool's first rows are loaded in their place,
-// their scores are -inf and their values zeroed.
 // ---------------------------------------------------------------------------------------------------------
 template <int DT, bool IDENT>
-__global__ __launch_bounds__(kBlock, 4) void paged_attend_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q,
-                                                                 int q_dtype, const int32_t *__restrict__ h2c,
-                                                                 const int32_t *__restrict__ rep, float scale,
-                                                                 float *__restrict__ partial, float2 *__restrict__ recs,
-                                                                 float *__restrict__ out)
+__global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 3 : 4) void paged_attend_kernel(
+    PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q, int q_dtype, const int32_t *__restrict__ h2c,
+    const int32_t *__restrict__ rep, float scale, float *__restrict__ partial, float2 *__restrict__ recs, float *__restrict__ out)
 {
     using TL = Tile<DT>;
     constexpr int U = TL::BATCH;
-    __shared__ float p_lds[kWaves][64];
+    __shared__ float strip[kWaves][64];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned int worker = blockIdx.x * kWaves + w;
     const int cg = lane % TL::LPR, rg = lane / TL::LPR;
     const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
 
     const Deal<U> deal(sh, lane);
-    const unsigned int quota = deal.quota(sh.H, sp), n_units = deal.total * (unsigned int)sh.H;
-    const unsigned long long x0l = (unsigned long long)worker * quota;
-    if (worker >= sp.workers || x0l >= n_units) return;
-    const unsigned int x0 = (unsigned int)x0l, x1 = min(x0 + quota, n_units);
-    unsigned int first;
-    int b = deal.row_at(sh, x0 / (unsigned int)sh.H, lane, &first);
-    unsigned int n_row = Deal<U>::units(sh, b);
-    int h = (int)((x0 - first * (unsigned int)sh.H) / n_row);
-    unsigned int ua = x0 - first * (unsigned int)sh.H - (unsigned int)h * n_row;
-
-    for (unsigned int x = x0; x < x1;) {
-        const unsigned int ue = min(n_row, ua + (x1 - x));
-        const int len = row_len(sh, b);
+    Walk<U> wk;
+    if (!wk.begin(sh, deal, worker, sh.H, sp, lane)) return;
+    do {
+        const int b = wk.b, h = wk.s, len = wk.len;
         const int c = IDENT ? h : min(max(h2c[(size_t)b * sh.H + h], 0), sh.k - 1);
         const int r = IDENT ? h : min(max(rep[(size_t)b * sh.k + c], 0), sh.H - 1);
         const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
@@ -186,53 +309,25 @@ __global__ __launch_bounds__(kBlock, 4) void paged_attend_kernel(PagedShape sh, 
 
         float acc[TL::EPL], m_ref, l_run, down = 1.f;
         for (;;) {
-            // page of load (lane % 8) of unit u, -1 past the end of the row and of the units
-            auto look = [&](unsigned int u) {
-                const int row = (int)(u * U) + (lane & 7) * TL::RPW;
-                const int at = table[min(block_of(sh, min(row, sh.T_max - 1)), sh.max_blocks - 1)];
-                return u < ue && row < len && (unsigned int)at < (unsigned int)sh.n_pages ? at : -1;
-            };
-            auto row_of = [&](int at, unsigned int u, int streams, int s) {
-                const int row = (int)(u * U) + (lane & 7) * TL::RPW;
-                return at < 0 ? 0u : (unsigned int)(at * streams + s) * (unsigned int)sh.page + (unsigned int)(row - block_of(sh, row) * sh.page);
-            };
-            auto request = [&](u32x4 (&buf)[kUnroll], const char *rows, unsigned int row) {
-#pragma unroll
-                for (int i = 0; i < kUnroll; ++i) {
-                    const char *base = rows + (size_t)(unsigned int)__builtin_amdgcn_readlane((int)row, i) * TL::ROW_BYTES;
-                    buf[i] = stream16(base + lane_off);
-                }
-            };
             u32x4 kb[kUnroll], vb[kUnroll];
             float ks = 1.f, vs = 1.f;
-            int at = look(ua), at1 = look(ua + 1);
-            unsigned int krow = row_of(at, ua, sh.k, c), vrow = row_of(at, ua, sh.H, h);
-            request(kb, pg.k, krow);
+            int at = look_up<DT>(sh, table, wk.ua, wk.ue, len, lane), at1 = look_up<DT>(sh, table, wk.ua + 1, wk.ue, len, lane);
+            unsigned int krow = pool_row<DT>(sh, at, wk.ua, sh.k, c, lane), vrow = pool_row<DT>(sh, at, wk.ua, sh.H, h, lane);
+            request<DT>(kb, pg.k, krow, lane_off);
             if (DT == DT_E4M3) ks = pg.k_scales[krow + (at < 0 ? 0 : rg)];
-            request(vb, pg.v, vrow);
+            request<DT>(vb, pg.v, vrow, lane_off);
             if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at < 0 ? 0 : rg)];
 #pragma unroll
             for (int e = 0; e < TL::EPL; ++e) acc[e] = 0.f;
             m_ref = -INFINITY;
             l_run = 0.f;
-            for (unsigned int u = ua; u < ue; ++u) {
-                const int at2 = look(u + 2);
-                float mine = 0.f;
-#pragma unroll
-                for (int i = 0; i < kUnroll; ++i) {
-                    float f[TL::EPL];
-                    unpack(kb[i], f);
-                    float dot = 0.f;
-#pragma unroll
-                    for (int e = 0; e < TL::EPL; ++e) dot = fmaf(qf[e], f[e], dot);
-                    dot = row_sum<DT>(dot);
-                    mine = cg == i ? dot : mine;
-                }
-                // lane cg < 8 of a lane group owns the row of load cg: row rg + cg * RPW of the unit
+            for (unsigned int u = wk.ua; u < wk.ue; ++u) {
+                const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
+                const float mine = dots<DT>(kb, qf, cg);
                 const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
-                const float sv = there ? (DT == DT_E4M3 ? (scale * ks) * mine : scale * mine) : -INFINITY;
-                krow = row_of(at1, u + 1, sh.k, c);
-                request(kb, pg.k, krow);
+                const float sv = there ? scaled<DT>(mine, scale, ks) : -INFINITY;
+                krow = pool_row<DT>(sh, at1, u + 1, sh.k, c, lane);
+                request<DT>(kb, pg.k, krow, lane_off);
                 if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
                 if (__any(sv > m_ref)) {
                     const float m_new = fmaxf(m_ref, wave_max(sv));
@@ -244,27 +339,9 @@ __global__ __launch_bounds__(kBlock, 4) void paged_attend_kernel(PagedShape sh, 
                 }
                 const float p = __expf(sv - (m_ref == -INFINITY ? 0.f : m_ref)) * down;
                 l_run += p;
-                if (cg < kUnroll) p_lds[w][rg * kUnroll + cg] = DT == DT_E4M3 ? (there ? p * vs : 0.f) : p;
-                __builtin_amdgcn_wave_barrier();
-                float pv[kUnroll];
-#pragma unroll
-                for (int i = 0; i < kUnroll; ++i) pv[i] = p_lds[w][rg * kUnroll + i];
-                __builtin_amdgcn_wave_barrier();
-                if (!__all(there || cg >= kUnroll)) {
-                    const unsigned long long have = __ballot(there) >> (rg * TL::LPR);
-#pragma unroll
-                    for (int i = 0; i < kUnroll; ++i)
-                        if (!((have >> i) & 1ull)) vb[i] = u32x4{0u, 0u, 0u, 0u};
-                }
-#pragma unroll
-                for (int i = 0; i < kUnroll; ++i) {
-                    float f[TL::EPL];
-                    unpack(vb[i], f);
-#pragma unroll
-                    for (int e = 0; e < TL::EPL; ++e) acc[e] = fmaf(pv[i], f[e], acc[e]);
-                }
-                vrow = row_of(at1, u + 1, sh.H, h);
-                request(vb, pg.v, vrow);
+                weigh<DT>(acc, vb, DT == DT_E4M3 ? (there ? p * vs : 0.f) : p, there, strip[w], cg, rg);
+                vrow = pool_row<DT>(sh, at1, u + 1, sh.H, h, lane);
+                request<DT>(vb, pg.v, vrow, lane_off);
                 if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
                 at = at1;
                 at1 = at2;
@@ -283,26 +360,150 @@ __global__ __launch_bounds__(kBlock, 4) void paged_attend_kernel(PagedShape sh, 
         const float l = wave_sum(l_run);
 #pragma unroll
         for (int e = 0; e < TL::EPL; ++e) acc[e] = l == 0.f ? 0.f : acc[e] / l;
-        if (ua == 0 && ue == n_row) {
+        if (wk.whole()) {
             if (rg == 0) store_floats(out + ((size_t)b * sh.H + h) * kHeadDim + cg * TL::EPL, acc);
         } else {
-            const size_t slot = 2 * (size_t)worker + (x == x0 ? 0 : 1);
+            const size_t slot = wk.slot(worker);
             if (rg == 0) store_floats(partial + slot * kHeadDim + cg * TL::EPL, acc);
             if (lane == 0) recs[slot] = make_float2(m_ref, l / down);
         }
-        x += ue - ua;
-        ua = 0;
-        if (++h == sh.H) {
-            h = 0;
-            do ++b;
-            while (b < sh.B && (n_row = Deal<U>::units(sh, b)) == 0u);
-        }
-    }
+    } while (wk.next(sh, deal, sh.H));
 }
 
-// Streams that several waves took: out = mean of their parts, each weighed by its sum of exponentials times exp(its reference - the
-// largest).  A wave per (row, head), two columns per lane; streams that one wave took are left alone, rows without a position get 0.
-template <int U>
+// ---------------------------------------------------------------------------------------------------------
+// Attention in two passes, for layers with fewer clusters than heads: the keys of a cluster are read once, not once per member.
+// Scores: a wave streams keys of its units, writes s[b][j][t] (-inf where nothing is to be attended to, whole units) and the maximum
+// and sum of exponentials of every stretch: `whole` of a stream that it took alone, else `parts` of the wave.
+// ---------------------------------------------------------------------------------------------------------
+template <int DT>
+__global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 5 : 6) void paged_scores_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q,
+                                                                 int q_dtype, const int32_t *__restrict__ rep, float scale, int T_pad,
+                                                                 float *__restrict__ scores, float2 *__restrict__ whole,
+                                                                 float2 *__restrict__ parts)
+{
+    using TL = Tile<DT>;
+    constexpr int U = TL::BATCH;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned int worker = blockIdx.x * kWaves + w;
+    const int cg = lane % TL::LPR, rg = lane / TL::LPR;
+    const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
+
+    const Deal<U> deal(sh, lane);
+    Walk<U> wk;
+    if (!wk.begin(sh, deal, worker, sh.k, sp, lane)) return;
+    do {
+        const int b = wk.b, j = wk.s, len = wk.len;
+        const int r = min(max(rep[(size_t)b * sh.k + j], 0), sh.H - 1);
+        const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
+        u32x4 kb[kUnroll];
+        float ks = 1.f;
+        int at = look_up<DT>(sh, table, wk.ua, wk.ue, len, lane), at1 = look_up<DT>(sh, table, wk.ua + 1, wk.ue, len, lane);
+        unsigned int krow = pool_row<DT>(sh, at, wk.ua, sh.k, j, lane);
+        request<DT>(kb, pg.k, krow, lane_off);
+        if (DT == DT_E4M3) ks = pg.k_scales[krow + (at < 0 ? 0 : rg)];
+        float qf[TL::EPL];
+        load_query<DT>(q, (size_t)b * sh.H + r, cg, q_dtype, qf);
+        float *srow = scores + ((size_t)b * sh.k + j) * T_pad;
+        float m_run = -INFINITY, l_run = 0.f;            // of the scores that this lane has seen
+        for (unsigned int u = wk.ua; u < wk.ue; ++u) {
+            const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
+            const float mine = dots<DT>(kb, qf, cg);
+            const int t = (int)(u * U) + cg * TL::RPW + rg;
+            const bool there = cg < kUnroll && at >= 0 && t < len;
+            const float sv = there ? scaled<DT>(mine, scale, ks) : -INFINITY;
+            krow = pool_row<DT>(sh, at1, u + 1, sh.k, j, lane);
+            request<DT>(kb, pg.k, krow, lane_off);
+            if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
+            if (cg < kUnroll) srow[t] = sv;
+            const float m_new = fmaxf(m_run, sv), ref = m_new == -INFINITY ? 0.f : m_new;
+            l_run = l_run * __expf(m_run - ref) + __expf(sv - ref);
+            m_run = m_new;
+            at = at1;
+            at1 = at2;
+        }
+        const float M = wave_max(m_run);
+        const float L = wave_sum(m_run == -INFINITY ? l_run : l_run * __expf(m_run - M));     // (lanes that saw only NaN hold it in l_run)
+        if (lane == 0) (wk.whole() ? whole[(size_t)b * sh.k + j] : parts[wk.slot(worker)]) = make_float2(M, L);
+    } while (wk.next(sh, deal, sh.k));
+}
+
+// Maximum and sum of exponentials over a stream's parts.
+__device__ __forceinline__ float2 merge(const float2 *parts, const Takers &tk, int lane)
+{
+    float m = -INFINITY;
+    for (unsigned int i = lane; i < tk.n; i += 64) m = fmaxf(m, parts[tk.slot(i)].x);
+    const float M = wave_max(m);
+    float l = 0.f;
+    for (unsigned int i = lane; i < tk.n; i += 64) {
+        const float2 rc = parts[tk.slot(i)];
+        l += rc.x == -INFINITY ? rc.y : rc.y * __expf(rc.x - M);         // (only -inf scores: 0, NaN among them: NaN)
+    }
+    return make_float2(M, wave_sum(l));
+}
+
+// Values: a wave streams the values of its units, each weighed by its cluster's probability exp(s - M) / L.
+template <int DT>
+__global__ __launch_bounds__(kBlock, DT == DT_F32 ? 6 : (DT == DT_BF16 ? 5 : 4)) void paged_values_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, PagedSplit sp_scores,
+                                                                 const int32_t *__restrict__ h2c, int T_pad,
+                                                                 const float *__restrict__ scores, const float2 *__restrict__ whole,
+                                                                 const float2 *__restrict__ parts, float *__restrict__ partial,
+                                                                 float *__restrict__ out)
+{
+    using TL = Tile<DT>;
+    constexpr int U = TL::BATCH;
+    __shared__ float strip[kWaves][64];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned int worker = blockIdx.x * kWaves + w;
+    const int cg = lane % TL::LPR, rg = lane / TL::LPR;
+    const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
+
+    const Deal<U> deal(sh, lane);
+    Walk<U> wk;
+    if (!wk.begin(sh, deal, worker, sh.H, sp, lane)) return;
+    do {
+        const int b = wk.b, h = wk.s, len = wk.len;
+        const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
+        const int c = min(max(h2c[(size_t)b * sh.H + h], 0), sh.k - 1);
+        u32x4 vb[kUnroll];
+        float vs = 1.f;
+        int at = look_up<DT>(sh, table, wk.ua, wk.ue, len, lane), at1 = look_up<DT>(sh, table, wk.ua + 1, wk.ue, len, lane);
+        unsigned int vrow = pool_row<DT>(sh, at, wk.ua, sh.H, h, lane);
+        request<DT>(vb, pg.v, vrow, lane_off);
+        if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at < 0 ? 0 : rg)];
+        const float *srow = scores + ((size_t)b * sh.k + c) * T_pad + (cg < kUnroll ? cg * TL::RPW + rg : 0);
+        float sv = srow[wk.ua * U];
+        const Takers tk(wk.first * (unsigned int)sh.k + (unsigned int)c * wk.n_row, wk.n_row, deal.quota(sh.k, sp_scores));
+        const float2 st = tk.n == 1 ? whole[(size_t)b * sh.k + c] : merge(parts, tk, lane);
+        const float M = st.x == -INFINITY ? 0.f : st.x, inv = st.y == 0.f ? 0.f : 1.f / st.y;
+        float acc[TL::EPL];
+#pragma unroll
+        for (int e = 0; e < TL::EPL; ++e) acc[e] = 0.f;
+        for (unsigned int u = wk.ua; u < wk.ue; ++u) {
+            const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
+            const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
+            const float p = there ? __expf(sv - M) * inv : 0.f;
+            weigh<DT>(acc, vb, DT == DT_E4M3 ? (there ? p * vs : 0.f) : p, there, strip[w], cg, rg);
+            vrow = pool_row<DT>(sh, at1, u + 1, sh.H, h, lane);
+            request<DT>(vb, pg.v, vrow, lane_off);
+            if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
+            sv = srow[min(u + 1, wk.ue - 1) * U];
+            at = at1;
+            at1 = at2;
+        }
+#pragma unroll
+        for (int e = 0; e < TL::EPL; ++e) {
+#pragma unroll
+            for (int o = TL::LPR; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
+        }
+        float *o = wk.whole() ? out + ((size_t)b * sh.H + h) * kHeadDim : partial + wk.slot(worker) * kHeadDim;
+        if (rg == 0) store_floats(o + cg * TL::EPL, acc);
+    } while (wk.next(sh, deal, sh.H));
+}
+
+// Streams that several waves took.  WEIGHED (one pass): out = mean of their parts, each weighed by its sum of exponentials times
+// exp(its reference - the largest); else their sum.  A wave per (row, head), two columns per lane; streams that one wave took are left
+// alone, rows without a position get 0.
+template <int U, bool WEIGHED>
 __global__ __launch_bounds__(kBlock) void paged_join_kernel(PagedShape sh, PagedSplit sp, const float *__restrict__ partial,
                                                             const float2 *__restrict__ recs, float *__restrict__ out)
 {
@@ -310,38 +511,33 @@ __global__ __launch_bounds__(kBlock) void paged_join_kernel(PagedShape sh, Paged
     const int h = blockIdx.x * kWaves + w, b = blockIdx.y;
     if (h >= sh.H) return;
     float2 *o = reinterpret_cast<float2 *>(out + ((size_t)b * sh.H + h) * kHeadDim) + lane;
-    const unsigned int n_row = Deal<U>::units(sh, b);
+    const Deal<U> deal(sh, lane);
+    const unsigned int n_row = Deal<U>::units(deal.len_of(sh, b));
     if (n_row == 0u) {
         *o = make_float2(0.f, 0.f);
         return;
     }
-    const Deal<U> deal(sh, lane);
-    const unsigned int quota = deal.quota(sh.H, sp);
-    const unsigned int a = deal.before(sh, b, lane) * (unsigned int)sh.H + (unsigned int)h * n_row;
-    const unsigned int wa = a / quota, n = (a + n_row - 1) / quota - wa + 1;
-    if (n == 1) return;
-    auto slot = [&](unsigned int i) { return 2 * (size_t)(wa + i) + (i == 0 && a != wa * quota ? 1 : 0); };
-    float M = -INFINITY;
-    for (unsigned int i = lane; i < n; i += 64) M = fmaxf(M, recs[slot(i)].x);
-    M = wave_max(M);
-    // (a part whose scores are all -inf has the sum 0, one with NaN among them NaN)
-    auto weight = [&](const float2 &rc) { return rc.x == -INFINITY ? rc.y : __expf(rc.x - M) * rc.y; };
-    float l = 0.f;
-    for (unsigned int i = lane; i < n; i += 64) l += weight(recs[slot(i)]);
-    l = wave_sum(l);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const Takers tk(deal.before(sh, b, lane) * (unsigned int)sh.H + (unsigned int)h * n_row, n_row, deal.quota(sh.H, sp));
+    if (tk.n == 1) return;
+    float2 st = make_float2(0.f, 1.f);
+    if (WEIGHED) st = merge(recs, tk, lane);
+    const float inv = st.y == 0.f ? 0.f : 1.f / st.y;
     float2 sum = make_float2(0.f, 0.f);
-    for (unsigned int i0 = 0; i0 < n; i0 += 64) {
-        const float wt = i0 + lane < n ? weight(recs[slot(i0 + lane)]) * inv : 0.f;
-        const unsigned int here = min(n - i0, 64u);
+    for (unsigned int i0 = 0; i0 < tk.n; i0 += 64) {
+        float wt = 0.f;
+        if (WEIGHED && i0 + lane < tk.n) {
+            const float2 rc = recs[tk.slot(i0 + lane)];
+            wt = (rc.x == -INFINITY ? rc.y : rc.y * __expf(rc.x - st.x)) * inv;
+        }
+        const unsigned int here = min(tk.n - i0, 64u);
         for (unsigned int i = 0; i < here; i += 8) {
             float2 v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                v[j] = reinterpret_cast<const float2 *>(partial + slot(i0 + min(i + j, here - 1)) * kHeadDim)[lane];
+                v[j] = reinterpret_cast<const float2 *>(partial + tk.slot(i0 + min(i + j, here - 1)) * kHeadDim)[lane];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float wj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), (int)min(i + j, 63u)));
+                const float wj = WEIGHED ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), (int)min(i + j, 63u))) : 1.f;
                 if (i + j < here) {
                     sum.x = fmaf(wj, v[j].x, sum.x);
                     sum.y = fmaf(wj, v[j].y, sum.y);
@@ -519,26 +715,39 @@ int unit_rows(int cache_dtype) { return cache_dtype == CHAI_F32 ? Tile<DT_F32>::
 
 }  // namespace
 
-constexpr unsigned int kPagedWorkers = 256 * 16;       // waves that fit the CUs beside each other
+// Waves of a launch.  Of the two passes, which have one stream of loads each, in us for 1024 / 2048 / 3072 / 4096 / 6144 to 8192:
+// scores of 64 x 8 rows of codes (4096 tokens at most, most short) 23.1 / 17.2 / 16.6 / 16.2 / 16.5 and values of 64 x 32 - / 49 / 45
+// / 41.6 / 44.6; 4 x 32 of 32768 bf16 tokens within 2 % up to 4096, 173 / 163 with 8192.  One pass has keys and values in flight: 8 x
+// 52 heads of up to 1777 bf16 tokens 37.4 / 36.4 / 41 / 43.6 / 42.
+constexpr unsigned int kStreamWorkers = 4096, kAttendWorkers = 2048, kPagedWorkers = 4096;
 constexpr unsigned int kPagedParts = 64;               // most waves of one stream
 
-PagedPlan make_paged_plan(int, int, int, int)
+static int padded_tokens(int T_max) { return (T_max + 63) / 64 * 64; }
+
+PagedPlan make_paged_plan(int B, int H, int k, int T_max)
 {
     PagedPlan pl;
-    pl.off_recs = 0;
-    pl.off_partial = align_up(2 * (size_t)kPagedWorkers * sizeof(float2), 256);
-    pl.bytes = pl.off_partial + 2 * (size_t)kPagedWorkers * kHeadDim * sizeof(float);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align_up(off + bytes, 256);
+        return at;
+    };
+    pl.off_recs = take(2 * (size_t)kPagedWorkers * sizeof(float2));
+    pl.off_partial = take(2 * (size_t)kPagedWorkers * kHeadDim * sizeof(float));
+    pl.off_whole = take((size_t)B * k * sizeof(float2));
+    pl.off_scores = take((size_t)B * k * padded_tokens(T_max) * sizeof(float));
+    pl.bytes = off;
     return pl;
 }
 
-static PagedSplit make_paged_split(int B, int streams, int T_max, int cache_dtype)
+static PagedSplit make_paged_split(int B, int streams, int T_max, int cache_dtype, unsigned int workers)
 {
     PagedSplit sp;
     const int u = unit_rows(cache_dtype);
     const long long row_units = ((long long)T_max + u - 1) / u, units = row_units * B * streams;
-    sp.workers = (unsigned int)(units < (long long)kPagedWorkers ? units : kPagedWorkers);
+    sp.workers = (unsigned int)(units < (long long)workers ? units : workers);
     sp.least = (unsigned int)((row_units + kPagedParts - 1) / kPagedParts);
-    if (sp.least < 2u) sp.least = 2u;
     return sp;
 }
 
@@ -551,30 +760,37 @@ void set_page_division(PagedShape *sh)
     sh->div_mul = (unsigned int)((((1ull << s) - (unsigned long long)sh->page) << 32) / (unsigned long long)sh->page + 1ull);
 }
 
+template <int DT>
+static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, const char *q, int dtype, const int32_t *h2c, const int32_t *rep,
+                                 float scale, float *out, char *ws, const PagedPlan &plan, hipStream_t stream)
+{
+    constexpr int U = Tile<DT>::BATCH, cache = DT;
+    float2 *recs = reinterpret_cast<float2 *>(ws + plan.off_recs), *whole = reinterpret_cast<float2 *>(ws + plan.off_whole);
+    float *partial = reinterpret_cast<float *>(ws + plan.off_partial), *scores = reinterpret_cast<float *>(ws + plan.off_scores);
+    const dim3 block(kBlock), heads((unsigned int)(sh.H + kWaves - 1) / kWaves, (unsigned int)sh.B);
+    auto waves = [](const PagedSplit &sp) { return dim3((sp.workers + kWaves - 1) / kWaves); };
+    const KernelEvents none;
+    if (h2c == nullptr) {
+        const PagedSplit sp = make_paged_split(sh.B, sh.H, sh.T_max, cache, kAttendWorkers);
+        const hipError_t e = launch_kernel(paged_attend_kernel<DT, true>, waves(sp), block, 0, stream,
+                                           none, sh, pg, sp, q, dtype, h2c, rep, scale, partial, recs, out);
+        if (e != hipSuccess) return (int)e;
+        return (int)launch_kernel(paged_join_kernel<U, true>, heads, block, 0, stream, none, sh, sp, partial, recs, out);
+    }
+    const PagedSplit ss = make_paged_split(sh.B, sh.k, sh.T_max, cache, kStreamWorkers), sv = make_paged_split(sh.B, sh.H, sh.T_max, cache, kStreamWorkers);
+    const int T_pad = padded_tokens(sh.T_max);
+    hipError_t e = launch_kernel(paged_scores_kernel<DT>, waves(ss), block, 0, stream, none, sh, pg, ss, q, dtype, rep, scale, T_pad, scores, whole, recs);
+    if (e != hipSuccess) return (int)e;
+    e = launch_kernel(paged_values_kernel<DT>, waves(sv), block, 0, stream, none, sh, pg, sv, ss, h2c, T_pad, scores, whole, recs, partial, out);
+    if (e != hipSuccess) return (int)e;
+    return (int)launch_kernel(paged_join_kernel<U, false>, heads, block, 0, stream, none, sh, sv, partial, nullptr, out);
+}
+
 int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const void *q, int dtype, int cache_dtype, const int32_t *h2c,
                            const int32_t *rep, float scale, float *out, void *workspace, const PagedPlan &plan, hipStream_t stream)
 {
-    float2 *recs = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + plan.off_recs);
-    float *partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.off_partial);
-    const PagedSplit sp = make_paged_split(sh.B, sh.H, sh.T_max, cache_dtype);
-    const dim3 grid((sp.workers + kWaves - 1) / kWaves), block(kBlock);
-    const char *qc = static_cast<const char *>(q);
-    auto go = [&](auto *attend, auto *join) {
-        const hipError_t e = launch_kernel(attend, grid, block, 0, stream, KernelEvents(), sh, pg, sp, qc, dtype, h2c, rep, scale,
-                                           partial, recs, out);
-        if (e != hipSuccess) return (int)e;
-        return (int)launch_kernel(join, dim3((unsigned int)(sh.H + kWaves - 1) / kWaves, (unsigned int)sh.B), block, 0, stream, KernelEvents(), sh,
-                                  sp, partial, recs, out);
-    };
-    const bool ident = h2c == nullptr;
-    if (cache_dtype == CHAI_F32)
-        return ident ? go(paged_attend_kernel<DT_F32, true>, paged_join_kernel<Tile<DT_F32>::BATCH>)
-                     : go(paged_attend_kernel<DT_F32, false>, paged_join_kernel<Tile<DT_F32>::BATCH>);
-    if (cache_dtype == CHAI_BF16)
-        return ident ? go(paged_attend_kernel<DT_BF16, true>, paged_join_kernel<Tile<DT_BF16>::BATCH>)
-                     : go(paged_attend_kernel<DT_BF16, false>, paged_join_kernel<Tile<DT_BF16>::BATCH>);
-    return ident ? go(paged_attend_kernel<DT_E4M3, true>, paged_join_kernel<Tile<DT_E4M3>::BATCH>)
-                 : go(paged_attend_kernel<DT_E4M3, false>, paged_join_kernel<Tile<DT_E4M3>::BATCH>);
+    auto *typed = cache_dtype == CHAI_F32 ? paged_attention_typed<DT_F32> : (cache_dtype == CHAI_BF16 ? paged_attention_typed<DT_BF16> : paged_attention_typed<DT_E4M3>);
+    return typed(sh, pg, static_cast<const char *>(q), dtype, h2c, rep, scale, out, static_cast<char *>(workspace), plan, stream);
 }
 
 int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *k_new, const void *v_new, int64_t k_stride,
