@@ -138,7 +138,8 @@ __device__ __forceinline__ Piece load_piece(const char *row, int piece)
     }
     return p;
 }
-__device__ __forceinline__ uint2 quantize_piece(const Piece &p, float &scale)
+// the largest magnitude of the row
+__device__ __forceinline__ float largest_of(const Piece &p)
 {
     float amax = 0.f;
 #pragma unroll
@@ -146,17 +147,25 @@ __device__ __forceinline__ uint2 quantize_piece(const Piece &p, float &scale)
     amax = dpp_max<0xB1>(amax);                      // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
     amax = dpp_max<0x4E>(amax);
     amax = dpp_max<0x141>(amax);
-    amax = dpp_max<0x140>(amax);
+    return dpp_max<0x140>(amax);
+}
+// the codes of a piece; inv = 448 / the largest magnitude
+__device__ __forceinline__ uint2 codes_of(const Piece &p, float inv)
+{
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(p.x[i] * inv, -448.0f), 448.0f);
+    return make_uint2(e4m3_codes(y[0], y[1], y[2], y[3]), e4m3_codes(y[4], y[5], y[6], y[7]));
+}
+__device__ __forceinline__ uint2 quantize_piece(const Piece &p, float &scale)
+{
+    const float amax = largest_of(p);
     if (amax == 0.f) {
         scale = 0.f;
         return make_uint2(0u, 0u);
     }
     scale = amax / 448.0f;
-    const float inv = 448.0f / amax;
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(p.x[i] * inv, -448.0f), 448.0f);
-    return make_uint2(e4m3_codes(y[0], y[1], y[2], y[3]), e4m3_codes(y[4], y[5], y[6], y[7]));
+    return codes_of(p, 448.0f / amax);
 }
 
 }  // namespace

@@ -7,11 +7,14 @@
 
 #include <hip/hip_ext.h>
 
+#include <type_traits>
+
 namespace chai {
 
 namespace {
 
 constexpr int kWaves = kBlock / 64;
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 // `workers` waves take at least `least` units each
 struct PagedSplit {
@@ -549,23 +552,28 @@ __global__ __launch_bounds__(kBlock) void paged_join_kernel(PagedShape sh, Paged
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// New rows into pages, and pages into contiguous rows.  A workgroup takes kMoveRows rows of one request: TB consecutive tokens (a
-// power of two, so that one new token of many streams fills a workgroup as well) of kMoveRows / TB streams; streams are the k key
-// slots, then the H value heads.  Sixteen lanes per row, eight elements each, all rows requested at once.
+// New rows into pages, and pages into contiguous rows.  A workgroup takes `rows` rows of one request: 1 << shift consecutive tokens (so
+// that one new token of many streams fills a workgroup as well) of rows >> shift streams; streams are the k key slots, then the H value
+// heads.  Sixteen lanes per row, eight elements each, all rows requested at once.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kMoveUnroll = 4, kMoveRows = kBlock / 16 * kMoveUnroll;
+template <bool BF16>
+constexpr int kMoveUnroll = BF16 ? 8 : 4;
+constexpr int move_rows(bool bf16) { return kBlock / 16 * (bf16 ? kMoveUnroll<true> : kMoveUnroll<false>); }
 
-struct MovedRow {
-    bool there, zero;                        // in a page; wanted but in none
-    unsigned int at;                         // row among the pool's rows of its kind
-    int stream, token;
+// Where a wave's rows are and go, one row per lane: row r of a wave is that of its lane group r % 4 (sixteen lanes) in round r / 4, and
+// the sixteen lanes of the group fetch it from lane r.  (Looked up by every lane for itself the multiplications took longer than the
+// rows: 16 x 40 streams of up to 2043 tokens quantised 79.7 us.)
+struct Places {
+    unsigned int at;                         // row among the pool's rows of its kind, kNowhere: in no page
+    unsigned int lo, hi;                     // the other side: 64 bits of offset below kIsKey, or a row
 };
+constexpr unsigned int kNowhere = 0xffffffffu, kIsKey = 0x80000000u;
 
-__device__ __forceinline__ MovedRow moved_row(const PagedShape &sh, const int32_t *start, const int32_t *count, int Tn, int shift, int local, int b)
+template <bool BF16, typename Other>
+__device__ __forceinline__ Places find_places(const PagedShape &sh, const int32_t *start, const int32_t *count, int Tn, int shift, int lane, int w, Other other)
 {
-    MovedRow m;
-    m.token = (int)(blockIdx.x << shift) + (local & ((1 << shift) - 1));
-    m.stream = blockIdx.y * (kMoveRows >> shift) + (local >> shift);
+    const int b = blockIdx.z;
+    Places pl = {kNowhere, kNowhere, 0u};
     int n = Tn, first;
     if (start == nullptr) {                  // the last position of every row
         first = sh.lens[b] - 1;
@@ -574,26 +582,59 @@ __device__ __forceinline__ MovedRow moved_row(const PagedShape &sh, const int32_
         first = start[b];
         if (count != nullptr) n = min(max(count[b], 0), Tn);
     }
-    const bool wanted = m.token < n && m.stream < sh.k + sh.H;
-    const int pos = (int)((unsigned int)first + (unsigned int)m.token);
-    const int block = block_of(sh, max(pos, 0));
-    int at = -1;
-    if (wanted && pos >= 0 && block < sh.max_blocks) at = sh.table[(size_t)b * sh.max_blocks + block];
-    m.there = (unsigned int)at < (unsigned int)sh.n_pages;
-    m.zero = wanted && !m.there;
-    const int streams = m.stream < sh.k ? sh.k : sh.H, s = m.stream < sh.k ? m.stream : m.stream - sh.k;
-    m.at = m.there ? (unsigned int)(at * streams + s) * (unsigned int)sh.page + (unsigned int)(pos - block * sh.page) : 0u;
-    return m;
+    const int local = (lane / 4) * (kBlock / 16) + w * 4 + lane % 4;
+    const int token = (int)(blockIdx.x << shift) + (local & ((1 << shift) - 1));
+    const int stream = blockIdx.y * (move_rows(BF16) >> shift) + (local >> shift);
+    if (lane < 4 * kMoveUnroll<BF16> && token < n && stream < sh.k + sh.H) {
+        const int pos = (int)((unsigned int)first + (unsigned int)token), block = block_of(sh, max(pos, 0));
+        const bool key = stream < sh.k;
+        const int streams = key ? sh.k : sh.H, s = key ? stream : stream - sh.k;
+        const int page_at = pos >= 0 && block < sh.max_blocks ? sh.table[(size_t)b * sh.max_blocks + block] : -1;
+        if ((unsigned int)page_at < (unsigned int)sh.n_pages)
+            pl.at = (unsigned int)(page_at * streams + s) * (unsigned int)sh.page + (unsigned int)(pos - block * sh.page);
+        other(pl, b, key, s, token);
+    }
+    return pl;
 }
 
-// eight bf16 values as they were before they were widened
-__device__ __forceinline__ uint4 packed(const Piece &p)
-{
-    unsigned int x[4];
+// a lane's eight elements of a row as they are held: one 16-byte word of bf16, two of fp32
+template <bool BF16>
+struct RawPiece {
+    u32x4 x[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const char *row, int piece)
+    {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = (__float_as_uint(p.x[2 * e]) >> 16) | (__float_as_uint(p.x[2 * e + 1]) & 0xffff0000u);
-    return make_uint4(x[0], x[1], x[2], x[3]);
-}
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) x[i] = stream16(row + piece * (BF16 ? 16 : 32) + i * 16);
+    }
+    __device__ __forceinline__ void store(char *row, int piece) const
+    {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(row + piece * (BF16 ? 16 : 32) + i * 16));
+    }
+    __device__ __forceinline__ Piece widened() const
+    {
+        Piece p;
+        if constexpr (BF16) {
+            unpack(x[0], p.x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p.x[e] = __uint_as_float(x[e / 4][e % 4]);
+        }
+        return p;
+    }
+    __device__ __forceinline__ void set(const float (&f)[8])
+    {
+        if constexpr (BF16) {
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[0][e] = __builtin_bit_cast(unsigned int, __builtin_convertvector(f32x2{f[2 * e], f[2 * e + 1]}, bf16x2));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e / 4][e % 4] = __float_as_uint(f[e]);
+        }
+    }
+};
 
 template <int DT, bool BF16>
 __global__ __launch_bounds__(kBlock) void paged_append_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ k_new,
@@ -601,47 +642,56 @@ __global__ __launch_bounds__(kBlock) void paged_append_kernel(PagedShape sh, Pag
                                                               const int32_t *__restrict__ rep, const int32_t *__restrict__ start,
                                                               const int32_t *__restrict__ count, int Tn, int shift)
 {
-    const int b = blockIdx.z, piece = threadIdx.x & 15, local = threadIdx.x >> 4;
-    constexpr int kBytes = BF16 ? 2 : 4;
-    MovedRow m[kMoveUnroll];
-    Piece p[kMoveUnroll];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, piece = lane & 15, rg = lane >> 4;
+    constexpr int kBytes = BF16 ? 2 : 4, N = kMoveUnroll<BF16>;
+    const Places pl = find_places<BF16>(sh, start, count, Tn, shift, lane, w, [&](Places &x, int b, bool key, int s, int token) {
+        const int h = key && rep != nullptr ? min(rep[(size_t)b * sh.k + s], sh.H - 1) : s;
+        if (h < 0) x.at = kNowhere;          // (a slot without a cluster keeps what it holds)
+        const unsigned long long from = (((unsigned long long)b * sh.H + max(h, 0)) * (key ? k_stride : v_stride) + (unsigned long long)token * kHeadDim) * kBytes;
+        x.lo = (unsigned int)from;
+        x.hi = (unsigned int)(from >> 32) | (key ? kIsKey : 0u);
+    });
+    if (!__any(pl.at != kNowhere)) return;
+    unsigned int at[N];
+    bool key[N];
+    RawPiece<BF16> p[N];
 #pragma unroll
-    for (int i = 0; i < kMoveUnroll; ++i) {
-        m[i] = moved_row(sh, start, count, Tn, shift, local + i * (kBlock / 16), b);
-        if (!m[i].there) continue;
-        const bool key = m[i].stream < sh.k;
-        int h = key ? m[i].stream : m[i].stream - sh.k;
-        if (key && rep != nullptr) h = min(rep[(size_t)b * sh.k + h], sh.H - 1);
-        m[i].there = h >= 0;                 // (a slot without a cluster keeps what it holds)
-        if (m[i].there)
-            p[i] = load_piece<BF16>((key ? k_new : v_new) + (((size_t)b * sh.H + h) * (key ? k_stride : v_stride) + (size_t)m[i].token * kHeadDim) * kBytes, piece);
+    for (int i = 0; i < N; ++i) {
+        const int r = i * 4 + rg;
+        at[i] = (unsigned int)__shfl((int)pl.at, r);
+        const unsigned int lo = (unsigned int)__shfl((int)pl.lo, r), hi = (unsigned int)__shfl((int)pl.hi, r);
+        key[i] = (hi & kIsKey) != 0u;
+        if (at[i] != kNowhere) p[i].load((key[i] ? k_new : v_new) + (((unsigned long long)(hi & ~kIsKey) << 32) | lo), piece);
     }
+    if constexpr (DT == DT_E4M3) {
+        // lane i of a group turns the largest value of the group's row i into its scale and factor, then hands the factor on
+        float amax[N], mine = 0.f;
+        unsigned int mine_at = kNowhere;
+        bool mine_key = false;
 #pragma unroll
-    for (int i = 0; i < kMoveUnroll; ++i) {
-        if (!m[i].there) continue;           // (the same for the sixteen lanes of a row)
-        const bool key = m[i].stream < sh.k;
-        char *rows = const_cast<char *>(key ? pg.k : pg.v);
-        if constexpr (DT == DT_E4M3) {
-            float scale;
-            const uint2 codes = quantize_piece(p[i], scale);
-            reinterpret_cast<uint2 *>(rows)[(size_t)m[i].at * 16 + piece] = codes;
-            if (piece == 0) const_cast<float *>(key ? pg.k_scales : pg.v_scales)[m[i].at] = scale;
-        } else if constexpr (BF16) {
-            reinterpret_cast<uint4 *>(rows)[(size_t)m[i].at * 16 + piece] = packed(p[i]);
-        } else {
-            store_floats(reinterpret_cast<float *>(rows) + (size_t)m[i].at * kHeadDim + piece * 8, p[i].x);
+        for (int i = 0; i < N; ++i) {
+            amax[i] = largest_of(p[i].widened());
+            mine = piece == i ? amax[i] : mine;
+            mine_at = piece == i ? at[i] : mine_at;
+            mine_key = piece == i ? key[i] : mine_key;
         }
+        const float factor = 448.0f / mine;
+        if (mine_at != kNowhere) const_cast<float *>(mine_key ? pg.k_scales : pg.v_scales)[mine_at] = mine == 0.f ? 0.f : mine / 448.0f;
+        auto write = [&](auto self, auto index) {
+            constexpr int i = decltype(index)::value;
+            const float inv = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(factor), 0x150 + i, 0xf, 0xf, false));     // row_newbcast: lane i
+            if (at[i] != kNowhere) {
+                const uint2 codes = codes_of(p[i].widened(), inv);
+                reinterpret_cast<uint2 *>(const_cast<char *>(key[i] ? pg.k : pg.v))[(size_t)at[i] * 16 + piece] = amax[i] == 0.f ? make_uint2(0u, 0u) : codes;
+            }
+            if constexpr (i + 1 < N) self(self, std::integral_constant<int, i + 1>{});
+        };
+        write(write, std::integral_constant<int, 0>{});
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (at[i] != kNowhere) p[i].store(const_cast<char *>(key[i] ? pg.k : pg.v) + (size_t)at[i] * (kHeadDim * kBytes), piece);
     }
-}
-
-__device__ __forceinline__ unsigned int bf16_pair(float lo, float hi)
-{
-    // nearest, ties to even; NaN stays NaN
-    auto bits = [](float x) {
-        const unsigned int u = __float_as_uint(x);
-        return x != x ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
-    };
-    return bits(lo) | (bits(hi) << 16);
 }
 
 template <int DT, bool BF16>
@@ -649,63 +699,66 @@ __global__ __launch_bounds__(kBlock) void paged_gather_kernel(PagedShape sh, Pag
                                                               const int32_t *__restrict__ count, char *__restrict__ k_out,
                                                               char *__restrict__ v_out, int Tn, int shift)
 {
-    const int b = blockIdx.z, piece = threadIdx.x & 15, local = threadIdx.x >> 4;
-    constexpr int kBytes = BF16 ? 2 : 4;
-    MovedRow m[kMoveUnroll];
-    Piece p[kMoveUnroll];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, piece = lane & 15, rg = lane >> 4;
+    constexpr int kBytes = BF16 ? 2 : 4, N = kMoveUnroll<BF16>;
+    const Places pl = find_places<BF16>(sh, start, count, Tn, shift, lane, w, [&](Places &x, int b, bool key, int s, int token) {
+        x.lo = (unsigned int)((b * (key ? sh.k : sh.H) + s) * (long long)Tn + token);        // (row of an output of 256 bytes and more a row)
+        x.hi = key ? kIsKey : 0u;
+    });
+    if (!__any(pl.lo != kNowhere)) return;
+    unsigned int at[N], to[N];
+    bool key[N];
+    RawPiece<BF16> p[N];
+    u32x2 codes[N];
+    float scale[N];
 #pragma unroll
-    for (int i = 0; i < kMoveUnroll; ++i) {
-        m[i] = moved_row(sh, start, count, Tn, shift, local + i * (kBlock / 16), b);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[i].x[e] = 0.f;
-        if (!m[i].there) continue;
-        const bool key = m[i].stream < sh.k;
-        const char *rows = key ? pg.k : pg.v;
+    for (int i = 0; i < N; ++i) {
+        const int r = i * 4 + rg;
+        at[i] = (unsigned int)__shfl((int)pl.at, r);
+        to[i] = (unsigned int)__shfl((int)pl.lo, r);
+        key[i] = __shfl((int)pl.hi, r) != 0;
+        if (at[i] == kNowhere) continue;
+        const char *rows = key[i] ? pg.k : pg.v;
         if constexpr (DT == DT_E4M3) {
-            const uint2 codes = reinterpret_cast<const uint2 *>(rows)[(size_t)m[i].at * 16 + piece];
-            const float scale = (key ? pg.k_scales : pg.v_scales)[m[i].at];
-            const unsigned int x[2] = {codes.x, codes.y};
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[e], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[e], true);
-                p[i].x[4 * e] = lo.x * scale;
-                p[i].x[4 * e + 1] = lo.y * scale;
-                p[i].x[4 * e + 2] = hi.x * scale;
-                p[i].x[4 * e + 3] = hi.y * scale;
-            }
+            codes[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(rows) + (size_t)at[i] * 16 + piece);
+            scale[i] = (key[i] ? pg.k_scales : pg.v_scales)[at[i]];
         } else {
-            p[i] = load_piece<BF16>(rows + (size_t)m[i].at * (kHeadDim * kBytes), piece);
+            p[i].load(rows + (size_t)at[i] * (kHeadDim * kBytes), piece);
         }
     }
 #pragma unroll
-    for (int i = 0; i < kMoveUnroll; ++i) {
-        if (!m[i].there && !m[i].zero) continue;
-        const bool key = m[i].stream < sh.k;
-        const int streams = key ? sh.k : sh.H, s = key ? m[i].stream : m[i].stream - sh.k;
-        const size_t row = ((size_t)b * streams + s) * Tn + m[i].token;
-        char *o = key ? k_out : v_out;
-        if constexpr (DT == DT_BF16) {
-            reinterpret_cast<uint4 *>(o)[row * 16 + piece] = packed(p[i]);
-        } else if constexpr (BF16) {
-            const float *x = p[i].x;
-            reinterpret_cast<uint4 *>(o)[row * 16 + piece] = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
-        } else {
-            store_floats(reinterpret_cast<float *>(o) + row * kHeadDim + piece * 8, p[i].x);
+    for (int i = 0; i < N; ++i) {
+        if (to[i] == kNowhere) continue;
+        if (at[i] == kNowhere) {
+#pragma unroll
+            for (auto &x : p[i].x) x = u32x4{0u, 0u, 0u, 0u};
+        } else if constexpr (DT == DT_E4M3) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[i][e], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[i][e], true);
+                f[4 * e] = lo.x * scale[i];
+                f[4 * e + 1] = lo.y * scale[i];
+                f[4 * e + 2] = hi.x * scale[i];
+                f[4 * e + 3] = hi.y * scale[i];
+            }
+            p[i].set(f);
         }
+        p[i].store((key[i] ? k_out : v_out) + (size_t)to[i] * (kHeadDim * kBytes), piece);
     }
 }
 
-// tokens per workgroup, as a power of two: all of them up to kMoveRows
-int move_shift(int Tn)
+// tokens per workgroup, as a power of two: all of them up to `rows`
+int move_shift(int Tn, int rows)
 {
     int shift = 0;
-    while ((1 << shift) < Tn && (1 << shift) < kMoveRows) ++shift;
+    while ((1 << shift) < Tn && (1 << shift) < rows) ++shift;
     return shift;
 }
 
-dim3 move_grid(const PagedShape &sh, int Tn, int shift)
+dim3 move_grid(const PagedShape &sh, int Tn, int shift, int rows)
 {
-    const int streams = kMoveRows >> shift;
+    const int streams = rows >> shift;
     return dim3((unsigned int)((Tn + (1 << shift) - 1) >> shift), (unsigned int)((sh.k + sh.H + streams - 1) / streams), (unsigned int)sh.B);
 }
 
@@ -797,10 +850,10 @@ int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *
                         int64_t v_stride, const int32_t *rep, const int32_t *start, const int32_t *count, int Tn, int dtype,
                         int cache_dtype, hipStream_t stream)
 {
-    const int shift = move_shift(Tn);
+    const int rows = move_rows(dtype == CHAI_BF16), shift = move_shift(Tn, rows);
     const char *kc = static_cast<const char *>(k_new), *vc = static_cast<const char *>(v_new);
     auto go = [&](auto *kernel) {
-        return (int)launch_kernel(kernel, move_grid(sh, Tn, shift), dim3(kBlock), 0, stream, KernelEvents(), sh, pg, kc, vc, k_stride, v_stride,
+        return (int)launch_kernel(kernel, move_grid(sh, Tn, shift, rows), dim3(kBlock), 0, stream, KernelEvents(), sh, pg, kc, vc, k_stride, v_stride,
                                   rep, start, count, Tn, shift);
     };
     if (cache_dtype == CHAI_E4M3) return dtype == CHAI_BF16 ? go(paged_append_kernel<DT_E4M3, true>) : go(paged_append_kernel<DT_E4M3, false>);
@@ -810,10 +863,10 @@ int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *
 int launch_paged_gather(const PagedShape &sh, const PagedPages &pg, const int32_t *start, const int32_t *count, void *k_out, void *v_out,
                         int Tn, int dtype, int cache_dtype, hipStream_t stream)
 {
-    const int shift = move_shift(Tn);
+    const int rows = move_rows(dtype == CHAI_BF16), shift = move_shift(Tn, rows);
     char *ko = static_cast<char *>(k_out), *vo = static_cast<char *>(v_out);
     auto go = [&](auto *kernel) {
-        return (int)launch_kernel(kernel, move_grid(sh, Tn, shift), dim3(kBlock), 0, stream, KernelEvents(), sh, pg, start, count, ko, vo, Tn,
+        return (int)launch_kernel(kernel, move_grid(sh, Tn, shift, rows), dim3(kBlock), 0, stream, KernelEvents(), sh, pg, start, count, ko, vo, Tn,
                                   shift);
     };
     if (cache_dtype == CHAI_E4M3) return dtype == CHAI_BF16 ? go(paged_gather_kernel<DT_E4M3, true>) : go(paged_gather_kernel<DT_E4M3, false>);
