@@ -661,8 +661,8 @@ int chai_paged_decode_attention(const void *q, const void *k_pages, const void *
     if (st == CHAI_OK)
         st = check_paged_decode(q, head_to_cluster, rep_heads, seq_lens, T_max, out, workspace, workspace_bytes, &sh, &plan);
     if (st != CHAI_OK || B == 0) return st;
-    return hip_status(launch_paged_attention(sh, pg, q, dtype, cache_dtype, head_to_cluster, rep_heads, scale, out, workspace, plan,
-                                             static_cast<hipStream_t>(stream)));
+    return hip_status(launch_paged_attention(sh, pg, q, nullptr, nullptr, dtype, cache_dtype, head_to_cluster, rep_heads, scale, out,
+                                             workspace, plan, static_cast<hipStream_t>(stream)));
 }
 
 int chai_paged_decode_step(const void *q, const void *k_new, const void *v_new, void *k_pages, void *v_pages, float *k_scales,
@@ -682,10 +682,8 @@ int chai_paged_decode_step(const void *q, const void *k_new, const void *v_new, 
     if (st != CHAI_OK) return st;
     if (!aligned16(k_new) || !aligned16(v_new)) return CHAI_ERR_ALIGN;
     if (B == 0) return CHAI_OK;
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    const int e = launch_paged_append(sh, pg, k_new, v_new, kHeadDim, kHeadDim, rep_heads, nullptr, nullptr, 1, dtype, cache_dtype, s);
-    if (e != (int)hipSuccess) return CHAI_ERR_HIP;
-    return hip_status(launch_paged_attention(sh, pg, q, dtype, cache_dtype, head_to_cluster, rep_heads, scale, out, workspace, plan, s));
+    return hip_status(launch_paged_attention(sh, pg, q, k_new, v_new, dtype, cache_dtype, head_to_cluster, rep_heads, scale, out,
+                                             workspace, plan, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -155,10 +155,11 @@ constexpr int kMaxPagedBatch = 4096;     // rows: two levels of 64 lanes add up 
 constexpr int kMaxPagedTokens = 1 << 24;
 PagedPlan make_paged_plan(int B, int H, int k, int T_max);
 void set_page_division(PagedShape *sh);
-// h2c = rep = NULL: every head its own cluster (k = H)
-int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const void *q, int dtype, int cache_dtype, const int32_t *h2c,
-                           const int32_t *rep, float scale, float *out, void *workspace, const PagedPlan &plan, hipStream_t stream);
-// start = NULL: the one new token of every row, at its last position (sh.lens)
+// h2c = rep = NULL: every head its own cluster (k = H).  k_new / v_new [B,H,d] (or NULL): the last position of every row is the token
+// being decoded, its rows are taken from there and written to the pages by the same kernels.
+int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const void *q, const void *k_new, const void *v_new, int dtype,
+                           int cache_dtype, const int32_t *h2c, const int32_t *rep, float scale, float *out, void *workspace,
+                           const PagedPlan &plan, hipStream_t stream);
 int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *k_new, const void *v_new, int64_t k_stride,
                         int64_t v_stride, const int32_t *rep, const int32_t *start, const int32_t *count, int Tn, int dtype,
                         int cache_dtype, hipStream_t stream);

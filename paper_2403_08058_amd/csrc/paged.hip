@@ -26,8 +26,9 @@ __device__ __forceinline__ int block_of(const PagedShape &sh, int pos)
     return (int)((__umulhi((unsigned int)pos, sh.div_mul) + (unsigned int)pos) >> sh.div_shift);
 }
 
-// positions of row b that are attended to
-__device__ __forceinline__ int row_len(const PagedShape &sh, int b) { return min(max(sh.lens[b], 0), sh.T_max); }
+// positions of a row that are attended to
+__device__ __forceinline__ int taken_len(const PagedShape &sh, int given) { return min(max(given, 0), sh.T_max); }
+__device__ __forceinline__ int row_len(const PagedShape &sh, int b) { return taken_len(sh, sh.lens[b]); }
 
 // ---------------------------------------------------------------------------------------------------------
 // How the work of a ragged batch is dealt out.  A unit is one batch of a wave's loads (16 rows of fp32, 32 of bf16, 64 of codes);
@@ -48,7 +49,7 @@ __device__ __forceinline__ unsigned int wave_scan(unsigned int x, int lane)
 template <int U>
 struct Deal {
     unsigned int incl, mine;                 // lane l: units of one stream over rows up to and with its own, and of its own rows
-    int len;                                 // (up to 64 rows) of the lane's row
+    int given;                               // (up to 64 rows) seq_lens of the lane's row
     int span;                                // rows per lane
     unsigned int total;                      // units of one stream over all rows
 
@@ -57,18 +58,18 @@ struct Deal {
     __device__ __forceinline__ Deal(const PagedShape &sh, int lane)
     {
         span = (sh.B + 63) / 64;
-        len = 0;
+        given = 0;
         mine = 0u;
         for (int i = 0; i < span; ++i) {
             const int b = lane * span + i;
-            len = b < sh.B ? row_len(sh, min(b, sh.B - 1)) : 0;
-            mine += units(len);
+            given = b < sh.B ? sh.lens[min(b, sh.B - 1)] : 0;
+            mine += units(taken_len(sh, given));
         }
         incl = wave_scan(mine, lane);
         total = (unsigned int)__builtin_amdgcn_readlane((int)incl, 63);
     }
 
-    __device__ __forceinline__ int len_of(const PagedShape &sh, int b) const { return span == 1 ? __builtin_amdgcn_readlane(len, b) : row_len(sh, b); }
+    __device__ __forceinline__ int given_len(const PagedShape &sh, int b) const { return span == 1 ? __builtin_amdgcn_readlane(given, b) : sh.lens[b]; }
 
     __device__ __forceinline__ unsigned int quota(int streams, const PagedSplit &sp) const
     {
@@ -113,6 +114,14 @@ template <int U>
 struct Walk {
     unsigned int x, x0, x1, ua, ue, n_row, first;        // n_row: units of the stream; first: units of one stream before row b
     int b, s, len;
+    int fresh;                                           // the position being decoded, -1: none (it is past T_max)
+    __device__ __forceinline__ void enter(const PagedShape &sh, const Deal<U> &deal)
+    {
+        const int given = deal.given_len(sh, b);
+        len = taken_len(sh, given);
+        fresh = given <= sh.T_max ? len - 1 : -1;
+        n_row = Deal<U>::units(len);
+    }
     __device__ __forceinline__ bool begin(const PagedShape &sh, const Deal<U> &deal, unsigned int worker, int streams, const PagedSplit &sp, int lane)
     {
         const unsigned int quota = deal.quota(streams, sp), n = deal.total * (unsigned int)streams;
@@ -120,8 +129,7 @@ struct Walk {
         x = x0 = worker * quota;
         x1 = min(x0 + quota, n);
         b = deal.row_at(sh, x / (unsigned int)streams, lane, &first);
-        len = deal.len_of(sh, b);
-        n_row = Deal<U>::units(len);
+        enter(sh, deal);
         const unsigned int at = x - first * (unsigned int)streams;
         s = (int)(at / n_row);
         ua = at - (unsigned int)s * n_row;
@@ -136,8 +144,8 @@ struct Walk {
             s = 0;
             first += n_row;
             do {
-                len = deal.len_of(sh, ++b);              // (units are left, so a row is)
-                n_row = Deal<U>::units(len);
+                ++b;                                     // (units are left, so a row is)
+                enter(sh, deal);
             } while (n_row == 0u);
         }
         ua = 0;
@@ -182,12 +190,18 @@ __device__ __forceinline__ unsigned int pool_row(const PagedShape &sh, int at, u
     return at < 0 ? 0u : (unsigned int)(at * streams + s) * (unsigned int)sh.page + (unsigned int)(row - block_of(sh, row) * sh.page);
 }
 
-template <int DT>
+// ONCE: nobody else reads these rows
+template <int DT, bool ONCE = true>
 __device__ __forceinline__ void request(u32x4 (&buf)[kUnroll], const char *rows, unsigned int row, unsigned int lane_off)
 {
 #pragma unroll
-    for (int i = 0; i < kUnroll; ++i)
-        buf[i] = stream16(rows + (size_t)(unsigned int)__builtin_amdgcn_readlane((int)row, i) * Tile<DT>::ROW_BYTES + lane_off);
+    for (int i = 0; i < kUnroll; ++i) {
+        unsigned long long base = (unsigned long long)rows + (unsigned long long)(unsigned int)__builtin_amdgcn_readlane((int)row, i) * Tile<DT>::ROW_BYTES;
+        asm("" : "+s"(base));                // a scalar base and the lanes' offset (else 64-bit additions per lane, and their registers)
+        const auto *p = reinterpret_cast<const u32x4 __attribute__((address_space(1))) *>(reinterpret_cast<const char __attribute__((address_space(1))) *>(base) + lane_off);
+        buf[i] = ONCE ? __builtin_nontemporal_load(p) : *p;
+    }
+    asm volatile("" ::: "memory");           // asked for here and not where they are used, one unit later
 }
 
 // scores of a unit: lane cg < 8 of a lane group gets that of load cg, row rg + cg * RPW of the unit
@@ -197,8 +211,10 @@ __device__ __forceinline__ float dots(const u32x4 (&kb)[kUnroll], const float (&
     float mine = 0.f;
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
+        u32x4 raw = kb[i];
+        if (DT == DT_E4M3) asm("" : "+v"(raw), "+v"(mine));      // one row is widened at a time (all at once they take 130 registers)
         float f[Tile<DT>::EPL];
-        unpack(kb[i], f);
+        unpack(raw, f);
         float dot = 0.f;
 #pragma unroll
         for (int e = 0; e < Tile<DT>::EPL; ++e) dot = fmaf(qf[e], f[e], dot);
@@ -226,8 +242,10 @@ __device__ __forceinline__ void weigh(float (&acc)[Tile<DT>::EPL], u32x4 (&vb)[k
     }
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
+        u32x4 raw = vb[i];
+        if (DT == DT_E4M3) asm("" : "+v"(raw), "+v"(acc[0]));
         float f[Tile<DT>::EPL];
-        unpack(vb[i], f);
+        unpack(raw, f);
 #pragma unroll
         for (int e = 0; e < Tile<DT>::EPL; ++e) acc[e] = fmaf(pv[i], f[e], acc[e]);
     }
@@ -276,6 +294,62 @@ __device__ __forceinline__ float scaled(float dot, float scale, float row_scale)
     return DT == DT_E4M3 ? (scale * row_scale) * dot : scale * dot;
 }
 
+// ---------------------------------------------------------------------------------------------------------
+// The row of the token being decoded, taken from k_new / v_new in the place of what the cache holds there.  A lane has the sixteen bytes
+// of the row that it would have loaded, quantised as the append does (the eight lanes of a row of codes together).
+// ---------------------------------------------------------------------------------------------------------
+template <int DT>
+struct FreshRow {
+    u32x4 raw;
+    float scale;
+    __device__ __forceinline__ FreshRow(const char *rows, size_t row, int cg, int q_dtype)
+    {
+        scale = 1.f;
+        if constexpr (DT == DT_E4M3) {
+            float f[16], amax = 0.f;
+            load_query<DT>(rows, row, cg, q_dtype, f);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(f[e]));
+            amax = dpp_max<0xB1>(amax);
+            amax = dpp_max<0x4E>(amax);
+            amax = dpp_max<0x141>(amax);
+            const float inv = 448.0f / amax;
+            scale = amax == 0.f ? 0.f : amax / 448.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = fminf(fmaxf(f[4 * i + e] * inv, -448.0f), 448.0f);
+                raw[i] = amax == 0.f ? 0u : e4m3_codes(y[0], y[1], y[2], y[3]);
+            }
+        } else {
+            raw = *reinterpret_cast<const u32x4 *>(rows + row * Tile<DT>::ROW_BYTES + cg * 16);
+        }
+    }
+    // to row `at` of the pool, by one lane group
+    __device__ __forceinline__ void store(const char *rows, const float *scales, unsigned int at, int cg) const
+    {
+        *reinterpret_cast<u32x4 *>(const_cast<char *>(rows) + (size_t)at * Tile<DT>::ROW_BYTES + cg * 16) = raw;
+        if (DT == DT_E4M3 && cg == 0) const_cast<float *>(scales)[at] = scale;
+    }
+};
+
+// Row `local` of a unit whose loads are in buf and begin at rows `row` of the pool becomes the fresh one.
+template <int DT>
+__device__ __forceinline__ void take_fresh(const FreshRow<DT> &fresh, u32x4 (&buf)[kUnroll], float &row_scale, const char *rows, const float *scales, int at, unsigned int row,
+                                           int local, bool keep, int cg, int rg)
+{
+    const int load = local / Tile<DT>::RPW, group = local % Tile<DT>::RPW;
+    if (__builtin_amdgcn_readlane(at, load) < 0) return;     // in no page
+    const unsigned int to = (unsigned int)__builtin_amdgcn_readlane((int)row, load) + (unsigned int)group;
+    if (rg != group) return;
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i)
+        if (i == load) buf[i] = fresh.raw;
+    if (DT == DT_E4M3 && cg == load) row_scale = fresh.scale;
+    if (keep) fresh.store(rows, scales, to, cg);
+}
+
 constexpr float kPagedDown = 0x1p-24f;       // times kMaxPagedTokens weights of at most 1: at most 1
 constexpr float kPagedLarge = 0x1p120f;
 
@@ -286,91 +360,161 @@ constexpr float kPagedLarge = 0x1p120f;
 // A stream that ends inside the wave's units and began there goes to `out` as acc / l; of others acc / l goes to `partial` and (m, l)
 // to `recs` of the wave, two of each (its first units, its last ones), and paged_join_kernel puts them together.
 // ---------------------------------------------------------------------------------------------------------
-template <int DT, bool IDENT>
-__global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 3 : 4) void paged_attend_kernel(
-    PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q, int q_dtype, const int32_t *__restrict__ h2c,
-    const int32_t *__restrict__ rep, float scale, float *__restrict__ partial, float2 *__restrict__ recs, float *__restrict__ out)
+// One wave's share of a stream: units ua, ua + step, .. below ue of head h of row b, as weighted mean acc (all lane groups have it), the
+// reference m and the sum of exponentials l.  The key of the token being decoded goes to slot c if it is the head's own (IDENT).
+template <int DT, bool IDENT, bool APPEND>
+__device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPages &pg, const char *__restrict__ q, int q_dtype, const int32_t *__restrict__ table,
+                                             float scale, const char *__restrict__ k_new, const char *__restrict__ v_new, int b, int h, int c, int r, int len, int fresh,
+                                             unsigned int ua, unsigned int ue, unsigned int step, float *strip, int lane, float (&acc)[Tile<DT>::EPL], float &m, float &l)
 {
     using TL = Tile<DT>;
     constexpr int U = TL::BATCH;
+    const int cg = lane % TL::LPR, rg = lane / TL::LPR;
+    const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
+    float qf[TL::EPL], l_run, down = 1.f;
+    load_query<DT>(q, (size_t)b * sh.H + r, cg, q_dtype, qf);
+    for (;;) {
+        unsigned int u0 = ua;
+        asm volatile("" : "+s"(u0));         // (what the first unit asks for is not kept for the second time around)
+        u32x4 kb[kUnroll], vb[kUnroll];
+        float ks = 1.f, vs = 1.f;
+        int at = look_up<DT>(sh, table, u0, ue, len, lane), at1 = look_up<DT>(sh, table, u0 + step, ue, len, lane);
+        unsigned int krow = pool_row<DT>(sh, at, u0, sh.k, c, lane), vrow = pool_row<DT>(sh, at, u0, sh.H, h, lane);
+        request<DT, IDENT>(kb, pg.k, krow, lane_off);
+        if (DT == DT_E4M3) ks = pg.k_scales[krow + (at < 0 ? 0 : rg)];
+        request<DT>(vb, pg.v, vrow, lane_off);
+        if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at < 0 ? 0 : rg)];
+#pragma unroll
+        for (int e = 0; e < TL::EPL; ++e) acc[e] = 0.f;
+        m = -INFINITY;
+        l_run = 0.f;
+#pragma unroll 1
+        for (unsigned int u = u0; u < ue; u += step) {
+            const int at2 = look_up<DT>(sh, table, u + 2 * step, ue, len, lane);
+            const bool has_fresh = APPEND && fresh >= (int)(u * U) && fresh < (int)((u + 1) * U);
+            if (has_fresh) take_fresh<DT>(FreshRow<DT>(k_new, (size_t)b * sh.H + r, cg, q_dtype), kb, ks, pg.k, pg.k_scales, at, krow, fresh - (int)(u * U), IDENT, cg, rg);
+            const float mine = dots<DT>(kb, qf, cg);
+            const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
+            const float sv = there ? scaled<DT>(mine, scale, ks) : -INFINITY;
+            krow = pool_row<DT>(sh, at1, u + step, sh.k, c, lane);
+            request<DT, IDENT>(kb, pg.k, krow, lane_off);
+            if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
+            if (__any(sv > m)) {
+                const float m_new = fmaxf(m, wave_max(sv));
+                const float f = __expf(m - m_new);
+#pragma unroll
+                for (int e = 0; e < TL::EPL; ++e) acc[e] *= f;
+                l_run *= f;
+                m = m_new;
+            }
+            const float p = __expf(sv - (m == -INFINITY ? 0.f : m)) * down;
+            l_run += p;
+            if (has_fresh) take_fresh<DT>(FreshRow<DT>(v_new, (size_t)b * sh.H + h, cg, q_dtype), vb, vs, pg.v, pg.v_scales, at, vrow, fresh - (int)(u * U), true, cg, rg);
+            weigh<DT>(acc, vb, DT == DT_E4M3 ? (there ? p * vs : 0.f) : p, there, strip, cg, rg);
+            vrow = pool_row<DT>(sh, at1, u + step, sh.H, h, lane);
+            request<DT>(vb, pg.v, vrow, lane_off);
+            if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
+            at = at1;
+            at1 = at2;
+        }
+        // lane groups; sums beyond the largest float (the quotient is not) are taken again with smaller weights
+        bool large = false;
+#pragma unroll
+        for (int e = 0; e < TL::EPL; ++e) {
+#pragma unroll
+            for (int o = TL::LPR; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
+            large = large || !(fabsf(acc[e]) <= kPagedLarge);
+        }
+        if (!__any(large) || down != 1.f) break;
+        down = kPagedDown;
+    }
+    l = wave_sum(l_run);
+#pragma unroll
+    for (int e = 0; e < TL::EPL; ++e) acc[e] = l == 0.f ? 0.f : acc[e] / l;
+    l /= down;
+}
+
+template <int DT, bool APPEND>
+__global__ __launch_bounds__(kBlock, 3) void paged_attend_kernel(
+    PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q, int q_dtype, float scale, const char *__restrict__ k_new,
+    const char *__restrict__ v_new, float *__restrict__ partial, float2 *__restrict__ recs, float *__restrict__ out)
+{
+    using TL = Tile<DT>;
     __shared__ float strip[kWaves][64];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned int worker = blockIdx.x * kWaves + w;
-    const int cg = lane % TL::LPR, rg = lane / TL::LPR;
-    const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
-
-    const Deal<U> deal(sh, lane);
-    Walk<U> wk;
+    const Deal<TL::BATCH> deal(sh, lane);
+    Walk<TL::BATCH> wk;
     if (!wk.begin(sh, deal, worker, sh.H, sp, lane)) return;
     do {
-        const int b = wk.b, h = wk.s, len = wk.len;
-        const int c = IDENT ? h : min(max(h2c[(size_t)b * sh.H + h], 0), sh.k - 1);
-        const int r = IDENT ? h : min(max(rep[(size_t)b * sh.k + c], 0), sh.H - 1);
-        const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
-        float qf[TL::EPL];
-        load_query<DT>(q, (size_t)b * sh.H + r, cg, q_dtype, qf);
-
-        float acc[TL::EPL], m_ref, l_run, down = 1.f;
-        for (;;) {
-            u32x4 kb[kUnroll], vb[kUnroll];
-            float ks = 1.f, vs = 1.f;
-            int at = look_up<DT>(sh, table, wk.ua, wk.ue, len, lane), at1 = look_up<DT>(sh, table, wk.ua + 1, wk.ue, len, lane);
-            unsigned int krow = pool_row<DT>(sh, at, wk.ua, sh.k, c, lane), vrow = pool_row<DT>(sh, at, wk.ua, sh.H, h, lane);
-            request<DT>(kb, pg.k, krow, lane_off);
-            if (DT == DT_E4M3) ks = pg.k_scales[krow + (at < 0 ? 0 : rg)];
-            request<DT>(vb, pg.v, vrow, lane_off);
-            if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at < 0 ? 0 : rg)];
-#pragma unroll
-            for (int e = 0; e < TL::EPL; ++e) acc[e] = 0.f;
-            m_ref = -INFINITY;
-            l_run = 0.f;
-            for (unsigned int u = wk.ua; u < wk.ue; ++u) {
-                const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
-                const float mine = dots<DT>(kb, qf, cg);
-                const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
-                const float sv = there ? scaled<DT>(mine, scale, ks) : -INFINITY;
-                krow = pool_row<DT>(sh, at1, u + 1, sh.k, c, lane);
-                request<DT>(kb, pg.k, krow, lane_off);
-                if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
-                if (__any(sv > m_ref)) {
-                    const float m_new = fmaxf(m_ref, wave_max(sv));
-                    const float f = __expf(m_ref - m_new);
-#pragma unroll
-                    for (int e = 0; e < TL::EPL; ++e) acc[e] *= f;
-                    l_run *= f;
-                    m_ref = m_new;
-                }
-                const float p = __expf(sv - (m_ref == -INFINITY ? 0.f : m_ref)) * down;
-                l_run += p;
-                weigh<DT>(acc, vb, DT == DT_E4M3 ? (there ? p * vs : 0.f) : p, there, strip[w], cg, rg);
-                vrow = pool_row<DT>(sh, at1, u + 1, sh.H, h, lane);
-                request<DT>(vb, pg.v, vrow, lane_off);
-                if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
-                at = at1;
-                at1 = at2;
-            }
-            // lane groups; sums beyond the largest float (the quotient is not) are taken again with smaller weights
-            bool large = false;
-#pragma unroll
-            for (int e = 0; e < TL::EPL; ++e) {
-#pragma unroll
-                for (int o = TL::LPR; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
-                large = large || !(fabsf(acc[e]) <= kPagedLarge);
-            }
-            if (!__any(large) || down != 1.f) break;
-            down = kPagedDown;
-        }
-        const float l = wave_sum(l_run);
-#pragma unroll
-        for (int e = 0; e < TL::EPL; ++e) acc[e] = l == 0.f ? 0.f : acc[e] / l;
-        if (wk.whole()) {
-            if (rg == 0) store_floats(out + ((size_t)b * sh.H + h) * kHeadDim + cg * TL::EPL, acc);
-        } else {
-            const size_t slot = wk.slot(worker);
-            if (rg == 0) store_floats(partial + slot * kHeadDim + cg * TL::EPL, acc);
-            if (lane == 0) recs[slot] = make_float2(m_ref, l / down);
-        }
+        float acc[TL::EPL], m, l;
+        attend_units<DT, true, APPEND>(sh, pg, q, q_dtype, sh.table + (size_t)wk.b * sh.max_blocks, scale, k_new, v_new, wk.b, wk.s, wk.s, wk.s, wk.len, wk.fresh,
+                                       wk.ua, wk.ue, 1u, strip[w], lane, acc, m, l);
+        const size_t slot = wk.slot(worker);
+        float *o = wk.whole() ? out + ((size_t)wk.b * sh.H + wk.s) * kHeadDim : partial + slot * kHeadDim;
+        if (lane < TL::LPR) store_floats(o + lane * TL::EPL, acc);
+        if (lane == 0 && !wk.whole()) recs[slot] = make_float2(m, l);
     } while (wk.next(sh, deal, sh.H));
+}
+
+// Short rows: a workgroup of kRowWaves waves per (head, row), no parts and one launch.  The members of a cluster then each read its keys
+// (out of L2), and head h writes the new token's key to every slot that it represents.
+template <int DT, bool IDENT, bool APPEND, int kRowWaves>
+__global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_rows_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ q, int q_dtype,
+                                                                    const int32_t *__restrict__ h2c, const int32_t *__restrict__ rep, float scale,
+                                                                    const char *__restrict__ k_new, const char *__restrict__ v_new, float *__restrict__ out)
+{
+    using TL = Tile<DT>;
+    constexpr unsigned int U = TL::BATCH;
+    __shared__ float strip[kRowWaves][64];
+    __shared__ float acc_lds[kRowWaves][kHeadDim];
+    __shared__ float2 rec_lds[kRowWaves];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = blockIdx.x, b = blockIdx.y;
+    const int cg = lane % TL::LPR, rg = lane / TL::LPR;
+    const int c = IDENT ? h : min(max(h2c[(size_t)b * sh.H + h], 0), sh.k - 1);
+    const int given = sh.lens[b], len = taken_len(sh, given), fresh = given <= sh.T_max ? len - 1 : -1;
+    const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
+    const int r = IDENT ? h : min(max(rep[(size_t)b * sh.k + c], 0), sh.H - 1);
+    const unsigned int n = (unsigned int)(len + U - 1) / U;
+    float acc[TL::EPL], m = -INFINITY, l = 0.f;
+    if ((unsigned int)w < n) {
+        attend_units<DT, IDENT, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, b, h, c, r, len, fresh, (unsigned int)w, n, (unsigned int)kRowWaves, strip[w], lane,
+                                        acc, m, l);
+        if (rg == 0) store_floats(&acc_lds[w][cg * TL::EPL], acc);
+    }
+    if (lane == 0) rec_lds[w] = make_float2(m, l);
+    if (APPEND && !IDENT && fresh >= 0 && w == kRowWaves - 1) {
+        const int block = block_of(sh, fresh);
+        const int at = table[min(block, sh.max_blocks - 1)];
+        for (int j0 = 0; j0 < sh.k; j0 += 64) {
+            const int rj = j0 + lane < sh.k ? rep[(size_t)b * sh.k + j0 + lane] : -1;
+            unsigned long long left = __ballot(rj >= 0 && min(rj, sh.H - 1) == h);
+            if (left == 0ull || (unsigned int)at >= (unsigned int)sh.n_pages) continue;
+            const FreshRow<DT> row(k_new, (size_t)b * sh.H + h, cg, q_dtype);
+            for (; left != 0ull; left &= left - 1ull) {
+                const int j = j0 + __ffsll((long long)left) - 1;
+                if (rg == 0) row.store(pg.k, pg.k_scales, (unsigned int)(at * sh.k + j) * (unsigned int)sh.page + (unsigned int)(fresh - block * sh.page), cg);
+            }
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < kHeadDim) {
+        float M = -INFINITY, L = 0.f, sum = 0.f, wt[kRowWaves];
+#pragma unroll
+        for (int i = 0; i < kRowWaves; ++i) M = fmaxf(M, rec_lds[i].x);
+#pragma unroll
+        for (int i = 0; i < kRowWaves; ++i) {
+            const float2 rc = rec_lds[i];
+            wt[i] = rc.x == -INFINITY ? rc.y : rc.y * __expf(rc.x - M);      // (only -inf scores: 0, NaN among them: NaN)
+            L += wt[i];
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+        for (int i = 0; i < kRowWaves; ++i)
+            if ((unsigned int)i < n) sum = fmaf(wt[i] * inv, acc_lds[i][threadIdx.x], sum);
+        out[((size_t)b * sh.H + h) * kHeadDim + threadIdx.x] = sum;
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -378,11 +522,11 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 3 : 4) void paged_attend_ke
 // Scores: a wave streams keys of its units, writes s[b][j][t] (-inf where nothing is to be attended to, whole units) and the maximum
 // and sum of exponentials of every stretch: `whole` of a stream that it took alone, else `parts` of the wave.
 // ---------------------------------------------------------------------------------------------------------
-template <int DT>
-__global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 5 : 6) void paged_scores_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q,
+template <int DT, bool APPEND>
+__global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? (APPEND ? 4 : 5) : 6) void paged_scores_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q,
                                                                  int q_dtype, const int32_t *__restrict__ rep, float scale, int T_pad,
-                                                                 float *__restrict__ scores, float2 *__restrict__ whole,
-                                                                 float2 *__restrict__ parts)
+                                                                 const char *__restrict__ k_new, float *__restrict__ scores,
+                                                                 float2 *__restrict__ whole, float2 *__restrict__ parts)
 {
     using TL = Tile<DT>;
     constexpr int U = TL::BATCH;
@@ -396,7 +540,7 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 5 : 6) void paged_scores_ke
     if (!wk.begin(sh, deal, worker, sh.k, sp, lane)) return;
     do {
         const int b = wk.b, j = wk.s, len = wk.len;
-        const int r = min(max(rep[(size_t)b * sh.k + j], 0), sh.H - 1);
+        const int rj = rep[(size_t)b * sh.k + j], r = min(max(rj, 0), sh.H - 1);
         const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
         u32x4 kb[kUnroll];
         float ks = 1.f;
@@ -410,6 +554,8 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 5 : 6) void paged_scores_ke
         float m_run = -INFINITY, l_run = 0.f;            // of the scores that this lane has seen
         for (unsigned int u = wk.ua; u < wk.ue; ++u) {
             const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
+            if (APPEND && wk.fresh >= (int)(u * U) && wk.fresh < (int)((u + 1) * U))
+                take_fresh<DT>(FreshRow<DT>(k_new, (size_t)b * sh.H + r, cg, q_dtype), kb, ks, pg.k, pg.k_scales, at, krow, wk.fresh - (int)(u * U), rj >= 0, cg, rg);
             const float mine = dots<DT>(kb, qf, cg);
             const int t = (int)(u * U) + cg * TL::RPW + rg;
             const bool there = cg < kUnroll && at >= 0 && t < len;
@@ -445,10 +591,10 @@ __device__ __forceinline__ float2 merge(const float2 *parts, const Takers &tk, i
 }
 
 // Values: a wave streams the values of its units, each weighed by its cluster's probability exp(s - M) / L.
-template <int DT>
-__global__ __launch_bounds__(kBlock, DT == DT_F32 ? 6 : (DT == DT_BF16 ? 5 : 4)) void paged_values_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, PagedSplit sp_scores,
+template <int DT, bool APPEND>
+__global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 4 : 5) void paged_values_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, PagedSplit sp_scores,
                                                                  const int32_t *__restrict__ h2c, int T_pad,
-                                                                 const float *__restrict__ scores, const float2 *__restrict__ whole,
+                                                                 const char *__restrict__ v_new, int q_dtype, const float *__restrict__ scores, const float2 *__restrict__ whole,
                                                                  const float2 *__restrict__ parts, float *__restrict__ partial,
                                                                  float *__restrict__ out)
 {
@@ -485,6 +631,8 @@ __global__ __launch_bounds__(kBlock, DT == DT_F32 ? 6 : (DT == DT_BF16 ? 5 : 4))
             const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
             const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
             const float p = there ? __expf(sv - M) * inv : 0.f;
+            if (APPEND && wk.fresh >= (int)(u * U) && wk.fresh < (int)((u + 1) * U))
+                take_fresh<DT>(FreshRow<DT>(v_new, (size_t)b * sh.H + h, cg, q_dtype), vb, vs, pg.v, pg.v_scales, at, vrow, wk.fresh - (int)(u * U), true, cg, rg);
             weigh<DT>(acc, vb, DT == DT_E4M3 ? (there ? p * vs : 0.f) : p, there, strip[w], cg, rg);
             vrow = pool_row<DT>(sh, at1, u + 1, sh.H, h, lane);
             request<DT>(vb, pg.v, vrow, lane_off);
@@ -504,48 +652,59 @@ __global__ __launch_bounds__(kBlock, DT == DT_F32 ? 6 : (DT == DT_BF16 ? 5 : 4))
 }
 
 // Streams that several waves took.  WEIGHED (one pass): out = mean of their parts, each weighed by its sum of exponentials times
-// exp(its reference - the largest); else their sum.  A wave per (row, head), two columns per lane; streams that one wave took are left
+// exp(its reference - the largest); else their sum.  JW waves per (row, head), two columns per lane; streams that one wave took are left
 // alone, rows without a position get 0.
-template <int U, bool WEIGHED>
+template <int U, bool WEIGHED, int JW>
 __global__ __launch_bounds__(kBlock) void paged_join_kernel(PagedShape sh, PagedSplit sp, const float *__restrict__ partial,
                                                             const float2 *__restrict__ recs, float *__restrict__ out)
 {
+    __shared__ float2 sums[kWaves][64];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = blockIdx.x * kWaves + w, b = blockIdx.y;
-    if (h >= sh.H) return;
+    const int h = blockIdx.x * (kWaves / JW) + w / JW, b = blockIdx.y, jw = w % JW;
+    if (h >= sh.H) return;                               // (with JW = kWaves none)
     float2 *o = reinterpret_cast<float2 *>(out + ((size_t)b * sh.H + h) * kHeadDim) + lane;
     const Deal<U> deal(sh, lane);
-    const unsigned int n_row = Deal<U>::units(deal.len_of(sh, b));
+    const unsigned int n_row = Deal<U>::units(taken_len(sh, deal.given_len(sh, b)));
     if (n_row == 0u) {
-        *o = make_float2(0.f, 0.f);
+        if (jw == 0) *o = make_float2(0.f, 0.f);
         return;
     }
     const Takers tk(deal.before(sh, b, lane) * (unsigned int)sh.H + (unsigned int)h * n_row, n_row, deal.quota(sh.H, sp));
     if (tk.n == 1) return;
+    float2 sum = make_float2(0.f, 0.f);
+    // the first parts are asked for before their weights are known
+    const unsigned int per = (tk.n + JW - 1) / JW, i_begin = min((unsigned int)jw * per, tk.n), i_end = min(i_begin + per, tk.n);
+    auto part = [&](unsigned int i) { return reinterpret_cast<const float2 *>(partial + tk.slot(min(i, tk.n - 1)) * kHeadDim)[lane]; };
+    float2 v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = part(i_begin + j);
     float2 st = make_float2(0.f, 1.f);
     if (WEIGHED) st = merge(recs, tk, lane);
     const float inv = st.y == 0.f ? 0.f : 1.f / st.y;
-    float2 sum = make_float2(0.f, 0.f);
-    for (unsigned int i0 = 0; i0 < tk.n; i0 += 64) {
-        float wt = 0.f;
-        if (WEIGHED && i0 + lane < tk.n) {
-            const float2 rc = recs[tk.slot(i0 + lane)];
+    for (unsigned int i = i_begin; i < i_end; i += 8) {
+        float wt = 1.f;
+        if (WEIGHED) {
+            const float2 rc = recs[tk.slot(min(i + (lane & 7), tk.n - 1))];
             wt = (rc.x == -INFINITY ? rc.y : rc.y * __expf(rc.x - st.x)) * inv;
         }
-        const unsigned int here = min(tk.n - i0, 64u);
-        for (unsigned int i = 0; i < here; i += 8) {
-            float2 v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                v[j] = reinterpret_cast<const float2 *>(partial + tk.slot(i0 + min(i + j, here - 1)) * kHeadDim)[lane];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float wj = WEIGHED ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), (int)min(i + j, 63u))) : 1.f;
-                if (i + j < here) {
-                    sum.x = fmaf(wj, v[j].x, sum.x);
-                    sum.y = fmaf(wj, v[j].y, sum.y);
-                }
+        for (int j = 0; j < 8; ++j) {
+            const float wj = WEIGHED ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), j)) : 1.f;
+            if (i + j < i_end) {
+                sum.x = fmaf(wj, v[j].x, sum.x);
+                sum.y = fmaf(wj, v[j].y, sum.y);
             }
+            v[j] = part(i + 8 + j);
+        }
+    }
+    if (JW > 1) {
+        sums[w][lane] = sum;
+        __syncthreads();
+        if (jw != 0) return;
+#pragma unroll
+        for (int i = 1; i < JW; ++i) {
+            sum.x += sums[w + i][lane].x;
+            sum.y += sums[w + i][lane].y;
         }
     }
     *o = sum;
@@ -574,14 +733,7 @@ __device__ __forceinline__ Places find_places(const PagedShape &sh, const int32_
 {
     const int b = blockIdx.z;
     Places pl = {kNowhere, kNowhere, 0u};
-    int n = Tn, first;
-    if (start == nullptr) {                  // the last position of every row
-        first = sh.lens[b] - 1;
-        n = first >= 0 && first < sh.T_max ? 1 : 0;
-    } else {
-        first = start[b];
-        if (count != nullptr) n = min(max(count[b], 0), Tn);
-    }
+    const int first = start[b], n = count != nullptr ? min(max(count[b], 0), Tn) : Tn;
     const int local = (lane / 4) * (kBlock / 16) + w * 4 + lane % 4;
     const int token = (int)(blockIdx.x << shift) + (local & ((1 << shift) - 1));
     const int stream = blockIdx.y * (move_rows(BF16) >> shift) + (local >> shift);
@@ -768,12 +920,27 @@ int unit_rows(int cache_dtype) { return cache_dtype == CHAI_F32 ? Tile<DT_F32>::
 
 }  // namespace
 
-// Waves of a launch.  Of the two passes, which have one stream of loads each, in us for 1024 / 2048 / 3072 / 4096 / 6144 to 8192:
-// scores of 64 x 8 rows of codes (4096 tokens at most, most short) 23.1 / 17.2 / 16.6 / 16.2 / 16.5 and values of 64 x 32 - / 49 / 45
-// / 41.6 / 44.6; 4 x 32 of 32768 bf16 tokens within 2 % up to 4096, 173 / 163 with 8192.  One pass has keys and values in flight: 8 x
-// 52 heads of up to 1777 bf16 tokens 37.4 / 36.4 / 41 / 43.6 / 42.
+// Waves of a launch; between 2048 and 6144 of them times differ by 3 % (one pass, which has keys and values in flight: 1024 to 4096).
 constexpr unsigned int kStreamWorkers = 4096, kAttendWorkers = 2048, kPagedWorkers = 4096;
-constexpr unsigned int kPagedParts = 64;               // most waves of one stream
+// Most waves of one stream: with 64 the parts of few heads take longer to join (1 x 32 dense heads of 2048 bf16 tokens 18.6 us, 15.5 with
+// 32, 16.6 with 16; of 8192 35.3, 31.8 and 38.4).
+constexpr unsigned int kPagedParts = 32;
+
+// Whether a workgroup takes a whole head's row (one launch) or shares of all rows' units go to independent waves (two or three).  Rows /
+// shares, in us, the new token's rows written too; "to T": lengths spread evenly up to T, else all T:
+// * clustered, 32 heads in 8, one row: 577 bf16 tokens 8.5 / 12.5, 1024 13.7 / 13.5, of codes 12.3 / 15.0, 2048 16.7 / 15.9, of fp32 577
+//   14.7 / 17.0; 4 x 72 in 16: to 577 bf16 16.3 / 20.3, 1024 31.5 / 30.4, to 1024 22.9 / 23.9; 16 x 32: 577 25.4 / 32.6, 1024 39.9 / 40.8,
+//   to 2048 of codes 29.6 / 33.9, all 2048 43.7 / 43.0, to 577 fp32 28.6 / 33.2; 32 x 32: 577 bf16 44.4 / 48.3, 1024 72 / 66.  Members of a
+//   cluster each read its keys, which costs long rows of many heads more than the launches.
+// * dense: 4 x 72 at 1024 bf16 34.3 / 33.8, 8 x 52 38.7 / 43.6, to 2048 50.6 / 45.7, 32 x 32 to 2048 98 / 104, all 2048 of codes 89 / 101.
+// Rows of one length fill the chip from some 768 heads on whatever the length; the rule goes by the longest row, the others' are not known.
+static bool take_rows(int B, int H, int T_max, int cache, bool dense)
+{
+    const long long heads = (long long)B * H, bytes = (long long)T_max * kHeadDim * (cache == CHAI_F32 ? 4 : (cache == CHAI_BF16 ? 2 : 1));
+    return bytes <= (dense ? (heads >= 768 ? 512 : 256) : (heads <= 512 ? 256 : 160)) * 1024ll;
+}
+// Eight waves per row where a CU has one row at most, else four (1 x 32 of 577 bf16 tokens 8.5 against 10.3 us; 16 x 32 of 256 16.8 against 15.5).
+constexpr long long kFewHeads = 128;
 
 static int padded_tokens(int T_max) { return (T_max + 63) / 64 * 64; }
 
@@ -813,37 +980,50 @@ void set_page_division(PagedShape *sh)
     sh->div_mul = (unsigned int)((((1ull << s) - (unsigned long long)sh->page) << 32) / (unsigned long long)sh->page + 1ull);
 }
 
-template <int DT>
-static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, const char *q, int dtype, const int32_t *h2c, const int32_t *rep,
-                                 float scale, float *out, char *ws, const PagedPlan &plan, hipStream_t stream)
+template <int DT, bool APPEND>
+static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, const char *q, const char *k_new, const char *v_new, int dtype,
+                                 const int32_t *h2c, const int32_t *rep, float scale, float *out, char *ws, const PagedPlan &plan, hipStream_t stream)
 {
     constexpr int U = Tile<DT>::BATCH, cache = DT;
     float2 *recs = reinterpret_cast<float2 *>(ws + plan.off_recs), *whole = reinterpret_cast<float2 *>(ws + plan.off_whole);
     float *partial = reinterpret_cast<float *>(ws + plan.off_partial), *scores = reinterpret_cast<float *>(ws + plan.off_scores);
-    const dim3 block(kBlock), heads((unsigned int)(sh.H + kWaves - 1) / kWaves, (unsigned int)sh.B);
+    const dim3 block(kBlock), heads((unsigned int)sh.H, (unsigned int)sh.B);
     auto waves = [](const PagedSplit &sp) { return dim3((sp.workers + kWaves - 1) / kWaves); };
     const KernelEvents none;
+    if (take_rows(sh.B, sh.H, sh.T_max, DT, h2c == nullptr)) {
+        const bool few = (long long)sh.B * sh.H <= kFewHeads;
+        auto rows = [&](auto *kernel) {
+            return (int)launch_kernel(kernel, dim3((unsigned int)sh.H, (unsigned int)sh.B), dim3(few ? 512 : 256), 0, stream, none, sh, pg, q, dtype, h2c, rep, scale,
+                                      k_new, v_new, out);
+        };
+        if (h2c == nullptr) return few ? rows(paged_rows_kernel<DT, true, APPEND, 8>) : rows(paged_rows_kernel<DT, true, APPEND, 4>);
+        return few ? rows(paged_rows_kernel<DT, false, APPEND, 8>) : rows(paged_rows_kernel<DT, false, APPEND, 4>);
+    }
     if (h2c == nullptr) {
         const PagedSplit sp = make_paged_split(sh.B, sh.H, sh.T_max, cache, kAttendWorkers);
-        const hipError_t e = launch_kernel(paged_attend_kernel<DT, true>, waves(sp), block, 0, stream,
-                                           none, sh, pg, sp, q, dtype, h2c, rep, scale, partial, recs, out);
+        const hipError_t e = launch_kernel(paged_attend_kernel<DT, APPEND>, waves(sp), block, 0, stream, none, sh, pg, sp, q, dtype, scale, k_new, v_new, partial, recs, out);
         if (e != hipSuccess) return (int)e;
-        return (int)launch_kernel(paged_join_kernel<U, true>, heads, block, 0, stream, none, sh, sp, partial, recs, out);
+        return (int)launch_kernel(paged_join_kernel<U, true, kWaves>, heads, block, 0, stream, none, sh, sp, partial, recs, out);
     }
     const PagedSplit ss = make_paged_split(sh.B, sh.k, sh.T_max, cache, kStreamWorkers), sv = make_paged_split(sh.B, sh.H, sh.T_max, cache, kStreamWorkers);
     const int T_pad = padded_tokens(sh.T_max);
-    hipError_t e = launch_kernel(paged_scores_kernel<DT>, waves(ss), block, 0, stream, none, sh, pg, ss, q, dtype, rep, scale, T_pad, scores, whole, recs);
+    hipError_t e = launch_kernel(paged_scores_kernel<DT, APPEND>, waves(ss), block, 0, stream, none, sh, pg, ss, q, dtype, rep, scale, T_pad, k_new, scores, whole, recs);
     if (e != hipSuccess) return (int)e;
-    e = launch_kernel(paged_values_kernel<DT>, waves(sv), block, 0, stream, none, sh, pg, sv, ss, h2c, T_pad, scores, whole, recs, partial, out);
+    e = launch_kernel(paged_values_kernel<DT, APPEND>, waves(sv), block, 0, stream, none, sh, pg, sv, ss, h2c, T_pad, v_new, dtype, scores, whole, recs, partial, out);
     if (e != hipSuccess) return (int)e;
-    return (int)launch_kernel(paged_join_kernel<U, false>, heads, block, 0, stream, none, sh, sv, partial, nullptr, out);
+    return (int)launch_kernel(paged_join_kernel<U, false, kWaves>, heads, block, 0, stream, none, sh, sv, partial, nullptr, out);
 }
 
-int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const void *q, int dtype, int cache_dtype, const int32_t *h2c,
-                           const int32_t *rep, float scale, float *out, void *workspace, const PagedPlan &plan, hipStream_t stream)
+int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const void *q, const void *k_new, const void *v_new, int dtype, int cache_dtype,
+                           const int32_t *h2c, const int32_t *rep, float scale, float *out, void *workspace, const PagedPlan &plan, hipStream_t stream)
 {
-    auto *typed = cache_dtype == CHAI_F32 ? paged_attention_typed<DT_F32> : (cache_dtype == CHAI_BF16 ? paged_attention_typed<DT_BF16> : paged_attention_typed<DT_E4M3>);
-    return typed(sh, pg, static_cast<const char *>(q), dtype, h2c, rep, scale, out, static_cast<char *>(workspace), plan, stream);
+    auto go = [&](auto *typed) {
+        return typed(sh, pg, static_cast<const char *>(q), static_cast<const char *>(k_new), static_cast<const char *>(v_new), dtype, h2c, rep, scale, out,
+                     static_cast<char *>(workspace), plan, stream);
+    };
+    if (cache_dtype == CHAI_F32) return k_new ? go(paged_attention_typed<DT_F32, true>) : go(paged_attention_typed<DT_F32, false>);
+    if (cache_dtype == CHAI_BF16) return k_new ? go(paged_attention_typed<DT_BF16, true>) : go(paged_attention_typed<DT_BF16, false>);
+    return k_new ? go(paged_attention_typed<DT_E4M3, true>) : go(paged_attention_typed<DT_E4M3, false>);
 }
 
 int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *k_new, const void *v_new, int64_t k_stride,
