@@ -499,34 +499,44 @@ def alloc_workspace(B: int, H: int, k: int, T: int, d: int, dtype: int, device="
     return torch.empty((n,), dtype=torch.uint8, device=device)
 
 
-def _paged_shapes(fn, k_pages, v_pages, k_scales, v_scales, block_table, dtype, maps):
-    """(B, H, k, n_pages, page, max_blocks, d, cache dtype code) of a call on pages; what does not fit together is refused here:
-    the library is given sizes once and cannot see the tensors."""
-    n_pages, k, page, d = k_pages.shape
-    H = v_pages.shape[1]
-    if v_pages.shape != (n_pages, H, page, d) or v_pages.dtype != k_pages.dtype:
-        raise ValueError(f"{fn}: k_pages {tuple(k_pages.shape)} {k_pages.dtype} and v_pages {tuple(v_pages.shape)} "
-                         f"{v_pages.dtype} do not fit together")
-    if k_pages.dtype == torch.uint8:
-        if k_scales is None or v_scales is None or k_scales.shape != (n_pages, k, page) or v_scales.shape != (n_pages, H, page) \
-                or k_scales.dtype != torch.float32 or v_scales.dtype != torch.float32:
-            raise ValueError(f"{fn}: pages of codes need fp32 scales of shape [n_pages, streams, page]")
-        code = CHAI_E4M3
-    elif k_pages.dtype != dtype:
-        raise TypeError(f"{fn}: pages of {k_pages.dtype} beside tensors of {dtype}")
-    else:
-        code = CHAI_BF16 if dtype == torch.bfloat16 else CHAI_F32
-    B, max_blocks = block_table.shape
-    for t, shape in ((block_table, (B, max_blocks)), *maps):
-        if t is not None and (t.shape != (shape if isinstance(shape, tuple) else (B, shape)) or t.dtype != torch.int32):
-            raise ValueError(f"{fn}: int32 [{B}, ...] expected, got {t.dtype} {tuple(t.shape)}")
-    return B, H, k, n_pages, page, max_blocks, d, code
+_I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
+# (type of q and new rows, type of the pages) -> their codes
+_PAGED_CODES = {(torch.float32, torch.float32): (CHAI_F32, CHAI_F32), (torch.bfloat16, torch.bfloat16): (CHAI_BF16, CHAI_BF16),
+                (torch.float32, torch.uint8): (CHAI_F32, CHAI_E4M3), (torch.bfloat16, torch.uint8): (CHAI_BF16, CHAI_E4M3)}
 
 
-def _same(fn, shape, dtype, *tensors):
+def _misfit(fn, what):
+    raise ValueError(f"{fn}: {what}")
+
+
+def _paged_types(fn, dtype, k_pages, v_pages, k_scales, v_scales, n_pages, H, k, page, d):
+    """Codes of the types of a call on pages.  What does not fit together is refused in Python: the library is given every size once
+    and cannot see the tensors.  (These checks are most of a small call's host time: each attribute is asked for once.)"""
+    pages = k_pages.dtype
+    codes = _PAGED_CODES.get((dtype, pages))
+    if codes is None:
+        raise TypeError(f"{fn}: pages of {pages} beside tensors of {dtype}")
+    if v_pages.dtype is not pages or v_pages.shape != (n_pages, H, page, d):
+        _misfit(fn, f"k_pages {tuple(k_pages.shape)} {pages} and v_pages {tuple(v_pages.shape)} {v_pages.dtype} do not fit together")
+    if pages is _U8 and (k_scales is None or v_scales is None or k_scales.dtype is not _F32 or v_scales.dtype is not _F32
+                         or k_scales.shape != (n_pages, k, page) or v_scales.shape != (n_pages, H, page)):
+        _misfit(fn, "pages of codes need fp32 scales of shape [n_pages, streams, page]")
+    return codes
+
+
+def _ptrs(tensors):
+    """Addresses of device tensors that lie in one piece, None for None."""
+    out = []
     for t in tensors:
-        if t.shape != shape or t.dtype != dtype:
-            raise ValueError(f"{fn}: {dtype} {tuple(shape)} expected, got {t.dtype} {tuple(t.shape)}")
+        if t is None:
+            out.append(None)
+        else:
+            if not t.is_cuda:
+                raise ValueError("libchai takes device tensors")
+            if not t.is_contiguous():
+                raise ValueError("libchai takes contiguous tensors")
+            out.append(t.data_ptr())
+    return out
 
 
 def chai_paged_workspace_bytes(B: int, H: int, k: int, T_max: int, d: int = 128) -> int:
@@ -544,70 +554,78 @@ def chai_paged_append_kv(k_new, v_new, rep_heads, block_table, start, count, k_p
     of its pages k_pages [n_pages,k,page,d], v_pages [n_pages,H,page,d] (uint8: quantised, beside scales
     [n_pages,streams,page]).  rep_heads [B,k], or None for every head (k = H)."""
     fn = "chai_paged_append_kv"
-    B, H, k, n_pages, page, max_blocks, d, code = _paged_shapes(
-        fn, k_pages, v_pages, k_scales, v_scales, block_table, k_new.dtype,
-        ((rep_heads, k_pages.shape[1]), (start, start.shape[:1]), (count, start.shape[:1])))
-    nk, nv = k_new.shape[2], v_new.shape[2]
-    Tn = min(nk, nv) if Tn is None else Tn
-    _same(fn, (B, H, nk, d), k_new.dtype, k_new)
-    _same(fn, (B, H, nv, d), k_new.dtype, v_new)
-    _same(fn, (B,), torch.int32, start)
-    _check(fn, _lib.chai_paged_append_kv(_ptr(k_new), _ptr(v_new), nk * d, nv * d, _ptr(rep_heads), _ptr(block_table),
-                                         _ptr(start), _ptr(count), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales),
-                                         _ptr(v_scales), B, H, k, Tn, n_pages, page, max_blocks, d, dtype_code(k_new), code,
-                                         _stream(stream)))
+    n_pages, k, page, d = k_pages.shape
+    B, H, nk, _ = k_new.shape
+    nv = v_new.shape[2]
+    dtype = k_new.dtype
+    code, pages = _paged_types(fn, dtype, k_pages, v_pages, k_scales, v_scales, n_pages, H, k, page, d)
+    rows, max_blocks = block_table.shape
+    if k_new.shape != (B, H, nk, d) or v_new.shape != (B, H, nv, d) or v_new.dtype is not dtype:
+        _misfit(fn, f"k_new {tuple(k_new.shape)} {dtype} and v_new {tuple(v_new.shape)} {v_new.dtype} do not fit the pages")
+    if rows != B or block_table.dtype is not _I32 or start.shape != (B,) or start.dtype is not _I32 \
+            or (count is not None and (count.shape != (B,) or count.dtype is not _I32)) \
+            or (rep_heads is not None and (rep_heads.shape != (B, k) or rep_heads.dtype is not _I32)):
+        _misfit(fn, "int32 tables, starts, counts and maps for every row expected")
+    p = _ptrs((k_new, v_new, rep_heads, block_table, start, count, k_pages, v_pages, k_scales, v_scales))
+    _check(fn, _lib.chai_paged_append_kv(p[0], p[1], nk * d, nv * d, *p[2:], B, H, k, min(nk, nv) if Tn is None else Tn, n_pages,
+                                         page, max_blocks, d, code, pages, _stream(stream)))
 
 
 def chai_paged_gather_kv(k_pages, v_pages, block_table, start, count, k_out, v_out, k_scales=None, v_scales=None, stream=None):
     """Positions start[b] .. start[b]+count[b]-1 (None: all Tn) of every row's pages -> the first rows of k_out [B,k,Tn,d] and
     v_out [B,H,Tn,d] (fp32 or bf16; codes times their scales)."""
     fn = "chai_paged_gather_kv"
-    B, H, k, n_pages, page, max_blocks, d, code = _paged_shapes(
-        fn, k_pages, v_pages, k_scales, v_scales, block_table, k_out.dtype,
-        ((start, start.shape[:1]), (count, start.shape[:1])))
-    Tn = k_out.shape[2]
-    _same(fn, (B, k, Tn, d), k_out.dtype, k_out)
-    _same(fn, (B, H, Tn, d), k_out.dtype, v_out)
-    _same(fn, (B,), torch.int32, start)
-    _check(fn, _lib.chai_paged_gather_kv(_ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(block_table),
-                                         _ptr(start), _ptr(count), _ptr(k_out), _ptr(v_out), B, H, k, Tn, n_pages, page,
-                                         max_blocks, d, dtype_code(k_out), code, _stream(stream)))
+    n_pages, k, page, d = k_pages.shape
+    B, H, Tn, _ = v_out.shape
+    dtype = k_out.dtype
+    code, pages = _paged_types(fn, dtype, k_pages, v_pages, k_scales, v_scales, n_pages, H, k, page, d)
+    rows, max_blocks = block_table.shape
+    if k_out.shape != (B, k, Tn, d) or v_out.shape != (B, H, Tn, d) or v_out.dtype is not dtype:
+        _misfit(fn, f"k_out {tuple(k_out.shape)} {dtype} and v_out {tuple(v_out.shape)} {v_out.dtype} do not fit the pages")
+    if rows != B or block_table.dtype is not _I32 or start.shape != (B,) or start.dtype is not _I32 \
+            or (count is not None and (count.shape != (B,) or count.dtype is not _I32)):
+        _misfit(fn, "int32 tables, starts and counts for every row expected")
+    p = _ptrs((k_pages, v_pages, k_scales, v_scales, block_table, start, count, k_out, v_out))
+    _check(fn, _lib.chai_paged_gather_kv(*p, B, H, k, Tn, n_pages, page, max_blocks, d, code, pages, _stream(stream)))
     return k_out, v_out
+
+
+def _paged_decode(fn, call, q, new, k_pages, v_pages, k_scales, v_scales, head_to_cluster, rep_heads, block_table, seq_lens, T_max,
+                  scale, out, workspace, stream):
+    n_pages, k, page, d = k_pages.shape
+    shape = q.shape
+    B, H, _ = shape
+    dtype = q.dtype
+    code, pages = _paged_types(fn, dtype, k_pages, v_pages, k_scales, v_scales, n_pages, H, k, page, d)
+    rows, max_blocks = block_table.shape
+    if shape != (B, H, d) or out.shape != shape or out.dtype is not _F32:
+        _misfit(fn, f"q {tuple(shape)} {dtype} and out {tuple(out.shape)} {out.dtype} do not fit the pages")
+    for t in new:
+        if t.shape != shape or t.dtype is not dtype:
+            _misfit(fn, f"new rows {tuple(t.shape)} {t.dtype} beside q {tuple(shape)} {dtype}")
+    if rows != B or block_table.dtype is not _I32 or seq_lens.shape != (B,) or seq_lens.dtype is not _I32 \
+            or (head_to_cluster is not None and (head_to_cluster.shape != (B, H) or head_to_cluster.dtype is not _I32)) \
+            or (rep_heads is not None and (rep_heads.shape != (B, k) or rep_heads.dtype is not _I32)):
+        _misfit(fn, "int32 tables, lengths and maps for every row expected")
+    p = _ptrs((q, *new, k_pages, v_pages, k_scales, v_scales, head_to_cluster, rep_heads, block_table, seq_lens, out, workspace))
+    _check(fn, call(*p[:-2], B, H, k, T_max, n_pages, page, max_blocks, d, code, pages, scale, p[-2], p[-1], workspace.nbytes,
+                    _stream(stream)))
+    return out
 
 
 def chai_paged_decode_attention(q, k_pages, v_pages, head_to_cluster, rep_heads, block_table, seq_lens, T_max: int, scale: float,
                                 out, workspace, k_scales=None, v_scales=None, stream=None):
     """One clustered decode step of one layer over pages: row b attends to its first seq_lens[b] positions.  Maps as for
     chai_decode_attention, or both None for a layer without clusters (k = H)."""
-    fn = "chai_paged_decode_attention"
-    B, H, k, n_pages, page, max_blocks, d, code = _paged_shapes(
-        fn, k_pages, v_pages, k_scales, v_scales, block_table, q.dtype,
-        ((head_to_cluster, v_pages.shape[1]), (rep_heads, k_pages.shape[1]), (seq_lens, seq_lens.shape[:1])))
-    _same(fn, (B, H, d), q.dtype, q)
-    _same(fn, (B, H, d), torch.float32, out)
-    _same(fn, (B,), torch.int32, seq_lens)
-    _check(fn, _lib.chai_paged_decode_attention(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales),
-                                                _ptr(head_to_cluster), _ptr(rep_heads), _ptr(block_table), _ptr(seq_lens), B,
-                                                H, k, T_max, n_pages, page, max_blocks, d, dtype_code(q), code, scale,
-                                                _ptr(out), _ptr(workspace), workspace.nbytes, _stream(stream)))
-    return out
+    return _paged_decode("chai_paged_decode_attention", _lib.chai_paged_decode_attention, q, (), k_pages, v_pages, k_scales, v_scales,
+                         head_to_cluster, rep_heads, block_table, seq_lens, T_max, scale, out, workspace, stream)
 
 
 def chai_paged_decode_step(q, k_new, v_new, k_pages, v_pages, head_to_cluster, rep_heads, block_table, seq_lens, T_max: int,
                            scale: float, out, workspace, k_scales=None, v_scales=None, stream=None):
     """Cache growth + attention in one call: position seq_lens[b]-1 of every row is taken from k_new / v_new [B,H,d]."""
-    fn = "chai_paged_decode_step"
-    B, H, k, n_pages, page, max_blocks, d, code = _paged_shapes(
-        fn, k_pages, v_pages, k_scales, v_scales, block_table, q.dtype,
-        ((head_to_cluster, v_pages.shape[1]), (rep_heads, k_pages.shape[1]), (seq_lens, seq_lens.shape[:1])))
-    _same(fn, (B, H, d), q.dtype, q, k_new, v_new)
-    _same(fn, (B, H, d), torch.float32, out)
-    _same(fn, (B,), torch.int32, seq_lens)
-    _check(fn, _lib.chai_paged_decode_step(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales),
-                                           _ptr(v_scales), _ptr(head_to_cluster), _ptr(rep_heads), _ptr(block_table),
-                                           _ptr(seq_lens), B, H, k, T_max, n_pages, page, max_blocks, d, dtype_code(q), code,
-                                           scale, _ptr(out), _ptr(workspace), workspace.nbytes, _stream(stream)))
-    return out
+    return _paged_decode("chai_paged_decode_step", _lib.chai_paged_decode_step, q, (k_new, v_new), k_pages, v_pages, k_scales, v_scales,
+                         head_to_cluster, rep_heads, block_table, seq_lens, T_max, scale, out, workspace, stream)
 
 
 class _Binding(types.ModuleType):

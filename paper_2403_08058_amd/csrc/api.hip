@@ -622,7 +622,7 @@ int chai_paged_append_kv(const void *k_new, const void *v_new, int64_t k_head_st
     if (st != CHAI_OK) return st;
     if (Tn < 0 || k_head_stride < (int64_t)Tn * d || v_head_stride < (int64_t)Tn * d || (k_head_stride & 7) || (v_head_stride & 7))
         return CHAI_ERR_SHAPE;
-    if (Tn > kMaxPagedTokens) return CHAI_ERR_UNSUPPORTED;
+    if (Tn > kMaxPagedTokens || (long long)B * (H + k) * Tn >= (1ll << 35)) return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(k_new) || !aligned16(v_new)) return CHAI_ERR_ALIGN;
     if (B == 0 || Tn == 0) return CHAI_OK;
     return hip_status(launch_paged_append(sh, pg, k_new, v_new, k_head_stride, v_head_stride, rep_heads, start, count, Tn, dtype,
@@ -641,7 +641,7 @@ int chai_paged_gather_kv(const void *k_pages, const void *v_pages, const float *
                                cache_dtype, &sh, &pg);
     if (st != CHAI_OK) return st;
     if (Tn < 0) return CHAI_ERR_SHAPE;
-    if (Tn > kMaxPagedTokens) return CHAI_ERR_UNSUPPORTED;
+    if (Tn > kMaxPagedTokens || (long long)B * (H + k) * Tn >= (1ll << 35)) return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(k_out) || !aligned16(v_out)) return CHAI_ERR_ALIGN;
     if (B == 0 || Tn == 0) return CHAI_OK;
     return hip_status(launch_paged_gather(sh, pg, start, count, k_out, v_out, Tn, dtype, cache_dtype, static_cast<hipStream_t>(stream)));

@@ -28,7 +28,8 @@ __device__ __forceinline__ int block_of(const PagedShape &sh, int pos)
 
 // positions of a row that are attended to
 __device__ __forceinline__ int taken_len(const PagedShape &sh, int given) { return min(max(given, 0), sh.T_max); }
-__device__ __forceinline__ int row_len(const PagedShape &sh, int b) { return taken_len(sh, sh.lens[b]); }
+__device__ __forceinline__ int given_of(const PagedShape &sh, int b) { return sh.lens != nullptr ? sh.lens[b] : sh.T_max; }
+__device__ __forceinline__ int row_len(const PagedShape &sh, int b) { return taken_len(sh, given_of(sh, b)); }
 
 // ---------------------------------------------------------------------------------------------------------
 // How the work of a ragged batch is dealt out.  A unit is one batch of a wave's loads (16 rows of fp32, 32 of bf16, 64 of codes);
@@ -62,14 +63,14 @@ struct Deal {
         mine = 0u;
         for (int i = 0; i < span; ++i) {
             const int b = lane * span + i;
-            given = b < sh.B ? sh.lens[min(b, sh.B - 1)] : 0;
+            given = b < sh.B ? given_of(sh, min(b, sh.B - 1)) : 0;
             mine += units(taken_len(sh, given));
         }
         incl = wave_scan(mine, lane);
         total = (unsigned int)__builtin_amdgcn_readlane((int)incl, 63);
     }
 
-    __device__ __forceinline__ int given_len(const PagedShape &sh, int b) const { return span == 1 ? __builtin_amdgcn_readlane(given, b) : sh.lens[b]; }
+    __device__ __forceinline__ int given_len(const PagedShape &sh, int b) const { return span == 1 ? __builtin_amdgcn_readlane(given, b) : given_of(sh, b); }
 
     __device__ __forceinline__ unsigned int quota(int streams, const PagedSplit &sp) const
     {
@@ -788,33 +789,21 @@ struct RawPiece {
     }
 };
 
-template <int DT, bool BF16>
-__global__ __launch_bounds__(kBlock) void paged_append_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ k_new,
-                                                              const char *__restrict__ v_new, long long k_stride, long long v_stride,
-                                                              const int32_t *__restrict__ rep, const int32_t *__restrict__ start,
-                                                              const int32_t *__restrict__ count, int Tn, int shift)
+// where position first + token of a row lies in a pool of `streams` streams (kNowhere beyond n tokens)
+__device__ __forceinline__ unsigned int place_of(const PagedShape &sh, const int32_t *table, int first, int token, int n, int streams, int s)
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, piece = lane & 15, rg = lane >> 4;
+    const int pos = (int)((unsigned int)first + (unsigned int)token), block = block_of(sh, max(pos, 0));
+    const int at = table[min(block, sh.max_blocks - 1)];
+    return token < n && pos >= 0 && block < sh.max_blocks && (unsigned int)at < (unsigned int)sh.n_pages
+               ? (unsigned int)(at * streams + s) * (unsigned int)sh.page + (unsigned int)(pos - block * sh.page) : kNowhere;
+}
+
+// Row i of every lane group to row at[i] of its pool.
+template <int DT, bool BF16>
+__device__ __forceinline__ void put_rows(const RawPiece<BF16> (&p)[kMoveUnroll<BF16>], const unsigned int (&at)[kMoveUnroll<BF16>], const bool (&key)[kMoveUnroll<BF16>],
+                                         const PagedPages &pg, int piece)
+{
     constexpr int kBytes = BF16 ? 2 : 4, N = kMoveUnroll<BF16>;
-    const Places pl = find_places<BF16>(sh, start, count, Tn, shift, lane, w, [&](Places &x, int b, bool key, int s, int token) {
-        const int h = key && rep != nullptr ? min(rep[(size_t)b * sh.k + s], sh.H - 1) : s;
-        if (h < 0) x.at = kNowhere;          // (a slot without a cluster keeps what it holds)
-        const unsigned long long from = (((unsigned long long)b * sh.H + max(h, 0)) * (key ? k_stride : v_stride) + (unsigned long long)token * kHeadDim) * kBytes;
-        x.lo = (unsigned int)from;
-        x.hi = (unsigned int)(from >> 32) | (key ? kIsKey : 0u);
-    });
-    if (!__any(pl.at != kNowhere)) return;
-    unsigned int at[N];
-    bool key[N];
-    RawPiece<BF16> p[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int r = i * 4 + rg;
-        at[i] = (unsigned int)__shfl((int)pl.at, r);
-        const unsigned int lo = (unsigned int)__shfl((int)pl.lo, r), hi = (unsigned int)__shfl((int)pl.hi, r);
-        key[i] = (hi & kIsKey) != 0u;
-        if (at[i] != kNowhere) p[i].load((key[i] ? k_new : v_new) + (((unsigned long long)(hi & ~kIsKey) << 32) | lo), piece);
-    }
     if constexpr (DT == DT_E4M3) {
         // lane i of a group turns the largest value of the group's row i into its scale and factor, then hands the factor on
         float amax[N], mine = 0.f;
@@ -844,6 +833,84 @@ __global__ __launch_bounds__(kBlock) void paged_append_kernel(PagedShape sh, Pag
         for (int i = 0; i < N; ++i)
             if (at[i] != kNowhere) p[i].store(const_cast<char *>(key[i] ? pg.k : pg.v) + (size_t)at[i] * (kHeadDim * kBytes), piece);
     }
+}
+
+template <int DT, bool BF16>
+__global__ __launch_bounds__(kBlock) void paged_append_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ k_new,
+                                                              const char *__restrict__ v_new, long long k_stride, long long v_stride,
+                                                              const int32_t *__restrict__ rep, const int32_t *__restrict__ start,
+                                                              const int32_t *__restrict__ count, int Tn, int shift)
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, piece = lane & 15, rg = lane >> 4;
+    constexpr int kBytes = BF16 ? 2 : 4, N = kMoveUnroll<BF16>;
+    const Places pl = find_places<BF16>(sh, start, count, Tn, shift, lane, w, [&](Places &x, int b, bool key, int s, int token) {
+        const int h = key && rep != nullptr ? min(rep[(size_t)b * sh.k + s], sh.H - 1) : s;
+        if (h < 0) x.at = kNowhere;          // (a slot without a cluster keeps what it holds)
+        const unsigned long long from = (((unsigned long long)b * sh.H + max(h, 0)) * (key ? k_stride : v_stride) + (unsigned long long)token * kHeadDim) * kBytes;
+        x.lo = (unsigned int)from;
+        x.hi = (unsigned int)(from >> 32) | (key ? kIsKey : 0u);
+    });
+    if (!__any(pl.at != kNowhere)) return;
+    unsigned int at[N];
+    bool key[N];
+    RawPiece<BF16> p[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int r = i * 4 + rg;
+        at[i] = (unsigned int)__shfl((int)pl.at, r);
+        const unsigned int lo = (unsigned int)__shfl((int)pl.lo, r), hi = (unsigned int)__shfl((int)pl.hi, r);
+        key[i] = (hi & kIsKey) != 0u;
+        if (at[i] != kNowhere) p[i].load((key[i] ? k_new : v_new) + (((unsigned long long)(hi & ~kIsKey) << 32) | lo), piece);
+    }
+    put_rows<DT, BF16>(p, at, key, pg, piece);
+}
+
+// The same for many rows: every wave takes its share of all rows' units, 4 * N tokens of one stream each, whatever the rows' lengths are.
+// (A unit's rows asked for before the ones before are stored take twice the registers and, with that, longer.)
+template <int DT, bool BF16>
+__global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? (BF16 ? 4 : 6) : 7) void paged_append_stream_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ k_new,
+                                                                        const char *__restrict__ v_new, long long k_stride, long long v_stride,
+                                                                        const int32_t *__restrict__ rep, const int32_t *__restrict__ start)
+{
+    constexpr int kBytes = BF16 ? 2 : 4, N = kMoveUnroll<BF16>, U = 4 * N;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane & 15, rg = lane >> 4;
+    const Deal<U> deal(sh, lane);
+    Walk<U> wk;
+    if (!wk.begin(sh, deal, blockIdx.x * kWaves + w, sh.k + sh.H, sp, lane)) return;
+    do {
+        const bool key = wk.s < sh.k;
+        const int s = key ? wk.s : wk.s - sh.k, streams = key ? sh.k : sh.H, b = wk.b, len = wk.len;
+        const int h = key && rep != nullptr ? min(rep[(size_t)b * sh.k + s], sh.H - 1) : s;
+        if (h < 0) continue;                 // a slot without a cluster keeps what it holds
+        const char *from = (key ? k_new : v_new) + ((size_t)b * sh.H + h) * (key ? k_stride : v_stride) * kBytes;
+        const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
+        const int first = start[b];
+        struct Unit {
+            unsigned int at;                 // of row `lane` of the unit
+            RawPiece<BF16> p[N];
+        };
+        auto request = [&](Unit &x, unsigned int u) {
+            x.at = place_of(sh, table, first, (int)(u * U) + lane, lane < U && u < wk.ue ? len : 0, streams, s);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x.p[i].load(from + (size_t)min((int)(u * U) + i * 4 + rg, len - 1) * (kHeadDim * kBytes), piece);
+            asm volatile("" ::: "memory");
+        };
+        auto put = [&](const Unit &x) {
+            unsigned int at[N];
+            bool keys[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                at[i] = (unsigned int)__shfl((int)x.at, i * 4 + rg);
+                keys[i] = key;
+            }
+            put_rows<DT, BF16>(x.p, at, keys, pg, piece);
+        };
+        Unit x;
+        for (unsigned int u = wk.ua; u < wk.ue; ++u) {
+            request(x, u);
+            put(x);
+        }
+    } while (wk.next(sh, deal, sh.k + sh.H));
 }
 
 template <int DT, bool BF16>
@@ -900,6 +967,76 @@ __global__ __launch_bounds__(kBlock) void paged_gather_kernel(PagedShape sh, Pag
     }
 }
 
+template <int DT, bool BF16>
+__global__ __launch_bounds__(kBlock, 8) void paged_gather_stream_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, const int32_t *__restrict__ start,
+                                                                        char *__restrict__ k_out, char *__restrict__ v_out)
+{
+    constexpr int kBytes = BF16 ? 2 : 4, N = kMoveUnroll<BF16>, U = 4 * N;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane & 15, rg = lane >> 4;
+    const Deal<U> deal(sh, lane);
+    Walk<U> wk;
+    if (!wk.begin(sh, deal, blockIdx.x * kWaves + w, sh.k + sh.H, sp, lane)) return;
+    do {
+        const bool key = wk.s < sh.k;
+        const int s = key ? wk.s : wk.s - sh.k, streams = key ? sh.k : sh.H, b = wk.b, len = wk.len;
+        const char *rows = key ? pg.k : pg.v;
+        const float *scales = key ? pg.k_scales : pg.v_scales;
+        char *to = (key ? k_out : v_out) + ((size_t)b * streams + s) * sh.T_max * (kHeadDim * kBytes);
+        const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
+        const int first = start[b];
+        auto look = [&](unsigned int u) { return place_of(sh, table, first, (int)(u * U) + lane, lane < U && u < wk.ue ? len : 0, streams, s); };
+        struct Unit {
+            unsigned int at;                 // of row `lane` of the unit
+            float scale;
+            RawPiece<BF16> p[N];
+            u32x2 codes[N];
+        };
+        auto request = [&](Unit &x, unsigned int at) {
+            x.at = at;
+            if (DT == DT_E4M3) x.scale = scales[at != kNowhere ? at : 0u];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const unsigned int r = (unsigned int)__shfl((int)at, i * 4 + rg);
+                const size_t row = r != kNowhere ? r : 0u;
+                if constexpr (DT == DT_E4M3) x.codes[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(rows) + row * 16 + piece);
+                else x.p[i].load(rows + row * (kHeadDim * kBytes), piece);
+            }
+            asm volatile("" ::: "memory");
+        };
+        auto put = [&](Unit &x, unsigned int u) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int token = (int)(u * U) + i * 4 + rg;
+                if constexpr (DT == DT_E4M3) {
+                    const float scale = __shfl(x.scale, i * 4 + rg);
+                    float f[8];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x.codes[i][e], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x.codes[i][e], true);
+                        f[4 * e] = lo.x * scale;
+                        f[4 * e + 1] = lo.y * scale;
+                        f[4 * e + 2] = hi.x * scale;
+                        f[4 * e + 3] = hi.y * scale;
+                    }
+                    x.p[i].set(f);
+                }
+                const bool there = (unsigned int)__shfl((int)x.at, i * 4 + rg) != kNowhere;
+#pragma unroll
+                for (auto &y : x.p[i].x) y = there ? y : u32x4{0u, 0u, 0u, 0u};
+                if (token < len) x.p[i].store(to + (size_t)token * (kHeadDim * kBytes), piece);
+            }
+        };
+        Unit x;
+        unsigned int next = look(wk.ua);
+        for (unsigned int u = wk.ua; u < wk.ue; ++u) {
+            const unsigned int at = next;
+            next = look(u + 1);
+            request(x, at);
+            put(x, u);
+        }
+    } while (wk.next(sh, deal, sh.k + sh.H));
+}
+
 // tokens per workgroup, as a power of two: all of them up to `rows`
 int move_shift(int Tn, int rows)
 {
@@ -922,9 +1059,12 @@ int unit_rows(int cache_dtype) { return cache_dtype == CHAI_F32 ? Tile<DT_F32>::
 
 // Waves of a launch; between 2048 and 6144 of them times differ by 3 % (one pass, which has keys and values in flight: 1024 to 4096).
 constexpr unsigned int kStreamWorkers = 4096, kAttendWorkers = 2048, kPagedWorkers = 4096;
-// Most waves of one stream: with 64 the parts of few heads take longer to join (1 x 32 dense heads of 2048 bf16 tokens 18.6 us, 15.5 with
-// 32, 16.6 with 16; of 8192 35.3, 31.8 and 38.4).
-constexpr unsigned int kPagedParts = 32;
+// Most waves of one stream: of dense attention and of values, whose parts are joined (1 x 52 dense heads of 8192 bf16 tokens 42.2 us, 43.5
+// with 64; 1 x 32 of 2048 15.5, 16.6 with 16), and of scores, of whose parts only two numbers are read again (4 x 4 streams of 32768 bf16
+// tokens and their values 212 us with 32, 197 with 64 or 128; 1 x 8 streams 84.9, 72.2 and 66.4).
+constexpr unsigned int kPagedParts = 32, kScoreParts = 128;
+// The parts of a head are joined by four waves, those of many heads by one each (64 x 32 heads 69.1 / 67.6 us in all, 1 x 52 25.7 / 27.7).
+constexpr long long kJoinedByOne = 512;
 
 // Whether a workgroup takes a whole head's row (one launch) or shares of all rows' units go to independent waves (two or three).  Rows /
 // shares, in us, the new token's rows written too; "to T": lengths spread evenly up to T, else all T:
@@ -961,13 +1101,31 @@ PagedPlan make_paged_plan(int B, int H, int k, int T_max)
     return pl;
 }
 
-static PagedSplit make_paged_split(int B, int streams, int T_max, int cache_dtype, unsigned int workers)
+static PagedSplit make_paged_split(int B, int streams, int T_max, int cache_dtype, unsigned int workers, unsigned int parts)
 {
     PagedSplit sp;
     const int u = unit_rows(cache_dtype);
     const long long row_units = ((long long)T_max + u - 1) / u, units = row_units * B * streams;
     sp.workers = (unsigned int)(units < (long long)workers ? units : workers);
-    sp.least = (unsigned int)((row_units + kPagedParts - 1) / kPagedParts);
+    sp.least = (unsigned int)((row_units + parts - 1) / parts);
+    return sp;
+}
+
+// Whether rows are moved by workgroups, a block of tokens each up to the longest row's, or by waves that are dealt units of what there is.
+// Workgroups / waves, in us: 16 x 40 streams of 256 tokens quantised 14.6 / 15.9, 512 25.6 / 26.3, 1024 44.8 / 47, evenly up to 1024 35.2 /
+// 27.6 and up to 2043 61.5 / 50; read back 12.1 / 13.6, 26.3 / 25.3, 48 / 47, 34.7 / 27.0 and 68 / 52.8; bf16 of 512 copied 33.3 / 32.5, read
+// back 32.5 / 31; fp32 70.7 / 79.6 and 97.8 / 70.7.  Many waves of few units each: 4096 to 8192 take up to a tenth longer than 16384 and more.
+constexpr long long kStreamedRows = 262144;
+constexpr unsigned int kMoveWorkers = 32768;
+static bool stream_moves(const PagedShape &sh, int Tn) { return Tn >= 32 && (long long)sh.B * (sh.k + sh.H) * Tn >= kStreamedRows; }
+
+static PagedSplit make_move_split(int B, int streams, int Tn, int dtype)
+{
+    const int u = 4 * (dtype == CHAI_BF16 ? kMoveUnroll<true> : kMoveUnroll<false>);
+    const long long units = ((long long)Tn + u - 1) / u * B * streams;
+    PagedSplit sp;
+    sp.workers = (unsigned int)(units < (long long)kMoveWorkers ? units : kMoveWorkers);
+    sp.least = 1u;
     return sp;
 }
 
@@ -987,9 +1145,14 @@ static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, con
     constexpr int U = Tile<DT>::BATCH, cache = DT;
     float2 *recs = reinterpret_cast<float2 *>(ws + plan.off_recs), *whole = reinterpret_cast<float2 *>(ws + plan.off_whole);
     float *partial = reinterpret_cast<float *>(ws + plan.off_partial), *scores = reinterpret_cast<float *>(ws + plan.off_scores);
-    const dim3 block(kBlock), heads((unsigned int)sh.H, (unsigned int)sh.B);
+    const dim3 block(kBlock);
     auto waves = [](const PagedSplit &sp) { return dim3((sp.workers + kWaves - 1) / kWaves); };
     const KernelEvents none;
+    auto join = [&](auto *one, auto *four, const PagedSplit &sp) {
+        const bool many = (long long)sh.B * sh.H > kJoinedByOne;
+        return (int)launch_kernel(many ? one : four, dim3((unsigned int)(many ? (sh.H + kWaves - 1) / kWaves : sh.H), (unsigned int)sh.B), block, 0, stream, none, sh, sp,
+                                  partial, recs, out);
+    };
     if (take_rows(sh.B, sh.H, sh.T_max, DT, h2c == nullptr)) {
         const bool few = (long long)sh.B * sh.H <= kFewHeads;
         auto rows = [&](auto *kernel) {
@@ -1000,18 +1163,18 @@ static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, con
         return few ? rows(paged_rows_kernel<DT, false, APPEND, 8>) : rows(paged_rows_kernel<DT, false, APPEND, 4>);
     }
     if (h2c == nullptr) {
-        const PagedSplit sp = make_paged_split(sh.B, sh.H, sh.T_max, cache, kAttendWorkers);
+        const PagedSplit sp = make_paged_split(sh.B, sh.H, sh.T_max, cache, kAttendWorkers, kPagedParts);
         const hipError_t e = launch_kernel(paged_attend_kernel<DT, APPEND>, waves(sp), block, 0, stream, none, sh, pg, sp, q, dtype, scale, k_new, v_new, partial, recs, out);
         if (e != hipSuccess) return (int)e;
-        return (int)launch_kernel(paged_join_kernel<U, true, kWaves>, heads, block, 0, stream, none, sh, sp, partial, recs, out);
+        return join(paged_join_kernel<U, true, 1>, paged_join_kernel<U, true, kWaves>, sp);
     }
-    const PagedSplit ss = make_paged_split(sh.B, sh.k, sh.T_max, cache, kStreamWorkers), sv = make_paged_split(sh.B, sh.H, sh.T_max, cache, kStreamWorkers);
+    const PagedSplit ss = make_paged_split(sh.B, sh.k, sh.T_max, cache, kStreamWorkers, kScoreParts), sv = make_paged_split(sh.B, sh.H, sh.T_max, cache, kStreamWorkers, kPagedParts);
     const int T_pad = padded_tokens(sh.T_max);
     hipError_t e = launch_kernel(paged_scores_kernel<DT, APPEND>, waves(ss), block, 0, stream, none, sh, pg, ss, q, dtype, rep, scale, T_pad, k_new, scores, whole, recs);
     if (e != hipSuccess) return (int)e;
     e = launch_kernel(paged_values_kernel<DT, APPEND>, waves(sv), block, 0, stream, none, sh, pg, sv, ss, h2c, T_pad, v_new, dtype, scores, whole, recs, partial, out);
     if (e != hipSuccess) return (int)e;
-    return (int)launch_kernel(paged_join_kernel<U, false, kWaves>, heads, block, 0, stream, none, sh, sv, partial, nullptr, out);
+    return join(paged_join_kernel<U, false, 1>, paged_join_kernel<U, false, kWaves>, sv);
 }
 
 int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const void *q, const void *k_new, const void *v_new, int dtype, int cache_dtype,
@@ -1030,6 +1193,18 @@ int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *
                         int64_t v_stride, const int32_t *rep, const int32_t *start, const int32_t *count, int Tn, int dtype,
                         int cache_dtype, hipStream_t stream)
 {
+    if (stream_moves(sh, Tn)) {
+        PagedShape each = sh;
+        each.lens = count;
+        each.T_max = Tn;
+        const PagedSplit sp = make_move_split(sh.B, sh.k + sh.H, Tn, dtype);
+        auto stream_rows = [&](auto *kernel) {
+            return (int)launch_kernel(kernel, dim3((sp.workers + kWaves - 1) / kWaves), dim3(kBlock), 0, stream, KernelEvents(), each, pg, sp,
+                                      static_cast<const char *>(k_new), static_cast<const char *>(v_new), k_stride, v_stride, rep, start);
+        };
+        if (cache_dtype == CHAI_E4M3) return dtype == CHAI_BF16 ? stream_rows(paged_append_stream_kernel<DT_E4M3, true>) : stream_rows(paged_append_stream_kernel<DT_E4M3, false>);
+        return dtype == CHAI_BF16 ? stream_rows(paged_append_stream_kernel<DT_BF16, true>) : stream_rows(paged_append_stream_kernel<DT_F32, false>);
+    }
     const int rows = move_rows(dtype == CHAI_BF16), shift = move_shift(Tn, rows);
     const char *kc = static_cast<const char *>(k_new), *vc = static_cast<const char *>(v_new);
     auto go = [&](auto *kernel) {
@@ -1043,6 +1218,18 @@ int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *
 int launch_paged_gather(const PagedShape &sh, const PagedPages &pg, const int32_t *start, const int32_t *count, void *k_out, void *v_out,
                         int Tn, int dtype, int cache_dtype, hipStream_t stream)
 {
+    if (stream_moves(sh, Tn)) {
+        PagedShape each = sh;
+        each.lens = count;
+        each.T_max = Tn;
+        const PagedSplit sp = make_move_split(sh.B, sh.k + sh.H, Tn, dtype);
+        auto stream_rows = [&](auto *kernel) {
+            return (int)launch_kernel(kernel, dim3((sp.workers + kWaves - 1) / kWaves), dim3(kBlock), 0, stream, KernelEvents(), each, pg, sp, start,
+                                      static_cast<char *>(k_out), static_cast<char *>(v_out));
+        };
+        if (cache_dtype == CHAI_E4M3) return dtype == CHAI_BF16 ? stream_rows(paged_gather_stream_kernel<DT_E4M3, true>) : stream_rows(paged_gather_stream_kernel<DT_E4M3, false>);
+        return dtype == CHAI_BF16 ? stream_rows(paged_gather_stream_kernel<DT_BF16, true>) : stream_rows(paged_gather_stream_kernel<DT_F32, false>);
+    }
     const int rows = move_rows(dtype == CHAI_BF16), shift = move_shift(Tn, rows);
     char *ko = static_cast<char *>(k_out), *vo = static_cast<char *>(v_out);
     auto go = [&](auto *kernel) {

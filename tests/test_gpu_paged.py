@@ -339,6 +339,8 @@ def copies(s):
     (33, 7, 64, 300, [10, 0], [290, 131]),
     (4, 2, 16, 50, [-7, 360, 2147483640], None),           # begins before the first position, ends past the table
     (3, 1, 128, 129, [64], [200]),                         # more than there are
+    (60, 12, 16, 390, [0] * 11 + [7], None),               # more than 262144 rows: shares of all rows' units
+    (100, 28, 24, 333, [3, 0, 67, 200, -5, 1, 9, 0], [333, 0, 1, 200, 32, 31, 33, 64]),
 ])
 def test_append_and_gather(cache, H, k, page, Tn, start, count):
     print(f"[paged] append {cache} H={H} k={k} page={page} Tn={Tn}", flush=True)
