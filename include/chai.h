@@ -530,7 +530,7 @@ int chai_project_qk_timed(const void *x, const void *w_q, const void *w_k, const
  * Layers without clusters: k = H with rep_heads and head_to_cluster both NULL.
  * page is a multiple of 8, at least 8.  Limits (CHAI_ERR_UNSUPPORTED): d = 128,
  * B <= 4096, H + k <= 65535, T_max and Tn <= 2^24, n_pages * H * page < 2^32
- * rows, B * H * T_max and B * (H + k) * Tn < 2^35.
+ * rows, B * H * T_max and B * (H + k) * Tn < 2^34.
  *
  * chai_paged_append_kv: rows i < count[b] (count NULL: all Tn) of a block of
  *   new tokens go to positions start[b] + i: keys of the representatives,

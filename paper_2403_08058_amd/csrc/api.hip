@@ -591,7 +591,7 @@ static int check_paged_decode(const void *q, const int32_t *h2c, const int32_t *
 {
     if (!q || !lens || !out || !h2c != !rep) return CHAI_ERR_NULL;
     if (T_max < 1 || (long long)sh->max_blocks * sh->page < T_max) return CHAI_ERR_SHAPE;
-    if (T_max > kMaxPagedTokens || (long long)sh->B * sh->H * T_max >= (1ll << 35)) return CHAI_ERR_UNSUPPORTED;
+    if (T_max > kMaxPagedTokens || (long long)sh->B * sh->H * T_max >= (1ll << 34)) return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(out)) return CHAI_ERR_ALIGN;
     sh->lens = lens;
     sh->T_max = T_max;
@@ -604,7 +604,7 @@ static int check_paged_decode(const void *q, const int32_t *h2c, const int32_t *
 size_t chai_paged_workspace_bytes(int B, int H, int k, int T_max, int d)
 {
     if (B < 0 || B > kMaxPagedBatch || H < 1 || k < 1 || k > H || (long long)H + k > kMaxGridYZ || T_max < 1 || T_max > kMaxPagedTokens ||
-        d != kHeadDim || (long long)B * H * T_max >= (1ll << 35))
+        d != kHeadDim || (long long)B * H * T_max >= (1ll << 34))
         return 0;
     return B == 0 ? 256 : make_paged_plan(B, H, k, T_max).bytes;
 }
@@ -622,7 +622,7 @@ int chai_paged_append_kv(const void *k_new, const void *v_new, int64_t k_head_st
     if (st != CHAI_OK) return st;
     if (Tn < 0 || k_head_stride < (int64_t)Tn * d || v_head_stride < (int64_t)Tn * d || (k_head_stride & 7) || (v_head_stride & 7))
         return CHAI_ERR_SHAPE;
-    if (Tn > kMaxPagedTokens || (long long)B * (H + k) * Tn >= (1ll << 35)) return CHAI_ERR_UNSUPPORTED;
+    if (Tn > kMaxPagedTokens || (long long)B * (H + k) * Tn >= (1ll << 34)) return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(k_new) || !aligned16(v_new)) return CHAI_ERR_ALIGN;
     if (B == 0 || Tn == 0) return CHAI_OK;
     return hip_status(launch_paged_append(sh, pg, k_new, v_new, k_head_stride, v_head_stride, rep_heads, start, count, Tn, dtype,
@@ -641,7 +641,7 @@ int chai_paged_gather_kv(const void *k_pages, const void *v_pages, const float *
                                cache_dtype, &sh, &pg);
     if (st != CHAI_OK) return st;
     if (Tn < 0) return CHAI_ERR_SHAPE;
-    if (Tn > kMaxPagedTokens || (long long)B * (H + k) * Tn >= (1ll << 35)) return CHAI_ERR_UNSUPPORTED;
+    if (Tn > kMaxPagedTokens || (long long)B * (H + k) * Tn >= (1ll << 34)) return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(k_out) || !aligned16(v_out)) return CHAI_ERR_ALIGN;
     if (B == 0 || Tn == 0) return CHAI_OK;
     return hip_status(launch_paged_gather(sh, pg, start, count, k_out, v_out, Tn, dtype, cache_dtype, static_cast<hipStream_t>(stream)));

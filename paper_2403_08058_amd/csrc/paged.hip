@@ -16,14 +16,58 @@ namespace {
 constexpr int kWaves = kBlock / 64;
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-// `workers` waves take at least `least` units each
-struct PagedSplit {
-    unsigned int workers, least;
+// n / d without a division, for 0 <= n < 2^31: (mulhi(n, mul) + n) >> shift
+struct Quotient {
+    unsigned int mul;
+    int shift;
 };
+// 1 << shift waves take at least `least` units each of `streams` streams a row
+struct PagedSplit {
+    int shift;
+    unsigned int least;
+    Quotient by_streams;
+};
+inline unsigned int workers_of(const PagedSplit &sp) { return 1u << sp.shift; }
 
 __device__ __forceinline__ int block_of(const PagedShape &sh, int pos)
 {
     return (int)((__umulhi((unsigned int)pos, sh.div_mul) + (unsigned int)pos) >> sh.div_shift);
+}
+
+// Sums and maxima over a wave without the LDS crossbar (six steps of it are some 600 cycles in a row): DPP within sixteen lanes, then the
+// four rows of them; on two halves or rows at once a swap leaves both partners in both places.
+__device__ __forceinline__ float rows_of_lane(float x, int row) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), row * 16)); }
+
+__device__ __forceinline__ float all_max(float x)
+{
+    x = dpp_max<0xB1>(x);                    // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
+    x = dpp_max<0x4E>(x);
+    x = dpp_max<0x141>(x);
+    x = dpp_max<0x140>(x);
+    return fmaxf(fmaxf(rows_of_lane(x, 0), rows_of_lane(x, 1)), fmaxf(rows_of_lane(x, 2), rows_of_lane(x, 3)));
+}
+
+__device__ __forceinline__ float all_sum(float x)
+{
+    x = dpp_add<0xB1>(x);
+    x = dpp_add<0x4E>(x);
+    x = dpp_add<0x141>(x);
+    x = dpp_add<0x140>(x);
+    return (rows_of_lane(x, 0) + rows_of_lane(x, 1)) + (rows_of_lane(x, 2) + rows_of_lane(x, 3));
+}
+
+// sum over the lane groups of a wave, LPR lanes each, in every lane
+template <int LPR>
+__device__ __forceinline__ float sum_groups(float x)
+{
+    typedef unsigned int pair __attribute__((ext_vector_type(2)));
+    if (LPR == 8) x = dpp_add<0x128>(x);     // row_ror:8
+    if (LPR <= 16) {
+        const pair y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(y.x) + __uint_as_float(y.y);
+    }
+    const pair y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(y.x) + __uint_as_float(y.y);
 }
 
 // positions of a row that are attended to
@@ -37,14 +81,20 @@ __device__ __forceinline__ int row_len(const PagedShape &sh, int b) { return tak
 // w * quota on: every wave streams the same number of bytes whatever the lengths are, which only the device knows.  Each wave adds up
 // the rows' units for itself (64 rows per load and six steps of a scan).
 // ---------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ unsigned int wave_scan(unsigned int x, int lane)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned int add_from(unsigned int x)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned int y = (unsigned int)__shfl_up((int)x, o);
-        x += lane >= o ? y : 0u;
-    }
-    return x;
+    return x + (unsigned int)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+// sums over lanes 0 .. l
+__device__ __forceinline__ unsigned int wave_scan(unsigned int x)
+{
+    x = add_from<0x111, 0xf>(x);             // row_shr:1, :2, :4, :8
+    x = add_from<0x112, 0xf>(x);
+    x = add_from<0x114, 0xf>(x);
+    x = add_from<0x118, 0xf>(x);
+    x = add_from<0x142, 0xa>(x);             // the last lane of rows 0 and 2 to rows 1 and 3, that of the lower half to the upper one
+    return add_from<0x143, 0xc>(x);
 }
 
 template <int U>
@@ -66,7 +116,7 @@ struct Deal {
             given = b < sh.B ? given_of(sh, min(b, sh.B - 1)) : 0;
             mine += units(taken_len(sh, given));
         }
-        incl = wave_scan(mine, lane);
+        incl = wave_scan(mine);
         total = (unsigned int)__builtin_amdgcn_readlane((int)incl, 63);
     }
 
@@ -75,7 +125,7 @@ struct Deal {
     __device__ __forceinline__ unsigned int quota(int streams, const PagedSplit &sp) const
     {
         const unsigned int n = total * (unsigned int)streams;
-        return max((n + sp.workers - 1) / sp.workers, sp.least);
+        return max((n + (1u << sp.shift) - 1u) >> sp.shift, sp.least);
     }
 
     // units of one stream before row b
@@ -86,7 +136,7 @@ struct Deal {
         if (span > 1) {
             const int r = l * span + lane;
             const unsigned int u = lane < span && r < b ? units(row_len(sh, min(r, sh.B - 1))) : 0u;
-            p += (unsigned int)__builtin_amdgcn_readlane((int)wave_scan(u, lane), 63);
+            p += (unsigned int)__builtin_amdgcn_readlane((int)wave_scan(u), 63);
         }
         return p;
     }
@@ -100,7 +150,7 @@ struct Deal {
         if (span > 1) {
             const int r = b + lane;
             const unsigned int u = lane < span && r < sh.B ? units(row_len(sh, min(r, sh.B - 1))) : 0u;
-            const unsigned int in = wave_scan(u, lane);
+            const unsigned int in = wave_scan(u);
             const int i = __ffsll((long long)__ballot(p + in > y)) - 1;
             p += (unsigned int)__builtin_amdgcn_readlane((int)(in - u), i);
             b += i;
@@ -126,10 +176,10 @@ struct Walk {
     __device__ __forceinline__ bool begin(const PagedShape &sh, const Deal<U> &deal, unsigned int worker, int streams, const PagedSplit &sp, int lane)
     {
         const unsigned int quota = deal.quota(streams, sp), n = deal.total * (unsigned int)streams;
-        if (worker >= sp.workers || (unsigned long long)worker * quota >= n) return false;
+        if (worker >= (1u << sp.shift) || (unsigned long long)worker * quota >= n) return false;
         x = x0 = worker * quota;
         x1 = min(x0 + quota, n);
-        b = deal.row_at(sh, x / (unsigned int)streams, lane, &first);
+        b = deal.row_at(sh, (__umulhi(x, sp.by_streams.mul) + x) >> sp.by_streams.shift, lane, &first);
         enter(sh, deal);
         const unsigned int at = x - first * (unsigned int)streams;
         s = (int)(at / n_row);
@@ -176,11 +226,22 @@ struct Takers {
 // their place, and masked where they are used.
 // ---------------------------------------------------------------------------------------------------------
 template <int DT>
-__device__ __forceinline__ int look_up(const PagedShape &sh, const int32_t *table, unsigned int u, unsigned int ue, int len, int lane)
+__device__ __forceinline__ int table_entry(const PagedShape &sh, const int32_t *table, unsigned int u, int lane)
 {
     const int row = (int)(u * Tile<DT>::BATCH) + (lane & 7) * Tile<DT>::RPW;
-    const int at = table[min(block_of(sh, min(row, sh.T_max - 1)), sh.max_blocks - 1)];
-    return u < ue && row < len && (unsigned int)at < (unsigned int)sh.n_pages ? at : -1;
+    return table[min(block_of(sh, min(row, sh.T_max - 1)), sh.max_blocks - 1)];
+}
+// the entry if the lane's load of unit u is one of a row's (u < ue, the row is not over), -1 else
+template <int DT>
+__device__ __forceinline__ int in_row(const PagedShape &sh, int entry, unsigned int u, unsigned int ue, int len, int lane)
+{
+    const int row = (int)(u * Tile<DT>::BATCH) + (lane & 7) * Tile<DT>::RPW;
+    return u < ue && row < len && (unsigned int)entry < (unsigned int)sh.n_pages ? entry : -1;
+}
+template <int DT>
+__device__ __forceinline__ int look_up(const PagedShape &sh, const int32_t *table, unsigned int u, unsigned int ue, int len, int lane)
+{
+    return in_row<DT>(sh, table_entry<DT>(sh, table, u, lane), u, ue, len, lane);
 }
 
 // the first row of the lane's load among the pool's rows (0 where there is none)
@@ -362,26 +423,28 @@ constexpr float kPagedLarge = 0x1p120f;
 // to `recs` of the wave, two of each (its first units, its last ones), and paged_join_kernel puts them together.
 // ---------------------------------------------------------------------------------------------------------
 // One wave's share of a stream: units ua, ua + step, .. below ue of head h of row b, as weighted mean acc (all lane groups have it), the
-// reference m and the sum of exponentials l.  The key of the token being decoded goes to slot c if it is the head's own (IDENT).
+// reference m and the sum of exponentials l.  entry0, entry1: table entries of the first two units.  The key of the token being decoded
+// goes to slot c if it is the head's own (IDENT).
 template <int DT, bool IDENT, bool APPEND>
 __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPages &pg, const char *__restrict__ q, int q_dtype, const int32_t *__restrict__ table,
-                                             float scale, const char *__restrict__ k_new, const char *__restrict__ v_new, int b, int h, int c, int r, int len, int fresh,
-                                             unsigned int ua, unsigned int ue, unsigned int step, float *strip, int lane, float (&acc)[Tile<DT>::EPL], float &m, float &l)
+                                             float scale, const char *__restrict__ k_new, const char *__restrict__ v_new, int b, int h, int c, const int32_t *__restrict__ rep, int len,
+                                             int fresh, int entry0, int entry1, unsigned int ua, unsigned int ue, unsigned int step, float *strip, int lane, float (&acc)[Tile<DT>::EPL], float &m, float &l)
 {
     using TL = Tile<DT>;
     constexpr int U = TL::BATCH;
     const int cg = lane % TL::LPR, rg = lane / TL::LPR;
     const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
+    const int r = IDENT ? h : min(max(rep[(size_t)b * sh.k + c], 0), sh.H - 1);
     float qf[TL::EPL], l_run, down = 1.f;
-    load_query<DT>(q, (size_t)b * sh.H + r, cg, q_dtype, qf);
     for (;;) {
         unsigned int u0 = ua;
         asm volatile("" : "+s"(u0));         // (what the first unit asks for is not kept for the second time around)
         u32x4 kb[kUnroll], vb[kUnroll];
         float ks = 1.f, vs = 1.f;
-        int at = look_up<DT>(sh, table, u0, ue, len, lane), at1 = look_up<DT>(sh, table, u0 + step, ue, len, lane);
+        int at = in_row<DT>(sh, entry0, u0, ue, len, lane), at1 = in_row<DT>(sh, entry1, u0 + step, ue, len, lane);
         unsigned int krow = pool_row<DT>(sh, at, u0, sh.k, c, lane), vrow = pool_row<DT>(sh, at, u0, sh.H, h, lane);
         request<DT, IDENT>(kb, pg.k, krow, lane_off);
+        load_query<DT>(q, (size_t)b * sh.H + r, cg, q_dtype, qf);
         if (DT == DT_E4M3) ks = pg.k_scales[krow + (at < 0 ? 0 : rg)];
         request<DT>(vb, pg.v, vrow, lane_off);
         if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at < 0 ? 0 : rg)];
@@ -401,7 +464,7 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
             request<DT, IDENT>(kb, pg.k, krow, lane_off);
             if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
             if (__any(sv > m)) {
-                const float m_new = fmaxf(m, wave_max(sv));
+                const float m_new = fmaxf(m, all_max(sv));
                 const float f = __expf(m - m_new);
 #pragma unroll
                 for (int e = 0; e < TL::EPL; ++e) acc[e] *= f;
@@ -422,14 +485,13 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
         bool large = false;
 #pragma unroll
         for (int e = 0; e < TL::EPL; ++e) {
-#pragma unroll
-            for (int o = TL::LPR; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
+            acc[e] = sum_groups<TL::LPR>(acc[e]);
             large = large || !(fabsf(acc[e]) <= kPagedLarge);
         }
         if (!__any(large) || down != 1.f) break;
         down = kPagedDown;
     }
-    l = wave_sum(l_run);
+    l = all_sum(l_run);
 #pragma unroll
     for (int e = 0; e < TL::EPL; ++e) acc[e] = l == 0.f ? 0.f : acc[e] / l;
     l /= down;
@@ -449,8 +511,9 @@ __global__ __launch_bounds__(kBlock, 3) void paged_attend_kernel(
     if (!wk.begin(sh, deal, worker, sh.H, sp, lane)) return;
     do {
         float acc[TL::EPL], m, l;
-        attend_units<DT, true, APPEND>(sh, pg, q, q_dtype, sh.table + (size_t)wk.b * sh.max_blocks, scale, k_new, v_new, wk.b, wk.s, wk.s, wk.s, wk.len, wk.fresh,
-                                       wk.ua, wk.ue, 1u, strip[w], lane, acc, m, l);
+        const int32_t *table = sh.table + (size_t)wk.b * sh.max_blocks;
+        attend_units<DT, true, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, wk.b, wk.s, wk.s, nullptr, wk.len, wk.fresh,
+                                       table_entry<DT>(sh, table, wk.ua, lane), table_entry<DT>(sh, table, wk.ua + 1, lane), wk.ua, wk.ue, 1u, strip[w], lane, acc, m, l);
         const size_t slot = wk.slot(worker);
         float *o = wk.whole() ? out + ((size_t)wk.b * sh.H + wk.s) * kHeadDim : partial + slot * kHeadDim;
         if (lane < TL::LPR) store_floats(o + lane * TL::EPL, acc);
@@ -473,14 +536,15 @@ __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = blockIdx.x, b = blockIdx.y;
     const int cg = lane % TL::LPR, rg = lane / TL::LPR;
+    const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
+    const int entry0 = table_entry<DT>(sh, table, (unsigned int)w, lane), entry1 = table_entry<DT>(sh, table, (unsigned int)(w + kRowWaves), lane);
     const int c = IDENT ? h : min(max(h2c[(size_t)b * sh.H + h], 0), sh.k - 1);
     const int given = sh.lens[b], len = taken_len(sh, given), fresh = given <= sh.T_max ? len - 1 : -1;
-    const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
-    const int r = IDENT ? h : min(max(rep[(size_t)b * sh.k + c], 0), sh.H - 1);
     const unsigned int n = (unsigned int)(len + U - 1) / U;
     float acc[TL::EPL], m = -INFINITY, l = 0.f;
     if ((unsigned int)w < n) {
-        attend_units<DT, IDENT, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, b, h, c, r, len, fresh, (unsigned int)w, n, (unsigned int)kRowWaves, strip[w], lane,
+        attend_units<DT, IDENT, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, b, h, c, rep, len, fresh, entry0, entry1, (unsigned int)w, n, (unsigned int)kRowWaves,
+                                        strip[w], lane,
                                         acc, m, l);
         if (rg == 0) store_floats(&acc_lds[w][cg * TL::EPL], acc);
     }
@@ -571,8 +635,8 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? (APPEND ? 4 : 5) : 6) void 
             at = at1;
             at1 = at2;
         }
-        const float M = wave_max(m_run);
-        const float L = wave_sum(m_run == -INFINITY ? l_run : l_run * __expf(m_run - M));     // (lanes that saw only NaN hold it in l_run)
+        const float M = all_max(m_run);
+        const float L = all_sum(m_run == -INFINITY ? l_run : l_run * __expf(m_run - M));     // (lanes that saw only NaN hold it in l_run)
         if (lane == 0) (wk.whole() ? whole[(size_t)b * sh.k + j] : parts[wk.slot(worker)]) = make_float2(M, L);
     } while (wk.next(sh, deal, sh.k));
 }
@@ -582,13 +646,13 @@ __device__ __forceinline__ float2 merge(const float2 *parts, const Takers &tk, i
 {
     float m = -INFINITY;
     for (unsigned int i = lane; i < tk.n; i += 64) m = fmaxf(m, parts[tk.slot(i)].x);
-    const float M = wave_max(m);
+    const float M = all_max(m);
     float l = 0.f;
     for (unsigned int i = lane; i < tk.n; i += 64) {
         const float2 rc = parts[tk.slot(i)];
         l += rc.x == -INFINITY ? rc.y : rc.y * __expf(rc.x - M);         // (only -inf scores: 0, NaN among them: NaN)
     }
-    return make_float2(M, wave_sum(l));
+    return make_float2(M, all_sum(l));
 }
 
 // Values: a wave streams the values of its units, each weighed by its cluster's probability exp(s - M) / L.
@@ -643,10 +707,7 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 4 : 5) void paged_values_ke
             at1 = at2;
         }
 #pragma unroll
-        for (int e = 0; e < TL::EPL; ++e) {
-#pragma unroll
-            for (int o = TL::LPR; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
-        }
+        for (int e = 0; e < TL::EPL; ++e) acc[e] = sum_groups<TL::LPR>(acc[e]);
         float *o = wk.whole() ? out + ((size_t)b * sh.H + h) * kHeadDim : partial + wk.slot(worker) * kHeadDim;
         if (rg == 0) store_floats(o + cg * TL::EPL, acc);
     } while (wk.next(sh, deal, sh.H));
@@ -1101,14 +1162,27 @@ PagedPlan make_paged_plan(int B, int H, int k, int T_max)
     return pl;
 }
 
+// floor(n / d) = (mulhi(n, mul) + n) >> shift for every 0 <= n < 2^31
+static Quotient quotient_by(int d)
+{
+    Quotient q = {0u, 0};
+    while ((1ll << q.shift) < d) ++q.shift;
+    q.mul = (unsigned int)((((1ull << q.shift) - (unsigned long long)d) << 32) / (unsigned long long)d + 1ull);
+    return q;
+}
+
+static PagedSplit make_split(long long units, int streams, unsigned int most, unsigned int least)
+{
+    PagedSplit sp = {0, least, quotient_by(streams)};
+    while ((1ll << sp.shift) < units && (1u << sp.shift) < most) ++sp.shift;
+    return sp;
+}
+
 static PagedSplit make_paged_split(int B, int streams, int T_max, int cache_dtype, unsigned int workers, unsigned int parts)
 {
-    PagedSplit sp;
     const int u = unit_rows(cache_dtype);
-    const long long row_units = ((long long)T_max + u - 1) / u, units = row_units * B * streams;
-    sp.workers = (unsigned int)(units < (long long)workers ? units : workers);
-    sp.least = (unsigned int)((row_units + parts - 1) / parts);
-    return sp;
+    const long long row_units = ((long long)T_max + u - 1) / u;
+    return make_split(row_units * B * streams, streams, workers, (unsigned int)((row_units + parts - 1) / parts));
 }
 
 // Whether rows are moved by workgroups, a block of tokens each up to the longest row's, or by waves that are dealt units of what there is.
@@ -1122,20 +1196,14 @@ static bool stream_moves(const PagedShape &sh, int Tn) { return Tn >= 32 && (lon
 static PagedSplit make_move_split(int B, int streams, int Tn, int dtype)
 {
     const int u = 4 * (dtype == CHAI_BF16 ? kMoveUnroll<true> : kMoveUnroll<false>);
-    const long long units = ((long long)Tn + u - 1) / u * B * streams;
-    PagedSplit sp;
-    sp.workers = (unsigned int)(units < (long long)kMoveWorkers ? units : kMoveWorkers);
-    sp.least = 1u;
-    return sp;
+    return make_split(((long long)Tn + u - 1) / u * B * streams, streams, kMoveWorkers, 1u);
 }
 
 void set_page_division(PagedShape *sh)
 {
-    // floor(n / page) = (mulhi(n, mul) + n) >> shift for every 0 <= n < 2^31
-    int s = 0;
-    while ((1ll << s) < sh->page) ++s;
-    sh->div_shift = s;
-    sh->div_mul = (unsigned int)((((1ull << s) - (unsigned long long)sh->page) << 32) / (unsigned long long)sh->page + 1ull);
+    const Quotient q = quotient_by(sh->page);
+    sh->div_mul = q.mul;
+    sh->div_shift = q.shift;
 }
 
 template <int DT, bool APPEND>
@@ -1146,7 +1214,7 @@ static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, con
     float2 *recs = reinterpret_cast<float2 *>(ws + plan.off_recs), *whole = reinterpret_cast<float2 *>(ws + plan.off_whole);
     float *partial = reinterpret_cast<float *>(ws + plan.off_partial), *scores = reinterpret_cast<float *>(ws + plan.off_scores);
     const dim3 block(kBlock);
-    auto waves = [](const PagedSplit &sp) { return dim3((sp.workers + kWaves - 1) / kWaves); };
+    auto waves = [](const PagedSplit &sp) { return dim3((workers_of(sp) + kWaves - 1) / kWaves); };
     const KernelEvents none;
     auto join = [&](auto *one, auto *four, const PagedSplit &sp) {
         const bool many = (long long)sh.B * sh.H > kJoinedByOne;
@@ -1199,7 +1267,7 @@ int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *
         each.T_max = Tn;
         const PagedSplit sp = make_move_split(sh.B, sh.k + sh.H, Tn, dtype);
         auto stream_rows = [&](auto *kernel) {
-            return (int)launch_kernel(kernel, dim3((sp.workers + kWaves - 1) / kWaves), dim3(kBlock), 0, stream, KernelEvents(), each, pg, sp,
+            return (int)launch_kernel(kernel, dim3((workers_of(sp) + kWaves - 1) / kWaves), dim3(kBlock), 0, stream, KernelEvents(), each, pg, sp,
                                       static_cast<const char *>(k_new), static_cast<const char *>(v_new), k_stride, v_stride, rep, start);
         };
         if (cache_dtype == CHAI_E4M3) return dtype == CHAI_BF16 ? stream_rows(paged_append_stream_kernel<DT_E4M3, true>) : stream_rows(paged_append_stream_kernel<DT_E4M3, false>);
@@ -1224,7 +1292,7 @@ int launch_paged_gather(const PagedShape &sh, const PagedPages &pg, const int32_
         each.T_max = Tn;
         const PagedSplit sp = make_move_split(sh.B, sh.k + sh.H, Tn, dtype);
         auto stream_rows = [&](auto *kernel) {
-            return (int)launch_kernel(kernel, dim3((sp.workers + kWaves - 1) / kWaves), dim3(kBlock), 0, stream, KernelEvents(), each, pg, sp, start,
+            return (int)launch_kernel(kernel, dim3((workers_of(sp) + kWaves - 1) / kWaves), dim3(kBlock), 0, stream, KernelEvents(), each, pg, sp, start,
                                       static_cast<char *>(k_out), static_cast<char *>(v_out));
         };
         if (cache_dtype == CHAI_E4M3) return dtype == CHAI_BF16 ? stream_rows(paged_gather_stream_kernel<DT_E4M3, true>) : stream_rows(paged_gather_stream_kernel<DT_E4M3, false>);
