@@ -444,6 +444,53 @@ def test_step(cache, H, k, page, lengths):
     assert ok, worst
 
 
+# sizes at which rows are shared between waves: up to 512 rows of heads and more, with and without clusters
+SHARED = [
+    (6, 6, 40, [2999, 1, 0, 700, 2048]),
+    (32, 32, 16, [4150] + [17 * i for i in range(20)]),
+    (32, 8, 16, [4150] + [17 * i for i in range(20)]),
+]
+
+
+@pytest.mark.parametrize("cache", CACHES)
+@pytest.mark.parametrize("H,k,page,lengths", SHARED)
+def test_step_of_shared_rows(cache, H, k, page, lengths):
+    """The same of long rows: written as by the append, attended to as stored, without the new rows the same again."""
+    print(f"[paged] shared rows {cache} H={H} k={k} page={page}", flush=True)
+    s = Setting(9960 + H + k, cache, H, k, page, lengths)
+    s.host_table[0, 2] = -1
+    s.table.copy_(torch.from_numpy(s.host_table))
+    q, k_new, v_new = s.normal(s.B, H, D), s.normal(s.B, H, D), s.normal(s.B, H, D)
+    expect = copies(s)
+    put(s, expect, k_new.unsqueeze(2), v_new.unsqueeze(2), s.host_lengths - 1, (s.host_lengths > 0).astype(int))
+    T_max = s.blocks * page
+    whole, out = guarded((s.B, H, D), torch.float32, float("nan"))
+    ws = C.alloc_paged_workspace(s.B, H, k, T_max)
+    ws.fill_(0xFF)
+    C.chai_paged_decode_step(q, k_new, v_new, s.k_pages, s.v_pages, s.h2c, s.rep, s.table, s.lengths, T_max, SCALE, out, ws, **s.scales)
+    torch.cuda.synchronize()
+    assert guards_intact(whole, out.shape, float("nan"))
+    same_pools(s, expect)
+    ok, worst = rows_close(out.cpu().numpy(), s.expected(q, T_max).cpu().numpy(), BAR[cache])
+    assert ok, worst
+    s.check(q)
+
+
+def test_slots_without_a_cluster():
+    """Fewer clusters than slots: what the others' keys hold reaches nobody, short rows and long ones."""
+    for T in (100, 3000):
+        s = Setting(9965, "bf16", 8, 3, 16, [T, T // 2])
+        s.h2c.clamp_(max=1)
+        s.rep[:, 2] = -1
+        s.k_pages[:, 2] = float("nan")
+        q = s.normal(2, 8, D)
+        out = s.attend(q, s.blocks * 16)
+        s.k_pages[:, 2] = 0.0
+        s.rep[:, 2] = 0
+        ok, worst = rows_close(out.cpu().numpy(), s.expected(q, s.blocks * 16).cpu().numpy(), BAR["bf16"])
+        assert ok, (T, worst)
+
+
 def test_step_beyond_the_bound_writes_nothing():
     s = Setting(9950, "bf16", 4, 2, 16, [200, 90])
     q, k_new, v_new = s.normal(2, 4, D), s.normal(2, 4, D), s.normal(2, 4, D)
