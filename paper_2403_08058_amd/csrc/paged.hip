@@ -427,14 +427,13 @@ constexpr float kPagedLarge = 0x1p120f;
 // goes to slot c if it is the head's own (IDENT).
 template <int DT, bool IDENT, bool APPEND>
 __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPages &pg, const char *__restrict__ q, int q_dtype, const int32_t *__restrict__ table,
-                                             float scale, const char *__restrict__ k_new, const char *__restrict__ v_new, int b, int h, int c, const int32_t *__restrict__ rep, int len,
+                                             float scale, const char *__restrict__ k_new, const char *__restrict__ v_new, int b, int h, int c, int r, int len,
                                              int fresh, int entry0, int entry1, unsigned int ua, unsigned int ue, unsigned int step, float *strip, int lane, float (&acc)[Tile<DT>::EPL], float &m, float &l)
 {
     using TL = Tile<DT>;
     constexpr int U = TL::BATCH;
     const int cg = lane % TL::LPR, rg = lane / TL::LPR;
     const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
-    const int r = IDENT ? h : min(max(rep[(size_t)b * sh.k + c], 0), sh.H - 1);
     float qf[TL::EPL], l_run, down = 1.f;
     for (;;) {
         unsigned int u0 = ua;
@@ -512,7 +511,7 @@ __global__ __launch_bounds__(kBlock, 3) void paged_attend_kernel(
     do {
         float acc[TL::EPL], m, l;
         const int32_t *table = sh.table + (size_t)wk.b * sh.max_blocks;
-        attend_units<DT, true, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, wk.b, wk.s, wk.s, nullptr, wk.len, wk.fresh,
+        attend_units<DT, true, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, wk.b, wk.s, wk.s, wk.s, wk.len, wk.fresh,
                                        table_entry<DT>(sh, table, wk.ua, lane), table_entry<DT>(sh, table, wk.ua + 1, lane), wk.ua, wk.ue, 1u, strip[w], lane, acc, m, l);
         const size_t slot = wk.slot(worker);
         float *o = wk.whole() ? out + ((size_t)wk.b * sh.H + wk.s) * kHeadDim : partial + slot * kHeadDim;
@@ -521,11 +520,33 @@ __global__ __launch_bounds__(kBlock, 3) void paged_attend_kernel(
     } while (wk.next(sh, deal, sh.H));
 }
 
+// The head that workgroup i of a row takes.  Workgroups go round the eight XCDs: the heads, in order of their clusters, are dealt out in
+// eight stretches, so that most members of a cluster share the L2 that its keys come through.  (One cluster's heads at a time are counted,
+// the scan ends at its own.)
+__device__ __forceinline__ int head_by_cluster(const int32_t *__restrict__ h2c, int H, int k, int i, int lane)
+{
+    const int r = i & 7;
+    int p = r * (H >> 3) + min(r, H & 7) + (i >> 3);
+    const int c0 = lane < H ? min(max(h2c[min(lane, H - 1)], 0), k - 1) : -1, c1 = lane + 64 < H ? min(max(h2c[min(lane + 64, H - 1)], 0), k - 1) : -1;
+    for (int j = 0; j < k; ++j) {
+        const unsigned long long m0 = __ballot(c0 == j), m1 = __ballot(c1 == j);
+        const int n0 = __popcll(m0), n = n0 + __popcll(m1);
+        if (p < n) {
+            const bool upper = p >= n0;
+            const unsigned long long m = upper ? m1 : m0;
+            const int before = __builtin_amdgcn_mbcnt_hi((unsigned int)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned int)m, 0u));
+            return __ffsll((long long)(__ballot(before == (upper ? p - n0 : p)) & m)) - 1 + (upper ? 64 : 0);
+        }
+        p -= n;
+    }
+    return i;                                // (every head is in a cluster: not reached)
+}
+
 // Short rows: a workgroup of kRowWaves waves per (head, row), no parts and one launch.  The members of a cluster then each read its keys
 // (out of L2), and head h writes the new token's key to every slot that it represents.
 template <int DT, bool IDENT, bool APPEND, int kRowWaves>
 __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_rows_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ q, int q_dtype,
-                                                                    const int32_t *__restrict__ h2c, const int32_t *__restrict__ rep, float scale,
+                                                                    const int32_t *__restrict__ h2c, const int32_t *__restrict__ rep, int by_cluster, float scale,
                                                                     const char *__restrict__ k_new, const char *__restrict__ v_new, float *__restrict__ out)
 {
     using TL = Tile<DT>;
@@ -534,16 +555,19 @@ __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_
     __shared__ float acc_lds[kRowWaves][kHeadDim];
     __shared__ float2 rec_lds[kRowWaves];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = blockIdx.x, b = blockIdx.y;
+    const int b = blockIdx.y;
+    const int reps = IDENT ? 0 : rep[(size_t)b * sh.k + min(lane, sh.k - 1)];        // (asked for before the cluster is known)
+    const int h = IDENT || !by_cluster ? (int)blockIdx.x : head_by_cluster(h2c + (size_t)b * sh.H, sh.H, sh.k, (int)blockIdx.x, lane);
     const int cg = lane % TL::LPR, rg = lane / TL::LPR;
     const int32_t *table = sh.table + (size_t)b * sh.max_blocks;
     const int entry0 = table_entry<DT>(sh, table, (unsigned int)w, lane), entry1 = table_entry<DT>(sh, table, (unsigned int)(w + kRowWaves), lane);
     const int c = IDENT ? h : min(max(h2c[(size_t)b * sh.H + h], 0), sh.k - 1);
+    const int r = IDENT ? h : min(max(sh.k <= 64 ? __builtin_amdgcn_readlane(reps, c) : rep[(size_t)b * sh.k + c], 0), sh.H - 1);
     const int given = sh.lens[b], len = taken_len(sh, given), fresh = given <= sh.T_max ? len - 1 : -1;
     const unsigned int n = (unsigned int)(len + U - 1) / U;
     float acc[TL::EPL], m = -INFINITY, l = 0.f;
     if ((unsigned int)w < n) {
-        attend_units<DT, IDENT, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, b, h, c, rep, len, fresh, entry0, entry1, (unsigned int)w, n, (unsigned int)kRowWaves,
+        attend_units<DT, IDENT, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, b, h, c, r, len, fresh, entry0, entry1, (unsigned int)w, n, (unsigned int)kRowWaves,
                                         strip[w], lane,
                                         acc, m, l);
         if (rg == 0) store_floats(&acc_lds[w][cg * TL::EPL], acc);
@@ -1138,10 +1162,12 @@ constexpr long long kJoinedByOne = 512;
 static bool take_rows(int B, int H, int T_max, int cache, bool dense)
 {
     const long long heads = (long long)B * H, bytes = (long long)T_max * kHeadDim * (cache == CHAI_F32 ? 4 : (cache == CHAI_BF16 ? 2 : 1));
-    return bytes <= (dense ? (heads >= 768 ? 512 : 256) : (heads <= 512 ? 256 : 160)) * 1024ll;
+    return bytes <= (dense ? (heads >= 768 ? 512 : 256) : (heads <= 512 ? 512 : heads <= 1024 ? 256 : 160)) * 1024ll;
 }
 // Eight waves per row where a CU has one row at most, else four (1 x 32 of 577 bf16 tokens 8.5 against 10.3 us; 16 x 32 of 256 16.8 against 15.5).
 constexpr long long kFewHeads = 128;
+
+constexpr int kOrderedHeads = 128;
 
 static int padded_tokens(int T_max) { return (T_max + 63) / 64 * 64; }
 
@@ -1223,8 +1249,9 @@ static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, con
     };
     if (take_rows(sh.B, sh.H, sh.T_max, DT, h2c == nullptr)) {
         const bool few = (long long)sh.B * sh.H <= kFewHeads;
+        const int by_cluster = !few && sh.H <= kOrderedHeads && 2 * sh.k <= sh.H ? 1 : 0;
         auto rows = [&](auto *kernel) {
-            return (int)launch_kernel(kernel, dim3((unsigned int)sh.H, (unsigned int)sh.B), dim3(few ? 512 : 256), 0, stream, none, sh, pg, q, dtype, h2c, rep, scale,
+            return (int)launch_kernel(kernel, dim3((unsigned int)sh.H, (unsigned int)sh.B), dim3(few ? 512 : 256), 0, stream, none, sh, pg, q, dtype, h2c, rep, by_cluster, scale,
                                       k_new, v_new, out);
         };
         if (h2c == nullptr) return few ? rows(paged_rows_kernel<DT, true, APPEND, 8>) : rows(paged_rows_kernel<DT, true, APPEND, 4>);
