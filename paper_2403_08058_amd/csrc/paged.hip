@@ -266,20 +266,41 @@ __device__ __forceinline__ void request(u32x4 (&buf)[kUnroll], const char *rows,
     asm volatile("" ::: "memory");           // asked for here and not where they are used, one unit later
 }
 
+// The query as a lane multiplies it: fp32, beside codes (QB) bf16 pairs.  A code is exact in bf16, and two products of such pairs are added
+// to an fp32 sum in one instruction: 16 instructions for sixteen codes where widening to fp32 takes 24, and half the registers.
+template <int DT, bool QB>
+struct Query {
+    float f[Tile<DT>::EPL];
+};
+template <>
+struct Query<DT_E4M3, true> {
+    u32x4 pairs[2];
+};
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 // scores of a unit: lane cg < 8 of a lane group gets that of load cg, row rg + cg * RPW of the unit
-template <int DT>
-__device__ __forceinline__ float dots(const u32x4 (&kb)[kUnroll], const float (&qf)[Tile<DT>::EPL], int cg)
+template <int DT, bool QB>
+__device__ __forceinline__ float dots(const u32x4 (&kb)[kUnroll], const Query<DT, QB> &q, int cg)
 {
     float mine = 0.f;
 #pragma unroll
     for (int i = 0; i < kUnroll; ++i) {
         u32x4 raw = kb[i];
         if (DT == DT_E4M3) asm("" : "+v"(raw), "+v"(mine));      // one row is widened at a time (all at once they take 130 registers)
-        float f[Tile<DT>::EPL];
-        unpack(raw, f);
         float dot = 0.f;
+        if constexpr (QB) {
 #pragma unroll
-        for (int e = 0; e < Tile<DT>::EPL; ++e) dot = fmaf(qf[e], f[e], dot);
+            for (int e = 0; e < 8; ++e) {
+                const unsigned int w = raw[e / 2];
+                const bf16x2 codes = e % 2 == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+                dot = __builtin_amdgcn_fdot2_f32_bf16(codes, __builtin_bit_cast(bf16x2, (unsigned int)q.pairs[e / 4][e % 4]), dot, false);
+            }
+        } else {
+            float f[Tile<DT>::EPL];
+            unpack(raw, f);
+#pragma unroll
+            for (int e = 0; e < Tile<DT>::EPL; ++e) dot = fmaf(q.f[e], f[e], dot);
+        }
         dot = row_sum<DT>(dot);
         mine = cg == i ? dot : mine;
     }
@@ -338,6 +359,18 @@ __device__ __forceinline__ void load_query(const char *q, size_t row, int cg, in
         }
     } else {
         unpack(*reinterpret_cast<const u32x4 *>(q + row * Tile<DT>::ROW_BYTES + cg * 16), qf);
+    }
+}
+
+template <int DT, bool QB>
+__device__ __forceinline__ void load_query(const char *q, size_t row, int cg, Query<DT, QB> &x)
+{
+    if constexpr (QB) {
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(q + row * (size_t)(kHeadDim * 2) + cg * 32);
+        x.pairs[0] = p[0];
+        x.pairs[1] = p[1];
+    } else {
+        load_query<DT>(q, row, cg, CHAI_F32, x.f);           // (q has the type of the rows, or is fp32 beside codes)
     }
 }
 
@@ -425,8 +458,8 @@ constexpr float kPagedLarge = 0x1p120f;
 // One wave's share of a stream: units ua, ua + step, .. below ue of head h of row b, as weighted mean acc (all lane groups have it), the
 // reference m and the sum of exponentials l.  entry0, entry1: table entries of the first two units.  The key of the token being decoded
 // goes to slot c if it is the head's own (IDENT).
-template <int DT, bool IDENT, bool APPEND>
-__device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPages &pg, const char *__restrict__ q, int q_dtype, const int32_t *__restrict__ table,
+template <int DT, bool QB, bool IDENT, bool APPEND>
+__device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPages &pg, const char *__restrict__ q, const int32_t *__restrict__ table,
                                              float scale, const char *__restrict__ k_new, const char *__restrict__ v_new, int b, int h, int c, int r, int len,
                                              int fresh, int entry0, int entry1, unsigned int ua, unsigned int ue, unsigned int step, float *strip, int lane, float (&acc)[Tile<DT>::EPL], float &m, float &l)
 {
@@ -434,7 +467,9 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
     constexpr int U = TL::BATCH;
     const int cg = lane % TL::LPR, rg = lane / TL::LPR;
     const unsigned int lane_off = rg * TL::ROW_BYTES + cg * 16;
-    float qf[TL::EPL], l_run, down = 1.f;
+    constexpr int q_dtype = DT == DT_BF16 || QB ? CHAI_BF16 : CHAI_F32;
+    Query<DT, QB> qf;
+    float l_run, down = 1.f;
     for (;;) {
         unsigned int u0 = ua;
         asm volatile("" : "+s"(u0));         // (what the first unit asks for is not kept for the second time around)
@@ -443,7 +478,7 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
         int at = in_row<DT>(sh, entry0, u0, ue, len, lane), at1 = in_row<DT>(sh, entry1, u0 + step, ue, len, lane);
         unsigned int krow = pool_row<DT>(sh, at, u0, sh.k, c, lane), vrow = pool_row<DT>(sh, at, u0, sh.H, h, lane);
         request<DT, IDENT>(kb, pg.k, krow, lane_off);
-        load_query<DT>(q, (size_t)b * sh.H + r, cg, q_dtype, qf);
+        load_query<DT, QB>(q, (size_t)b * sh.H + r, cg, qf);
         if (DT == DT_E4M3) ks = pg.k_scales[krow + (at < 0 ? 0 : rg)];
         request<DT>(vb, pg.v, vrow, lane_off);
         if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at < 0 ? 0 : rg)];
@@ -456,7 +491,7 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
             const int at2 = look_up<DT>(sh, table, u + 2 * step, ue, len, lane);
             const bool has_fresh = APPEND && fresh >= (int)(u * U) && fresh < (int)((u + 1) * U);
             if (has_fresh) take_fresh<DT>(FreshRow<DT>(k_new, (size_t)b * sh.H + r, cg, q_dtype), kb, ks, pg.k, pg.k_scales, at, krow, fresh - (int)(u * U), IDENT, cg, rg);
-            const float mine = dots<DT>(kb, qf, cg);
+            const float mine = dots<DT, QB>(kb, qf, cg);
             const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
             const float sv = there ? scaled<DT>(mine, scale, ks) : -INFINITY;
             krow = pool_row<DT>(sh, at1, u + step, sh.k, c, lane);
@@ -496,9 +531,9 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
     l /= down;
 }
 
-template <int DT, bool APPEND>
+template <int DT, bool QB, bool APPEND>
 __global__ __launch_bounds__(kBlock, 3) void paged_attend_kernel(
-    PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q, int q_dtype, float scale, const char *__restrict__ k_new,
+    PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q, float scale, const char *__restrict__ k_new,
     const char *__restrict__ v_new, float *__restrict__ partial, float2 *__restrict__ recs, float *__restrict__ out)
 {
     using TL = Tile<DT>;
@@ -511,7 +546,7 @@ __global__ __launch_bounds__(kBlock, 3) void paged_attend_kernel(
     do {
         float acc[TL::EPL], m, l;
         const int32_t *table = sh.table + (size_t)wk.b * sh.max_blocks;
-        attend_units<DT, true, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, wk.b, wk.s, wk.s, wk.s, wk.len, wk.fresh,
+        attend_units<DT, QB, true, APPEND>(sh, pg, q, table, scale, k_new, v_new, wk.b, wk.s, wk.s, wk.s, wk.len, wk.fresh,
                                        table_entry<DT>(sh, table, wk.ua, lane), table_entry<DT>(sh, table, wk.ua + 1, lane), wk.ua, wk.ue, 1u, strip[w], lane, acc, m, l);
         const size_t slot = wk.slot(worker);
         float *o = wk.whole() ? out + ((size_t)wk.b * sh.H + wk.s) * kHeadDim : partial + slot * kHeadDim;
@@ -544,8 +579,8 @@ __device__ __forceinline__ int head_by_cluster(const int32_t *__restrict__ h2c, 
 
 // Short rows: a workgroup of kRowWaves waves per (head, row), no parts and one launch.  The members of a cluster then each read its keys
 // (out of L2), and head h writes the new token's key to every slot that it represents.
-template <int DT, bool IDENT, bool APPEND, int kRowWaves>
-__global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_rows_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ q, int q_dtype,
+template <int DT, bool QB, bool IDENT, bool APPEND, int kRowWaves>
+__global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_rows_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ q,
                                                                     const int32_t *__restrict__ h2c, const int32_t *__restrict__ rep, int by_cluster, float scale,
                                                                     const char *__restrict__ k_new, const char *__restrict__ v_new, float *__restrict__ out)
 {
@@ -567,7 +602,7 @@ __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_
     const unsigned int n = (unsigned int)(len + U - 1) / U;
     float acc[TL::EPL], m = -INFINITY, l = 0.f;
     if ((unsigned int)w < n) {
-        attend_units<DT, IDENT, APPEND>(sh, pg, q, q_dtype, table, scale, k_new, v_new, b, h, c, r, len, fresh, entry0, entry1, (unsigned int)w, n, (unsigned int)kRowWaves,
+        attend_units<DT, QB, IDENT, APPEND>(sh, pg, q, table, scale, k_new, v_new, b, h, c, r, len, fresh, entry0, entry1, (unsigned int)w, n, (unsigned int)kRowWaves,
                                         strip[w], lane,
                                         acc, m, l);
         if (rg == 0) store_floats(&acc_lds[w][cg * TL::EPL], acc);
@@ -580,7 +615,7 @@ __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_
             const int rj = j0 + lane < sh.k ? rep[(size_t)b * sh.k + j0 + lane] : -1;
             unsigned long long left = __ballot(rj >= 0 && min(rj, sh.H - 1) == h);
             if (left == 0ull || (unsigned int)at >= (unsigned int)sh.n_pages) continue;
-            const FreshRow<DT> row(k_new, (size_t)b * sh.H + h, cg, q_dtype);
+            const FreshRow<DT> row(k_new, (size_t)b * sh.H + h, cg, DT == DT_BF16 || QB ? CHAI_BF16 : CHAI_F32);
             for (; left != 0ull; left &= left - 1ull) {
                 const int j = j0 + __ffsll((long long)left) - 1;
                 if (rg == 0) row.store(pg.k, pg.k_scales, (unsigned int)(at * sh.k + j) * (unsigned int)sh.page + (unsigned int)(fresh - block * sh.page), cg);
@@ -611,14 +646,14 @@ __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_
 // Scores: a wave streams keys of its units, writes s[b][j][t] (-inf where nothing is to be attended to, whole units) and the maximum
 // and sum of exponentials of every stretch: `whole` of a stream that it took alone, else `parts` of the wave.
 // ---------------------------------------------------------------------------------------------------------
-template <int DT, bool APPEND>
+template <int DT, bool QB, bool APPEND>
 __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? (APPEND ? 4 : 5) : 6) void paged_scores_kernel(PagedShape sh, PagedPages pg, PagedSplit sp, const char *__restrict__ q,
-                                                                 int q_dtype, const int32_t *__restrict__ rep, float scale, int T_pad,
+                                                                 const int32_t *__restrict__ rep, float scale, int T_pad,
                                                                  const char *__restrict__ k_new, float *__restrict__ scores,
                                                                  float2 *__restrict__ whole, float2 *__restrict__ parts)
 {
     using TL = Tile<DT>;
-    constexpr int U = TL::BATCH;
+    constexpr int U = TL::BATCH, q_dtype = DT == DT_BF16 || QB ? CHAI_BF16 : CHAI_F32;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned int worker = blockIdx.x * kWaves + w;
     const int cg = lane % TL::LPR, rg = lane / TL::LPR;
@@ -637,15 +672,15 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? (APPEND ? 4 : 5) : 6) void 
         unsigned int krow = pool_row<DT>(sh, at, wk.ua, sh.k, j, lane);
         request<DT>(kb, pg.k, krow, lane_off);
         if (DT == DT_E4M3) ks = pg.k_scales[krow + (at < 0 ? 0 : rg)];
-        float qf[TL::EPL];
-        load_query<DT>(q, (size_t)b * sh.H + r, cg, q_dtype, qf);
+        Query<DT, QB> qf;
+        load_query<DT, QB>(q, (size_t)b * sh.H + r, cg, qf);
         float *srow = scores + ((size_t)b * sh.k + j) * T_pad;
         float m_run = -INFINITY, l_run = 0.f;            // of the scores that this lane has seen
         for (unsigned int u = wk.ua; u < wk.ue; ++u) {
             const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
             if (APPEND && wk.fresh >= (int)(u * U) && wk.fresh < (int)((u + 1) * U))
                 take_fresh<DT>(FreshRow<DT>(k_new, (size_t)b * sh.H + r, cg, q_dtype), kb, ks, pg.k, pg.k_scales, at, krow, wk.fresh - (int)(u * U), rj >= 0, cg, rg);
-            const float mine = dots<DT>(kb, qf, cg);
+            const float mine = dots<DT, QB>(kb, qf, cg);
             const int t = (int)(u * U) + cg * TL::RPW + rg;
             const bool there = cg < kUnroll && at >= 0 && t < len;
             const float sv = there ? scaled<DT>(mine, scale, ks) : -INFINITY;
@@ -1232,7 +1267,7 @@ void set_page_division(PagedShape *sh)
     sh->div_shift = q.shift;
 }
 
-template <int DT, bool APPEND>
+template <int DT, bool QB, bool APPEND>
 static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, const char *q, const char *k_new, const char *v_new, int dtype,
                                  const int32_t *h2c, const int32_t *rep, float scale, float *out, char *ws, const PagedPlan &plan, hipStream_t stream)
 {
@@ -1251,21 +1286,21 @@ static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, con
         const bool few = (long long)sh.B * sh.H <= kFewHeads;
         const int by_cluster = !few && sh.H <= kOrderedHeads && 2 * sh.k <= sh.H ? 1 : 0;
         auto rows = [&](auto *kernel) {
-            return (int)launch_kernel(kernel, dim3((unsigned int)sh.H, (unsigned int)sh.B), dim3(few ? 512 : 256), 0, stream, none, sh, pg, q, dtype, h2c, rep, by_cluster, scale,
+            return (int)launch_kernel(kernel, dim3((unsigned int)sh.H, (unsigned int)sh.B), dim3(few ? 512 : 256), 0, stream, none, sh, pg, q, h2c, rep, by_cluster, scale,
                                       k_new, v_new, out);
         };
-        if (h2c == nullptr) return few ? rows(paged_rows_kernel<DT, true, APPEND, 8>) : rows(paged_rows_kernel<DT, true, APPEND, 4>);
-        return few ? rows(paged_rows_kernel<DT, false, APPEND, 8>) : rows(paged_rows_kernel<DT, false, APPEND, 4>);
+        if (h2c == nullptr) return few ? rows(paged_rows_kernel<DT, QB, true, APPEND, 8>) : rows(paged_rows_kernel<DT, QB, true, APPEND, 4>);
+        return few ? rows(paged_rows_kernel<DT, QB, false, APPEND, 8>) : rows(paged_rows_kernel<DT, QB, false, APPEND, 4>);
     }
     if (h2c == nullptr) {
         const PagedSplit sp = make_paged_split(sh.B, sh.H, sh.T_max, cache, kAttendWorkers, kPagedParts);
-        const hipError_t e = launch_kernel(paged_attend_kernel<DT, APPEND>, waves(sp), block, 0, stream, none, sh, pg, sp, q, dtype, scale, k_new, v_new, partial, recs, out);
+        const hipError_t e = launch_kernel(paged_attend_kernel<DT, QB, APPEND>, waves(sp), block, 0, stream, none, sh, pg, sp, q, scale, k_new, v_new, partial, recs, out);
         if (e != hipSuccess) return (int)e;
         return join(paged_join_kernel<U, true, 1>, paged_join_kernel<U, true, kWaves>, sp);
     }
     const PagedSplit ss = make_paged_split(sh.B, sh.k, sh.T_max, cache, kStreamWorkers, kScoreParts), sv = make_paged_split(sh.B, sh.H, sh.T_max, cache, kStreamWorkers, kPagedParts);
     const int T_pad = padded_tokens(sh.T_max);
-    hipError_t e = launch_kernel(paged_scores_kernel<DT, APPEND>, waves(ss), block, 0, stream, none, sh, pg, ss, q, dtype, rep, scale, T_pad, k_new, scores, whole, recs);
+    hipError_t e = launch_kernel(paged_scores_kernel<DT, QB, APPEND>, waves(ss), block, 0, stream, none, sh, pg, ss, q, rep, scale, T_pad, k_new, scores, whole, recs);
     if (e != hipSuccess) return (int)e;
     e = launch_kernel(paged_values_kernel<DT, APPEND>, waves(sv), block, 0, stream, none, sh, pg, sv, ss, h2c, T_pad, v_new, dtype, scores, whole, recs, partial, out);
     if (e != hipSuccess) return (int)e;
@@ -1279,9 +1314,10 @@ int launch_paged_attention(const PagedShape &sh, const PagedPages &pg, const voi
         return typed(sh, pg, static_cast<const char *>(q), static_cast<const char *>(k_new), static_cast<const char *>(v_new), dtype, h2c, rep, scale, out,
                      static_cast<char *>(workspace), plan, stream);
     };
-    if (cache_dtype == CHAI_F32) return k_new ? go(paged_attention_typed<DT_F32, true>) : go(paged_attention_typed<DT_F32, false>);
-    if (cache_dtype == CHAI_BF16) return k_new ? go(paged_attention_typed<DT_BF16, true>) : go(paged_attention_typed<DT_BF16, false>);
-    return k_new ? go(paged_attention_typed<DT_E4M3, true>) : go(paged_attention_typed<DT_E4M3, false>);
+    if (cache_dtype == CHAI_F32) return k_new ? go(paged_attention_typed<DT_F32, false, true>) : go(paged_attention_typed<DT_F32, false, false>);
+    if (cache_dtype == CHAI_BF16) return k_new ? go(paged_attention_typed<DT_BF16, false, true>) : go(paged_attention_typed<DT_BF16, false, false>);
+    if (dtype == CHAI_BF16) return k_new ? go(paged_attention_typed<DT_E4M3, true, true>) : go(paged_attention_typed<DT_E4M3, true, false>);
+    return k_new ? go(paged_attention_typed<DT_E4M3, false, true>) : go(paged_attention_typed<DT_E4M3, false, false>);
 }
 
 int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *k_new, const void *v_new, int64_t k_stride,
