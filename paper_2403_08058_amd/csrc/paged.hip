@@ -577,11 +577,24 @@ __device__ __forceinline__ int head_by_cluster(const int32_t *__restrict__ h2c, 
     return i;                                // (every head is in a cluster: not reached)
 }
 
+// The row that workgroups y * H .. take: of up to 64 rows the y-th in an order of their lengths (`ordered`: rows whose workgroups are the
+// first of a CU each).  A CU's loads bound what its workgroups share: the shortest of the first rows come first, and so are on the CUs that
+// get a second workgroup of the longest of the others.
+__device__ __forceinline__ int row_by_length(const PagedShape &sh, int ordered, int y, int lane)
+{
+    const int len = taken_len(sh, sh.lens[min(lane, sh.B - 1)]);
+    const int key = lane < sh.B ? len * 64 + 63 - lane : -1;             // (lengths are at most 2^24; no two are alike)
+    int rank = 0;
+    for (int i = 0; i < sh.B; ++i) rank += __builtin_amdgcn_readlane(key, i) > key ? 1 : 0;
+    const int want = y < ordered ? ordered - 1 - y : y;
+    return __ffsll((long long)__ballot(lane < sh.B && rank == want)) - 1;
+}
+
 // Short rows: a workgroup of kRowWaves waves per (head, row), no parts and one launch.  The members of a cluster then each read its keys
 // (out of L2), and head h writes the new token's key to every slot that it represents.
 template <int DT, bool QB, bool IDENT, bool APPEND, int kRowWaves>
 __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_rows_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ q,
-                                                                    const int32_t *__restrict__ h2c, const int32_t *__restrict__ rep, int by_cluster, float scale,
+                                                                    const int32_t *__restrict__ h2c, const int32_t *__restrict__ rep, int by_cluster, int ordered, float scale,
                                                                     const char *__restrict__ k_new, const char *__restrict__ v_new, float *__restrict__ out)
 {
     using TL = Tile<DT>;
@@ -590,7 +603,7 @@ __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_
     __shared__ float acc_lds[kRowWaves][kHeadDim];
     __shared__ float2 rec_lds[kRowWaves];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int b = blockIdx.y;
+    const int b = ordered < 0 ? (int)blockIdx.y : row_by_length(sh, ordered, (int)blockIdx.y, lane);
     const int reps = IDENT ? 0 : rep[(size_t)b * sh.k + min(lane, sh.k - 1)];        // (asked for before the cluster is known)
     const int h = IDENT || !by_cluster ? (int)blockIdx.x : head_by_cluster(h2c + (size_t)b * sh.H, sh.H, sh.k, (int)blockIdx.x, lane);
     const int cg = lane % TL::LPR, rg = lane / TL::LPR;
@@ -1187,22 +1200,35 @@ constexpr unsigned int kPagedParts = 32, kScoreParts = 128;
 constexpr long long kJoinedByOne = 512;
 
 // Whether a workgroup takes a whole head's row (one launch) or shares of all rows' units go to independent waves (two or three).  Rows /
-// shares, in us, the new token's rows written too; "to T": lengths spread evenly up to T, else all T:
-// * clustered, 32 heads in 8, one row: 577 bf16 tokens 8.5 / 12.5, 1024 13.7 / 13.5, of codes 12.3 / 15.0, 2048 16.7 / 15.9, of fp32 577
-//   14.7 / 17.0; 4 x 72 in 16: to 577 bf16 16.3 / 20.3, 1024 31.5 / 30.4, to 1024 22.9 / 23.9; 16 x 32: 577 25.4 / 32.6, 1024 39.9 / 40.8,
-//   to 2048 of codes 29.6 / 33.9, all 2048 43.7 / 43.0, to 577 fp32 28.6 / 33.2; 32 x 32: 577 bf16 44.4 / 48.3, 1024 72 / 66.  Members of a
-//   cluster each read its keys, which costs long rows of many heads more than the launches.
-// * dense: 4 x 72 at 1024 bf16 34.3 / 33.8, 8 x 52 38.7 / 43.6, to 2048 50.6 / 45.7, 32 x 32 to 2048 98 / 104, all 2048 of codes 89 / 101.
-// Rows of one length fill the chip from some 768 heads on whatever the length; the rule goes by the longest row, the others' are not known.
+// shares, in us, the new token's rows written too, bf16 unless said; "to T": lengths spread evenly up to T, "few long": as their fourth power,
+// else all T:
+// * few heads, a CU's rate bounds a row: 1 x 32 in 8 of 577 tokens 10.3 / 15.8, 1024 14.4 / 16.0, 1400 16.5 / 16.3, 2048 22.3 / 18.3, of 2048 codes
+//   18.0 / 17.2, 4000 26.8 / 19.1; 1 x 52 dense of 1400 18.3 / 16.8, 2048 24.8 / 17.8; 2 x 32 of 2048 23.1 / 21.2, 4 x 32 24.9 / 27.1;
+// * clustered: 4 x 72 in 16 of 577 18.8 / 23.2, to 2048 28.9 / 33.0, 2048 47.3 / 43.3, to 2048 codes 22.9 / 24.2; 16 x 32 in 8: of 577 21.9 / 31.5,
+//   1024 32.5 / 39.2, to 2048 34.1 / 43.8, 2048 57.5 / 63.1, few long 27.0 / 26.6, to 4000 codes 39.4 / 45.4, few long to 4096 36.0 / 27.8, to 1000 fp32
+//   33.8 / 42.9; 32 x 32: to 1024 35.9 / 43.9, 1024 59.1 / 61.5, to 2048 63.2 / 68.8, 2048 112.5 / 111.3, few long 32.6 / 39.3; beyond: 64 x 32 to 1024
+//   codes 48.1 / 47.7, bf16 69.5 / 73.0, 1024 113.3 / 111.7, few long to 2048 codes 51.4 / 43.3;
+// * dense: 8 x 52 to 1777 36.1 / 38.9, 2048 69.1 / 73.1, 4 x 72 to 577 14.2 / 19.8, to 2048 34.1 / 37.4, 2048 61.6 / 53.5 (two workgroups on some
+//   CUs, one on most), 16 x 32 to 2048 46.1 / 51.9, few long 28.9 / 33.5.
+// The rule goes by the longest row, the others' lengths are not known here; the longer it may be, the more a lone long row costs (with rows of 1 MB
+// 16 x 32, few long to 4096, 46.1 / 39.4).
 static bool take_rows(int B, int H, int T_max, int cache, bool dense)
 {
     const long long heads = (long long)B * H, bytes = (long long)T_max * kHeadDim * (cache == CHAI_F32 ? 4 : (cache == CHAI_BF16 ? 2 : 1));
-    return bytes <= (dense ? (heads >= 768 ? 512 : 256) : (heads <= 512 ? 512 : heads <= 1024 ? 256 : 160)) * 1024ll;
+    return bytes <= (heads <= 64 ? 320 : (dense || heads <= 1024 ? 512 : 160)) * 1024ll;
 }
-// Eight waves per row where a CU has one row at most, else four (1 x 32 of 577 bf16 tokens 8.5 against 10.3 us; 16 x 32 of 256 16.8 against 15.5).
+// Eight waves per row where half the CUs have one, else four (1 x 32 of 1024 bf16 tokens 14.4 against 15.4 us, 4 x 32 15.8 / 16.5, 6 x 32 18.4 /
+// 18.0, 16 x 32 38.9 / 32.0).
 constexpr long long kFewHeads = 128;
-
+// Heads in order of their clusters from 129 (head, row) pairs on: 16 x 32 in 8 of 577 bf16 tokens 24.4 -> 21.5 us, 1024 38.8 -> 31.8, 2048 codes 43.3 -> 37.3, 4 x 72 in 16
+// of 1024 30.4 -> 27.2; a row alone pays for the counting (1 x 32 of 1024 14.5 -> 15.0), clusters of less than two heads
+// would have nothing for it.  A lane counts two heads at most.
 constexpr int kOrderedHeads = 128;
+// Rows in order of their lengths where CUs get a second workgroup and not many more (64 x 32 to 1024 codes 47.9 -> 52.6): 16 x 32 to 1024 bf16 tokens
+// 23.8 -> 20.8 us, to 2048 42.3 -> 34.1 and of codes 27.9 -> 24.3, 8 x 52 dense to 1024 26.3 -> 22.9; in order of falling lengths throughout 23.1,
+// 39.2, 25.9 and 24.9.  Rows that are all alike pay for the look at them: 16 x 32 of 1024 31.9 -> 32.4, 2048 56.9 -> 57.5.
+constexpr int kOrderedRows = 64, kCus = 256;
+constexpr long long kMostOrdered = 1024;
 
 static int padded_tokens(int T_max) { return (T_max + 63) / 64 * 64; }
 
@@ -1283,10 +1309,12 @@ static int paged_attention_typed(const PagedShape &sh, const PagedPages &pg, con
                                   partial, recs, out);
     };
     if (take_rows(sh.B, sh.H, sh.T_max, DT, h2c == nullptr)) {
-        const bool few = (long long)sh.B * sh.H <= kFewHeads;
+        const long long heads = (long long)sh.B * sh.H;
+        const bool few = heads <= kFewHeads;
+        const int ordered = sh.B <= kOrderedRows && heads > kCus && heads <= kMostOrdered ? kCus / sh.H : -1;
         const int by_cluster = !few && sh.H <= kOrderedHeads && 2 * sh.k <= sh.H ? 1 : 0;
         auto rows = [&](auto *kernel) {
-            return (int)launch_kernel(kernel, dim3((unsigned int)sh.H, (unsigned int)sh.B), dim3(few ? 512 : 256), 0, stream, none, sh, pg, q, h2c, rep, by_cluster, scale,
+            return (int)launch_kernel(kernel, dim3((unsigned int)sh.H, (unsigned int)sh.B), dim3(few ? 512 : 256), 0, stream, none, sh, pg, q, h2c, rep, by_cluster, ordered, scale,
                                       k_new, v_new, out);
         };
         if (h2c == nullptr) return few ? rows(paged_rows_kernel<DT, QB, true, APPEND, 8>) : rows(paged_rows_kernel<DT, QB, true, APPEND, 4>);
