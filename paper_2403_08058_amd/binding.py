@@ -526,17 +526,7 @@ def _paged_types(fn, dtype, k_pages, v_pages, k_scales, v_scales, n_pages, H, k,
 
 def _ptrs(tensors):
     """Addresses of device tensors that lie in one piece, None for None."""
-    out = []
-    for t in tensors:
-        if t is None:
-            out.append(None)
-        else:
-            if not t.is_cuda:
-                raise ValueError("libchai takes device tensors")
-            if not t.is_contiguous():
-                raise ValueError("libchai takes contiguous tensors")
-            out.append(t.data_ptr())
-    return out
+    return [None if t is None else t.data_ptr() if t.is_cuda and t.is_contiguous() else _ptr(t) for t in tensors]
 
 
 def chai_paged_workspace_bytes(B: int, H: int, k: int, T_max: int, d: int = 128) -> int:

@@ -476,6 +476,51 @@ def test_step_of_shared_rows(cache, H, k, page, lengths):
     s.check(q)
 
 
+# more than 256 (head, row) pairs of short rows: taken in the order of their lengths, a row's heads in that of their clusters
+ORDERED = [
+    (32, 8, [40, 0, 300, 300, 1, 40, 555, 0, 300, 17, 64, 65]),
+    (52, 52, [100, 700, 0, 700, 3, 699]),
+    (100, 30, [33, 400, 33]),                              # two heads per lane
+    (130, 20, [200, 5, 90]),                               # more heads than that
+    (300, 7, [70, 128]),                                   # one row is more than a workgroup per CU
+    (5, 2, [(37 * i) % 211 for i in range(64)]),           # as many rows as lanes
+    (5, 2, [(37 * i) % 211 for i in range(65)]),           # one more
+    (16, 8, [0] * 20),
+    (20, 3, [128] * 51),
+]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3", "f32"])
+@pytest.mark.parametrize("H,k,lengths", ORDERED)
+def test_rows_in_the_order_of_their_lengths(cache, H, k, lengths):
+    print(f"[paged] ordered rows {cache} H={H} k={k} lengths={lengths}", flush=True)
+    s = Setting(9980 + H, cache, H, k, 16, lengths, blocks=64)
+    q = s.normal(s.B, H, D)
+    first = s.check(q, T_max=999)
+    s.lengths.copy_(torch.tensor([n if n else -5 - i for i, n in enumerate(lengths)]))      # rows without a position
+    assert torch.equal(s.attend(q, 999), first)
+    if len(lengths) > 2:
+        s.lengths[2], s.host_lengths[2] = 1 << 30, 500                                      # one longer than the bound
+        s.host_table[2, :32] = np.arange(32) % s.n_pages
+        s.table.copy_(torch.from_numpy(s.host_table))
+        s.check(q, T_max=500)
+
+
+@pytest.mark.parametrize("maps", ["one", "skewed", "last"])
+def test_clusters_of_any_size(maps):
+    """All heads in one cluster, one cluster of nearly all, clusters without a head."""
+    H, k = 72, 9
+    s = Setting(9990, "bf16", H, k, 16, [100, 333, 20, 64])
+    h2c, rep = torch.zeros((4, H), dtype=torch.int32), torch.zeros((4, k), dtype=torch.int32)
+    if maps == "skewed":
+        h2c[:, 3:11] = torch.arange(1, 9, dtype=torch.int32)
+        rep[:, 1:] = torch.arange(3, 11, dtype=torch.int32)
+    if maps == "last":
+        h2c[:], rep[:, k - 1], rep[:, :k - 1] = k - 1, 5, -1
+    s.h2c, s.rep = h2c.cuda(), rep.cuda()
+    s.check(s.normal(4, H, D))
+
+
 def test_slots_without_a_cluster():
     """Fewer clusters than slots: what the others' keys hold reaches nobody, short rows and long ones."""
     for T in (100, 3000):
