@@ -437,12 +437,16 @@ __device__ __forceinline__ void take_fresh(const FreshRow<DT> &fresh, u32x4 (&bu
     const int load = local / Tile<DT>::RPW, group = local % Tile<DT>::RPW;
     if (__builtin_amdgcn_readlane(at, load) < 0) return;     // in no page
     const unsigned int to = (unsigned int)__builtin_amdgcn_readlane((int)row, load) + (unsigned int)group;
-    if (rg != group) return;
+    // (selections: an element chosen at run time would put the buffer into memory)
 #pragma unroll
-    for (int i = 0; i < kUnroll; ++i)
-        if (i == load) buf[i] = fresh.raw;
-    if (DT == DT_E4M3 && cg == load) row_scale = fresh.scale;
-    if (keep) fresh.store(rows, scales, to, cg);
+    for (int i = 0; i < kUnroll; ++i) {
+        const bool here = i == load && rg == group;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) buf[i][e] = here ? fresh.raw[e] : buf[i][e];
+        asm("" : "+v"(buf[i]));
+    }
+    if (DT == DT_E4M3 && cg == load && rg == group) row_scale = fresh.scale;
+    if (keep && rg == group) fresh.store(rows, scales, to, cg);
 }
 
 constexpr float kPagedDown = 0x1p-24f;       // times kMaxPagedTokens weights of at most 1: at most 1
@@ -486,17 +490,21 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
         for (int e = 0; e < TL::EPL; ++e) acc[e] = 0.f;
         m = -INFINITY;
         l_run = 0.f;
-#pragma unroll 1
-        for (unsigned int u = u0; u < ue; u += step) {
-            const int at2 = look_up<DT>(sh, table, u + 2 * step, ue, len, lane);
-            const bool has_fresh = APPEND && fresh >= (int)(u * U) && fresh < (int)((u + 1) * U);
+        // The last unit apart: what it would ask for is nobody's, and the barrier after it would wait for that (1 x 32 heads of 1024 bf16 tokens
+        // 14.4 -> 13.5 us).  The token being decoded is the row's last, so in none of the others.
+        auto take = [&](unsigned int u, auto more) __attribute__((always_inline)) {
+            constexpr bool kMore = decltype(more)::value;
+            const int at2 = kMore ? look_up<DT>(sh, table, u + 2 * step, ue, len, lane) : -1;
+            const bool has_fresh = APPEND && !kMore && fresh >= (int)(u * U) && fresh < (int)((u + 1) * U);
             if (has_fresh) take_fresh<DT>(FreshRow<DT>(k_new, (size_t)b * sh.H + r, cg, q_dtype), kb, ks, pg.k, pg.k_scales, at, krow, fresh - (int)(u * U), IDENT, cg, rg);
             const float mine = dots<DT, QB>(kb, qf, cg);
             const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
             const float sv = there ? scaled<DT>(mine, scale, ks) : -INFINITY;
-            krow = pool_row<DT>(sh, at1, u + step, sh.k, c, lane);
-            request<DT, IDENT>(kb, pg.k, krow, lane_off);
-            if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
+            if constexpr (kMore) {
+                krow = pool_row<DT>(sh, at1, u + step, sh.k, c, lane);
+                request<DT, IDENT>(kb, pg.k, krow, lane_off);
+                if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
+            }
             if (__any(sv > m)) {
                 const float m_new = fmaxf(m, all_max(sv));
                 const float f = __expf(m - m_new);
@@ -509,12 +517,18 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
             l_run += p;
             if (has_fresh) take_fresh<DT>(FreshRow<DT>(v_new, (size_t)b * sh.H + h, cg, q_dtype), vb, vs, pg.v, pg.v_scales, at, vrow, fresh - (int)(u * U), true, cg, rg);
             weigh<DT>(acc, vb, DT == DT_E4M3 ? (there ? p * vs : 0.f) : p, there, strip, cg, rg);
-            vrow = pool_row<DT>(sh, at1, u + step, sh.H, h, lane);
-            request<DT>(vb, pg.v, vrow, lane_off);
-            if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
+            if constexpr (kMore) {
+                vrow = pool_row<DT>(sh, at1, u + step, sh.H, h, lane);
+                request<DT>(vb, pg.v, vrow, lane_off);
+                if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
+            }
             at = at1;
             at1 = at2;
-        }
+        };
+        unsigned int u = u0;
+#pragma unroll 1
+        for (; u + step < ue; u += step) take(u, std::true_type());
+        take(u, std::false_type());
         // lane groups; sums beyond the largest float (the quotient is not) are taken again with smaller weights
         bool large = false;
 #pragma unroll
@@ -689,24 +703,31 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? (APPEND ? 4 : 5) : 6) void 
         load_query<DT, QB>(q, (size_t)b * sh.H + r, cg, qf);
         float *srow = scores + ((size_t)b * sh.k + j) * T_pad;
         float m_run = -INFINITY, l_run = 0.f;            // of the scores that this lane has seen
-        for (unsigned int u = wk.ua; u < wk.ue; ++u) {
-            const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
-            if (APPEND && wk.fresh >= (int)(u * U) && wk.fresh < (int)((u + 1) * U))
+        auto take = [&](unsigned int u, auto more) __attribute__((always_inline)) {        // (the last unit asks for none)
+            constexpr bool kMore = decltype(more)::value;
+            const int at2 = kMore ? look_up<DT>(sh, table, u + 2, wk.ue, len, lane) : -1;
+            if (APPEND && !kMore && wk.fresh >= (int)(u * U) && wk.fresh < (int)((u + 1) * U))
                 take_fresh<DT>(FreshRow<DT>(k_new, (size_t)b * sh.H + r, cg, q_dtype), kb, ks, pg.k, pg.k_scales, at, krow, wk.fresh - (int)(u * U), rj >= 0, cg, rg);
             const float mine = dots<DT, QB>(kb, qf, cg);
             const int t = (int)(u * U) + cg * TL::RPW + rg;
             const bool there = cg < kUnroll && at >= 0 && t < len;
             const float sv = there ? scaled<DT>(mine, scale, ks) : -INFINITY;
-            krow = pool_row<DT>(sh, at1, u + 1, sh.k, j, lane);
-            request<DT>(kb, pg.k, krow, lane_off);
-            if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
+            if constexpr (kMore) {
+                krow = pool_row<DT>(sh, at1, u + 1, sh.k, j, lane);
+                request<DT>(kb, pg.k, krow, lane_off);
+                if (DT == DT_E4M3) ks = pg.k_scales[krow + (at1 < 0 ? 0 : rg)];
+            }
             if (cg < kUnroll) srow[t] = sv;
             const float m_new = fmaxf(m_run, sv), ref = m_new == -INFINITY ? 0.f : m_new;
             l_run = l_run * __expf(m_run - ref) + __expf(sv - ref);
             m_run = m_new;
             at = at1;
             at1 = at2;
-        }
+        };
+        unsigned int u = wk.ua;
+#pragma unroll 1
+        for (; u + 1 < wk.ue; ++u) take(u, std::true_type());
+        take(u, std::false_type());
         const float M = all_max(m_run);
         const float L = all_sum(m_run == -INFINITY ? l_run : l_run * __expf(m_run - M));     // (lanes that saw only NaN hold it in l_run)
         if (lane == 0) (wk.whole() ? whole[(size_t)b * sh.k + j] : parts[wk.slot(worker)]) = make_float2(M, L);
@@ -764,20 +785,27 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 4 : 5) void paged_values_ke
         float acc[TL::EPL];
 #pragma unroll
         for (int e = 0; e < TL::EPL; ++e) acc[e] = 0.f;
-        for (unsigned int u = wk.ua; u < wk.ue; ++u) {
-            const int at2 = look_up<DT>(sh, table, u + 2, wk.ue, len, lane);
+        auto take = [&](unsigned int u, auto more) __attribute__((always_inline)) {
+            constexpr bool kMore = decltype(more)::value;
+            const int at2 = kMore ? look_up<DT>(sh, table, u + 2, wk.ue, len, lane) : -1;
             const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
             const float p = there ? __expf(sv - M) * inv : 0.f;
-            if (APPEND && wk.fresh >= (int)(u * U) && wk.fresh < (int)((u + 1) * U))
+            if (APPEND && !kMore && wk.fresh >= (int)(u * U) && wk.fresh < (int)((u + 1) * U))
                 take_fresh<DT>(FreshRow<DT>(v_new, (size_t)b * sh.H + h, cg, q_dtype), vb, vs, pg.v, pg.v_scales, at, vrow, wk.fresh - (int)(u * U), true, cg, rg);
             weigh<DT>(acc, vb, DT == DT_E4M3 ? (there ? p * vs : 0.f) : p, there, strip[w], cg, rg);
-            vrow = pool_row<DT>(sh, at1, u + 1, sh.H, h, lane);
-            request<DT>(vb, pg.v, vrow, lane_off);
-            if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
-            sv = srow[min(u + 1, wk.ue - 1) * U];
+            if constexpr (kMore) {
+                vrow = pool_row<DT>(sh, at1, u + 1, sh.H, h, lane);
+                request<DT>(vb, pg.v, vrow, lane_off);
+                if (DT == DT_E4M3) vs = pg.v_scales[vrow + (at1 < 0 ? 0 : rg)];
+                sv = srow[(u + 1) * U];
+            }
             at = at1;
             at1 = at2;
-        }
+        };
+        unsigned int u = wk.ua;
+#pragma unroll 1
+        for (; u + 1 < wk.ue; ++u) take(u, std::true_type());
+        take(u, std::false_type());
 #pragma unroll
         for (int e = 0; e < TL::EPL; ++e) acc[e] = sum_groups<TL::LPR>(acc[e]);
         float *o = wk.whole() ? out + ((size_t)b * sh.H + h) * kHeadDim : partial + wk.slot(worker) * kHeadDim;
@@ -1202,20 +1230,22 @@ constexpr long long kJoinedByOne = 512;
 // Whether a workgroup takes a whole head's row (one launch) or shares of all rows' units go to independent waves (two or three).  Rows /
 // shares, in us, the new token's rows written too, bf16 unless said; "to T": lengths spread evenly up to T, "few long": as their fourth power,
 // else all T:
-// * few heads, a CU's rate bounds a row: 1 x 32 in 8 of 577 tokens 10.3 / 15.8, 1024 14.4 / 16.0, 1400 16.5 / 16.3, 2048 22.3 / 18.3, of 2048 codes
-//   18.0 / 17.2, 4000 26.8 / 19.1; 1 x 52 dense of 1400 18.3 / 16.8, 2048 24.8 / 17.8; 2 x 32 of 2048 23.1 / 21.2, 4 x 32 24.9 / 27.1;
-// * clustered: 4 x 72 in 16 of 577 18.8 / 23.2, to 2048 28.9 / 33.0, 2048 47.3 / 43.3, to 2048 codes 22.9 / 24.2; 16 x 32 in 8: of 577 21.9 / 31.5,
-//   1024 32.5 / 39.2, to 2048 34.1 / 43.8, 2048 57.5 / 63.1, few long 27.0 / 26.6, to 4000 codes 39.4 / 45.4, few long to 4096 36.0 / 27.8, to 1000 fp32
-//   33.8 / 42.9; 32 x 32: to 1024 35.9 / 43.9, 1024 59.1 / 61.5, to 2048 63.2 / 68.8, 2048 112.5 / 111.3, few long 32.6 / 39.3; beyond: 64 x 32 to 1024
-//   codes 48.1 / 47.7, bf16 69.5 / 73.0, 1024 113.3 / 111.7, few long to 2048 codes 51.4 / 43.3;
-// * dense: 8 x 52 to 1777 36.1 / 38.9, 2048 69.1 / 73.1, 4 x 72 to 577 14.2 / 19.8, to 2048 34.1 / 37.4, 2048 61.6 / 53.5 (two workgroups on some
-//   CUs, one on most), 16 x 32 to 2048 46.1 / 51.9, few long 28.9 / 33.5.
+// * few heads, a CU's rate bounds a row: 1 x 32 in 8 of 577 tokens 9.7 / 15.9, 1024 13.5 / 15.9, 1400 16.0 / 15.8, 2048 21.6 / 15.6, of 2048 codes
+//   17.3 / 17.1, 4000 26.2 / 18.0; 1 x 52 dense of 1400 17.2 / 15.7, 2048 23.3 / 16.8; 2 x 32 of 2048 22.3 / 18.3, 4 x 32 24.1 / 24.5, to 2048
+//   22.9 / 20.0;
+// * clustered: 4 x 72 in 16 of 577 18.0 / 21.5, to 1400 21.4 / 24.8, to 2048 28.1 / 29.8, 2048 46.7 / 39.5 (two workgroups on some CUs, one on most),
+//   to 2048 codes 22.3 / 22.9; 8 x 32 in 8 of 2048 32.4 / 36.6; 16 x 32: of 577 21.3 / 28.2, 1024 32.0 / 37.2, to 2048 34.1 / 41.1, 2048 57.4 / 62.2, few
+//   long 26.1 / 24.3, to 4000 codes 38.6 / 43.7, few long to 4096 35.1 / 26.8, to 1000 fp32 33.2 / 40.9; 32 x 32: to 1024 37.2 / 40.6, 1024 58.2 / 60.6,
+//   to 2048 62.4 / 65.8, 2048 111.7 / 111.1, few long 32.5 / 35.8; beyond: 64 x 32 to 1024 codes 47.1 / 45.6, bf16 67.0 / 67.2, 1024 110.7 / 111.2, few
+//   long to 2048 codes 49.2 / 40.2;
+// * dense: 8 x 52 to 1777 35.9 / 38.2, 2048 68.1 / 72.9, 4 x 72 to 577 13.4 / 19.1, to 2048 33.5 / 36.9, 2048 60.0 / 52.6, 16 x 32 to 2048 46.0 /
+//   51.0, few long 28.6 / 31.8.
 // The rule goes by the longest row, the others' lengths are not known here; the longer it may be, the more a lone long row costs (with rows of 1 MB
-// 16 x 32, few long to 4096, 46.1 / 39.4).
+// 16 x 32, few long to 4096, 45.2 / 36.3).
 static bool take_rows(int B, int H, int T_max, int cache, bool dense)
 {
     const long long heads = (long long)B * H, bytes = (long long)T_max * kHeadDim * (cache == CHAI_F32 ? 4 : (cache == CHAI_BF16 ? 2 : 1));
-    return bytes <= (heads <= 64 ? 320 : (dense || heads <= 1024 ? 512 : 160)) * 1024ll;
+    return bytes <= (heads <= 64 ? 320 : heads <= 128 ? 400 : dense || heads <= 1024 ? 512 : 160) * 1024ll;
 }
 // Eight waves per row where half the CUs have one, else four (1 x 32 of 1024 bf16 tokens 14.4 against 15.4 us, 4 x 32 15.8 / 16.5, 6 x 32 18.4 /
 // 18.0, 16 x 32 38.9 / 32.0).
