@@ -605,7 +605,12 @@ __device__ __forceinline__ int row_by_length(const PagedShape &sh, int ordered, 
 }
 
 // Short rows: a workgroup of kRowWaves waves per (head, row), no parts and one launch.  The members of a cluster then each read its keys
-// (out of L2), and head h writes the new token's key to every slot that it represents.
+// (out of L2), and head h writes the new token's key to every slot that it represents.  Waves take units in turn, each with a softmax of its
+// own, and join them in LDS.
+// Bound by HBM where the rows fill the CUs evenly: 16 x 32 heads in 8 clusters of up to 2048 bf16 tokens 34.0 us a step, 179 MB at 5.3 TB/s (a
+// cluster's keys come from beyond the L2s 1.6 times: 201 MB), 8 x 52 dense of up to 1777 35.6 us, 6.0 TB/s; of codes 23.5 us,
+// 3.9 TB/s, of which the products are 5.  Below some 15 us by launch, look-ups one after the other (map and lengths, page, rows) and the longest row:
+// 4 x 72 of up to 577 12.5 us, a row of 32 fp32 heads at 256 8.1 us.
 template <int DT, bool QB, bool IDENT, bool APPEND, int kRowWaves>
 __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_rows_kernel(PagedShape sh, PagedPages pg, const char *__restrict__ q,
                                                                     const int32_t *__restrict__ h2c, const int32_t *__restrict__ rep, int by_cluster, int ordered, float scale,
@@ -669,7 +674,9 @@ __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// Attention in two passes, for layers with fewer clusters than heads: the keys of a cluster are read once, not once per member.
+// Attention in two passes, for layers with fewer clusters than heads whose rows are shared: the keys of a cluster are read once, not once per
+// member.  Both are bound by HBM: 4 x 32 heads in 4 clusters of 32768 bf16 tokens 24 us of scores (134 MB, 5.6 TB/s), 165 us of values (1.07 GB, 6.5
+// TB/s) and 5 us that join the parts; 64 x 32 of up to 4096 codes, most short, 12.6, 37 and 5 us (289 MB with the absent pages, 5.5 TB/s in all).
 // Scores: a wave streams keys of its units, writes s[b][j][t] (-inf where nothing is to be attended to, whole units) and the maximum
 // and sum of exponentials of every stretch: `whole` of a stream that it took alone, else `parts` of the wave.
 // ---------------------------------------------------------------------------------------------------------
@@ -813,7 +820,7 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 4 : 5) void paged_values_ke
     } while (wk.next(sh, deal, sh.H));
 }
 
-// Streams that several waves took.  WEIGHED (one pass): out = mean of their parts, each weighed by its sum of exponentials times
+// Streams that several waves took, 5 us of launch and look-ups, whatever the sizes.  WEIGHED (one pass): out = mean of their parts, each weighed by its sum of exponentials times
 // exp(its reference - the largest); else their sum.  JW waves per (row, head), two columns per lane; streams that one wave took are left
 // alone, rows without a position get 0.
 template <int U, bool WEIGHED, int JW>
@@ -876,6 +883,8 @@ __global__ __launch_bounds__(kBlock) void paged_join_kernel(PagedShape sh, Paged
 // New rows into pages, and pages into contiguous rows.  A workgroup takes `rows` rows of one request: 1 << shift consecutive tokens (so
 // that one new token of many streams fills a workgroup as well) of rows >> shift streams; streams are the k key slots, then the H value
 // heads.  Sixteen lanes per row, eight elements each, all rows requested at once.
+// Bound by HBM at the rate of a copy: 16 x 40 streams of up to 2043 bf16 tokens quantised 48 us (270 MB, 5.6 TB/s), up to 2048 codes read back 51.5 us
+// (5.2 TB/s), 4 x 88 of 512 copied 16 us (92 MB, 5.8 TB/s); one token of 16 x 40 streams 4.0 us, a launch and two look-ups.
 // ---------------------------------------------------------------------------------------------------------
 template <bool BF16>
 constexpr int kMoveUnroll = BF16 ? 8 : 4;
@@ -1250,9 +1259,9 @@ static bool take_rows(int B, int H, int T_max, int cache, bool dense)
 // Eight waves per row where half the CUs have one, else four (1 x 32 of 1024 bf16 tokens 14.4 against 15.4 us, 4 x 32 15.8 / 16.5, 6 x 32 18.4 /
 // 18.0, 16 x 32 38.9 / 32.0).
 constexpr long long kFewHeads = 128;
-// Heads in order of their clusters from 129 (head, row) pairs on: 16 x 32 in 8 of 577 bf16 tokens 24.4 -> 21.5 us, 1024 38.8 -> 31.8, 2048 codes 43.3 -> 37.3, 4 x 72 in 16
-// of 1024 30.4 -> 27.2; a row alone pays for the counting (1 x 32 of 1024 14.5 -> 15.0), clusters of less than two heads
-// would have nothing for it.  A lane counts two heads at most.
+// Heads in order of their clusters from 129 (head, row) pairs on: 16 x 32 in 8 of 577 bf16 tokens 24.4 -> 21.5 us, 1024 38.8 -> 31.8, of 2048 codes
+// 43.3 -> 37.3, 4 x 72 in 16 of 1024 30.4 -> 27.2; a row alone pays for the counting (1 x 32 of 1024 14.5 -> 15.0), clusters of less than two
+// heads would have nothing for it.  A lane counts two heads at most.
 constexpr int kOrderedHeads = 128;
 // Rows in order of their lengths where CUs get a second workgroup and not many more (64 x 32 to 1024 codes 47.9 -> 52.6): 16 x 32 to 1024 bf16 tokens
 // 23.8 -> 20.8 us, to 2048 42.3 -> 34.1 and of codes 27.9 -> 24.3, 8 x 52 dense to 1024 26.3 -> 22.9; in order of falling lengths throughout 23.1,
