@@ -1,7 +1,7 @@
 """Requests of different lengths served out of one pool of pages, the way the calls on pages are meant to be used.
 
     python examples/paged_serving.py [--layers 4] [--heads 32] [--clusters 8] [--rows 16] [--page 64] [--cache bf16|e4m3]
-                                     [--requests 48] [--steps 1024] [--eager] [--seed 1]
+                                     [--requests 48] [--steps 2048] [--eager] [--seed 1]
 
 Requests arrive and leave.  A new one gets pages for its prompt; layer by layer its membership is decided on the first five
 positions, its prompt attended to, and its keys (the representatives') and values written into pages.  Every step then adds a
@@ -187,7 +187,7 @@ class Server:
 
 def main():
     ap = argparse.ArgumentParser(description="Requests of different lengths out of one pool of pages.")
-    for name, default in (("layers", 4), ("heads", 32), ("clusters", 8), ("rows", 16), ("page", 64), ("requests", 48), ("steps", 1024),
+    for name, default in (("layers", 4), ("heads", 32), ("clusters", 8), ("rows", 16), ("page", 64), ("requests", 48), ("steps", 2048),
                           ("longest", 2048), ("seed", 1)):
         ap.add_argument("--" + name, type=int, default=default)
     ap.add_argument("--cache", choices=["bf16", "e4m3"], default="bf16")
