@@ -551,7 +551,8 @@ int chai_project_qk_timed(const void *x, const void *w_q, const void *w_k, const
  *   positions t < seq_lens[b] of its row (taken into [0,T_max]) that are in a
  *   page, as chai_decode_attention does:
  *     q [B,H,d] dtype;  out [B,H,d] fp32, written;  maps as there
- *   Rows without such a position, and heads whose scores are all -inf, get 0.
+ *   Positions whose score is -inf weigh nothing, whatever their values hold.
+ *   Rows without a position, and heads whose scores are all -inf, get 0.
  *   T_max (1 <= T_max <= max_blocks * page) bounds the rows' lengths; what the
  *   masked places hold (infinities, NaN) does not matter.
  * chai_paged_decode_step: position seq_lens[b]-1 of every row (if seq_lens[b]

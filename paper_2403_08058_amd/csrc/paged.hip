@@ -307,7 +307,8 @@ __device__ __forceinline__ float dots(const u32x4 (&kb)[kUnroll], const Query<DT
     return mine;
 }
 
-// acc += weight * row over a unit's rows; `weight` lies with the lane that owns the row (as in dots), `there` says whether it counts
+// acc += weight * row over a unit's rows; `weight` lies with the lane that owns the row (as in dots), `there` says whether it counts: rows
+// that are not attended to and those whose score is -inf do not, else a weight of 0 times an infinite value would be NaN
 template <int DT>
 __device__ __forceinline__ void weigh(float (&acc)[Tile<DT>::EPL], u32x4 (&vb)[kUnroll], float weight, bool there, float *strip, int cg, int rg)
 {
@@ -516,7 +517,8 @@ __device__ __forceinline__ void attend_units(const PagedShape &sh, const PagedPa
             const float p = __expf(sv - (m == -INFINITY ? 0.f : m)) * down;
             l_run += p;
             if (has_fresh) take_fresh<DT>(FreshRow<DT>(v_new, (size_t)b * sh.H + h, cg, q_dtype), vb, vs, pg.v, pg.v_scales, at, vrow, fresh - (int)(u * U), true, cg, rg);
-            weigh<DT>(acc, vb, DT == DT_E4M3 ? (there ? p * vs : 0.f) : p, there, strip, cg, rg);
+            const bool counts = sv != -INFINITY;
+            weigh<DT>(acc, vb, DT == DT_E4M3 ? (counts ? p * vs : 0.f) : p, counts, strip, cg, rg);
             if constexpr (kMore) {
                 vrow = pool_row<DT>(sh, at1, u + step, sh.H, h, lane);
                 request<DT>(vb, pg.v, vrow, lane_off);
@@ -795,7 +797,7 @@ __global__ __launch_bounds__(kBlock, DT == DT_E4M3 ? 4 : 5) void paged_values_ke
         auto take = [&](unsigned int u, auto more) __attribute__((always_inline)) {
             constexpr bool kMore = decltype(more)::value;
             const int at2 = kMore ? look_up<DT>(sh, table, u + 2, wk.ue, len, lane) : -1;
-            const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len;
+            const bool there = cg < kUnroll && at >= 0 && (int)(u * U) + cg * TL::RPW + rg < len && sv != -INFINITY;
             const float p = there ? __expf(sv - M) * inv : 0.f;
             if (APPEND && !kMore && wk.fresh >= (int)(u * U) && wk.fresh < (int)((u + 1) * U))
                 take_fresh<DT>(FreshRow<DT>(v_new, (size_t)b * sh.H + h, cg, q_dtype), vb, vs, pg.v, pg.v_scales, at, vrow, wk.fresh - (int)(u * U), true, cg, rg);
