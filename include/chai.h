@@ -528,6 +528,7 @@ int chai_project_qk_timed(const void *x, const void *w_q, const void *w_k, const
  *               the calls can be captured and replayed with other lengths.
  *
  * Layers without clusters: k = H with rep_heads and head_to_cluster both NULL.
+ * B = 0 and Tn = 0 are no-ops; arrays that then have no elements may be NULL.
  * page is a multiple of 8, at least 8.  Limits (CHAI_ERR_UNSUPPORTED): d = 128,
  * B <= 4096, H + k <= 65535, T_max and Tn <= 2^24, n_pages * H * page < 2^32
  * rows, B * H * T_max and B * (H + k) * Tn < 2^34.

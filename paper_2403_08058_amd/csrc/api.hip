@@ -557,15 +557,16 @@ int chai_dense_prefill_attention(const void *q, const void *k_cache, const void 
                                      out, workspace, true, KernelEvents{}, static_cast<hipStream_t>(stream)));
 }
 
-// Checks common to the calls on pages, and what the kernels are told of them.
+// Checks common to the calls on pages, and what the kernels are told of them.  Arrays of no elements (B = 0, Tn = 0) may be NULL, as an
+// allocator may give them.
 static int check_pages(const void *k_pages, const void *v_pages, const float *k_scales, const float *v_scales, const int32_t *table, int B,
                        int H, int k, bool maps, int n_pages, int page, int max_blocks, int d, int dtype, int cache_dtype, PagedShape *sh,
                        PagedPages *pg)
 {
-    if (!k_pages || !v_pages || !table) return CHAI_ERR_NULL;
+    if (!k_pages || !v_pages || (!table && B != 0)) return CHAI_ERR_NULL;
     if (bad_dtype(dtype) || (cache_dtype != dtype && cache_dtype != CHAI_E4M3)) return CHAI_ERR_DTYPE;
     if (cache_dtype == CHAI_E4M3 && (!k_scales || !v_scales)) return CHAI_ERR_NULL;
-    if (B < 0 || H < 1 || k < 1 || k > H || (!maps && k != H) || n_pages < 1 || page < 8 || page % 8 != 0 || max_blocks < 1 || d < 1)
+    if (B < 0 || H < 1 || k < 1 || k > H || (!maps && k != H && B != 0) || n_pages < 1 || page < 8 || page % 8 != 0 || max_blocks < 1 || d < 1)
         return CHAI_ERR_SHAPE;
     if (d != kHeadDim || B > kMaxPagedBatch || (long long)H + k > kMaxGridYZ || page > kMaxPagedTokens ||
         (unsigned long long)n_pages * (unsigned long long)H >= (1ull << 32) / (unsigned int)page)
@@ -589,7 +590,7 @@ static int check_pages(const void *k_pages, const void *v_pages, const float *k_
 static int check_paged_decode(const void *q, const int32_t *h2c, const int32_t *rep, const int32_t *lens, int T_max, const float *out,
                               const void *workspace, size_t workspace_bytes, PagedShape *sh, PagedPlan *plan)
 {
-    if (!q || !lens || !out || !h2c != !rep) return CHAI_ERR_NULL;
+    if (sh->B > 0 && (!q || !lens || !out || !h2c != !rep)) return CHAI_ERR_NULL;
     if (T_max < 1 || (long long)sh->max_blocks * sh->page < T_max) return CHAI_ERR_SHAPE;
     if (T_max > kMaxPagedTokens || (long long)sh->B * sh->H * T_max >= (1ll << 34)) return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(out)) return CHAI_ERR_ALIGN;
@@ -614,7 +615,7 @@ int chai_paged_append_kv(const void *k_new, const void *v_new, int64_t k_head_st
                          void *k_pages, void *v_pages, float *k_scales, float *v_scales, int B, int H, int k, int Tn,
                          int n_pages, int page, int max_blocks, int d, int dtype, int cache_dtype, void *stream)
 {
-    if (!k_new || !v_new || !start) return CHAI_ERR_NULL;
+    if (B != 0 && (!start || (Tn != 0 && (!k_new || !v_new)))) return CHAI_ERR_NULL;
     PagedShape sh;
     PagedPages pg;
     const int st = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, B, H, k, rep_heads != nullptr, n_pages, page,
@@ -634,7 +635,7 @@ int chai_paged_gather_kv(const void *k_pages, const void *v_pages, const float *
                          int B, int H, int k, int Tn, int n_pages, int page, int max_blocks, int d, int dtype,
                          int cache_dtype, void *stream)
 {
-    if (!start || !k_out || !v_out) return CHAI_ERR_NULL;
+    if (B != 0 && (!start || (Tn != 0 && (!k_out || !v_out)))) return CHAI_ERR_NULL;
     PagedShape sh;
     PagedPages pg;
     const int st = check_pages(k_pages, v_pages, k_scales, v_scales, block_table, B, H, k, true, n_pages, page, max_blocks, d, dtype,
@@ -671,7 +672,7 @@ int chai_paged_decode_step(const void *q, const void *k_new, const void *v_new, 
                            int page, int max_blocks, int d, int dtype, int cache_dtype, float scale, float *out,
                            void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!k_new || !v_new) return CHAI_ERR_NULL;
+    if (B != 0 && (!k_new || !v_new)) return CHAI_ERR_NULL;
     PagedShape sh;
     PagedPages pg;
     PagedPlan plan;
