@@ -569,7 +569,7 @@ static int check_pages(const void *k_pages, const void *v_pages, const float *k_
     if (B < 0 || H < 1 || k < 1 || k > H || (!maps && k != H && B != 0) || n_pages < 1 || page < 8 || page % 8 != 0 || max_blocks < 1 || d < 1)
         return CHAI_ERR_SHAPE;
     if (d != kHeadDim || B > kMaxPagedBatch || (long long)H + k > kMaxGridYZ || page > kMaxPagedTokens ||
-        (unsigned long long)n_pages * (unsigned long long)H >= (1ull << 32) / (unsigned int)page)
+        (unsigned long long)n_pages * (unsigned long long)H > 0xffffffffull / (unsigned int)page)
         return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(k_pages) || !aligned16(v_pages)) return CHAI_ERR_ALIGN;
     sh->table = table;
