@@ -78,16 +78,19 @@ class Server:
         return (k, v), {"k_scales": scales[0], "v_scales": scales[1]}
 
     # ---- pages
-    def pages_left(self, tokens: int) -> bool:
-        return len(self.free) >= -(-tokens // self.page)
-
-    def _grow(self, row: int, length: int):
-        """Pages for positions up to `length`; the row's length becomes that."""
-        if length > self.longest:
-            raise ValueError(f"row {row}: {length} tokens, {self.longest} at most")
-        for block in range(-(-int(self.lens_h[row]) // self.page), -(-length // self.page)):
-            self.table_h[row, block] = self.free.pop()
-        self.lens_h[row] = length
+    def _grow(self, lengths: dict):
+        """Rows get the lengths {row: tokens} and pages for their positions, all of them or, where there are too few, none."""
+        for row, length in lengths.items():
+            if length > self.longest:
+                raise ValueError(f"row {row}: {length} tokens, {self.longest} at most")
+        blocks = {row: range(-(-int(self.lens_h[row]) // self.page), -(-length // self.page)) for row, length in lengths.items()}
+        need = sum(map(len, blocks.values()))
+        if need > len(self.free):
+            raise RuntimeError(f"{need} pages needed, {len(self.free)} of {self.n_pages} are free")
+        for row, new in blocks.items():
+            for block in new:
+                self.table_h[row, block] = self.free.pop()
+            self.lens_h[row] = lengths[row]
 
     def _tell_device(self):
         self.table.copy_(self.table_h, non_blocking=True)
@@ -111,7 +114,7 @@ class Server:
 
     def admit(self, row: int, n: int):
         """A request with a prompt of n tokens (at least five) takes an empty row; the layers' outputs."""
-        self._grow(row, n)
+        self._grow({row: n})
         self._tell_device()
         start = torch.zeros((1,), dtype=torch.int32, device="cuda")
         outs = []
@@ -130,7 +133,7 @@ class Server:
     def resume(self, row: int, n: int):
         """n more tokens of a row at once, after what its pages hold; the layers' outputs."""
         before = int(self.lens_h[row])
-        self._grow(row, before + n)
+        self._grow({row: before + n})
         self._tell_device()
         at = torch.tensor([before], dtype=torch.int32, device="cuda")
         outs = []
@@ -172,9 +175,7 @@ class Server:
 
     def step(self):
         """One token more for every row that holds a request; out[layer] [rows,H,128], zeros in the other rows."""
-        for row in range(self.rows):
-            if int(self.lens_h[row]) > 0:
-                self._grow(row, int(self.lens_h[row]) + 1)
+        self._grow({row: n + 1 for row, n in enumerate(self.lens_h.tolist()) if n > 0})
         self._tell_device()
         for l in range(self.L):
             self.source.token(l, self.q[l], self.k_new[l], self.v_new[l])
