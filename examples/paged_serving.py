@@ -195,7 +195,8 @@ def main():
     ap.add_argument("--eager", action="store_true", help="the step's calls one by one instead of a recorded graph")
     a = ap.parse_args()
 
-    n_pages = a.rows * -(-a.longest // a.page) * 3 // 4      # fewer than all rows at full length would take
+    blocks = -(-a.longest // a.page)
+    n_pages = max(a.rows * blocks * 3 // 4, blocks)          # fewer than all rows at full length would take, enough for one
     server = Server(Source(a.heads, a.seed), a.layers, a.heads, a.clusters, a.rows, a.longest, a.page, n_pages, a.cache, a.seed)
     if not a.eager:
         server.record()
@@ -230,7 +231,7 @@ def main():
         for row in alive:
             left[row] -= 1
     print(f"{served} of {a.requests} requests ended, {tokens} tokens of {a.layers} layers x {a.heads} heads in {a.clusters} clusters over {a.cache} "
-          f"pages: {1e3 * spent:.1f} ms in steps, {tokens / spent:.0f} tokens/s; at most {peak} of {n_pages} pages in use")
+          f"pages: {1e3 * spent:.1f} ms in steps, {tokens / spent if tokens else 0:.0f} tokens/s; at most {peak} of {n_pages} pages in use")
 
 
 if __name__ == "__main__":

@@ -1,6 +1,7 @@
-"""The serving example's account of pages, on the host: the calls on the GPU are left out (no GPU needed)."""
+"""The serving example's account of pages and requests, on the host: the calls on the GPU are left out (no GPU needed)."""
 import importlib.util
 import os
+import sys
 
 import pytest
 import torch
@@ -63,3 +64,21 @@ def test_a_pool_that_is_too_small_is_left_as_it_was():
     whole(server)
     assert server.lens_h.tolist() == [0, 41, 0]
 
+def run_main(monkeypatch, capsys, *args):
+    monkeypatch.setattr(S, "Server", HostServer)
+    monkeypatch.setattr(S, "Source", lambda heads, seed: None)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda: None)
+    monkeypatch.setattr(sys, "argv", ["paged_serving.py", "--eager", "--layers", "0", *args])
+    S.main()
+    return capsys.readouterr().out
+
+
+@pytest.mark.parametrize("rows,page,seed", [(1, 64, 1), (1, 64, 2), (1, 2048, 3), (2, 512, 1), (16, 64, 1)])
+def test_every_request_is_served(monkeypatch, capsys, rows, page, seed):
+    out = run_main(monkeypatch, capsys, "--rows", str(rows), "--page", str(page), "--seed", str(seed), "--requests", "12", "--steps", "20000")
+    assert "12 of 12 requests ended" in out
+
+
+def test_nothing_to_do(monkeypatch, capsys):
+    assert "0 of 0 requests ended, 0 tokens" in run_main(monkeypatch, capsys, "--requests", "0")
+    assert "0 of 48 requests ended, 0 tokens" in run_main(monkeypatch, capsys, "--steps", "0")
