@@ -16,3 +16,20 @@ PATHS = {
     "shares of many heads, dense": (180, 180, LONG, ROWS, ["paged_attend", "paged_join"]),
 }
 CACHES = ["f32", "bf16", "e4m3"]
+
+# heads, clusters: batches of more rows than lanes, one of them long (their lengths are added up in two levels)
+MANY_ROWS, LONGEST = [65, 130, 200, 300], 4200
+MANY_HEADS = [(3, 2), (3, 3)]
+
+
+def many_lengths(B):
+    """Rows without a position at either end, inside and over a lane's whole share of the rows, a long one behind them."""
+    lengths = [(37 * i + 11) % 90 for i in range(B)]
+    for i in [0, 1, 2, *range(B // 2, B // 2 + 9), B - 2, B - 1]:
+        lengths[i] = 0
+    lengths[B // 2 + 10] = LONGEST
+    return lengths
+
+
+# rows, heads, clusters, tokens of a call: rows moved by waves that are dealt units of more rows than lanes
+MOVED = [(70, 60, 12, 61), (130, 40, 40, 33)]
