@@ -555,7 +555,8 @@ int chai_project_qk_timed(const void *x, const void *w_q, const void *w_k, const
  *   Positions whose score is -inf weigh nothing, whatever their values hold.
  *   Rows without a position, and heads whose scores are all -inf, get 0.
  *   T_max (1 <= T_max <= max_blocks * page) bounds the rows' lengths; what the
- *   masked places hold (infinities, NaN) does not matter.
+ *   masked places hold (infinities, NaN) does not matter.  Work is dealt out by
+ *   T_max: far above the longest row (16 times and more) calls take longer.
  * chai_paged_decode_step: position seq_lens[b]-1 of every row (if seq_lens[b]
  *   is in [1,T_max]) is the token being decoded: its rows k_new, v_new [B,H,d]
  *   are written to the pages as by chai_paged_append_kv, then attention as

@@ -21,7 +21,7 @@ struct Quotient {
     unsigned int mul;
     int shift;
 };
-// 1 << shift waves take at least `least` units each of `streams` streams a row
+// 1 << shift waves take at least `least` units each of `streams` streams a row; both go by the bound of the lengths (make_paged_split)
 struct PagedSplit {
     int shift;
     unsigned int least;
@@ -78,8 +78,9 @@ __device__ __forceinline__ int row_len(const PagedShape &sh, int b) { return tak
 // ---------------------------------------------------------------------------------------------------------
 // How the work of a ragged batch is dealt out.  A unit is one batch of a wave's loads (16 rows of fp32, 32 of bf16, 64 of codes);
 // the units of all streams of all rows are laid end to end, (row, stream, unit), and worker w, one wave, takes the quota units from
-// w * quota on: every wave streams the same number of bytes whatever the lengths are, which only the device knows.  Each wave adds up
-// the rows' units for itself (64 rows per load and six steps of a scan).
+// w * quota on: waves that have work stream the same number of bytes whatever the lengths are, which only the device knows.  How many
+// have work goes by the bound as well: a share is at least 1 / 32 of a row at the bound (1 / 128 of its scores), so a bound far above the rows
+// leaves waves without any.  Each wave adds up the rows' units for itself (64 rows per load and six steps of a scan).
 // ---------------------------------------------------------------------------------------------------------
 template <int CTRL, int ROWS>
 __device__ __forceinline__ unsigned int add_from(unsigned int x)
@@ -677,8 +678,9 @@ __global__ __launch_bounds__(kRowWaves * 64, kRowWaves == 8 ? 2 : 3) void paged_
 
 // ---------------------------------------------------------------------------------------------------------
 // Attention in two passes, for layers with fewer clusters than heads whose rows are shared: the keys of a cluster are read once, not once per
-// member.  Both are bound by HBM: 4 x 32 heads in 4 clusters of 32768 bf16 tokens 24 us of scores (134 MB, 5.6 TB/s), 165 us of values (1.07 GB, 6.5
-// TB/s) and 5 us that join the parts; 64 x 32 of up to 4096 codes, most short, 12.6, 37 and 5 us (289 MB with the absent pages, 5.5 TB/s in all).
+// member.  Both are bound by HBM where rows are long: 4 x 32 heads in 4 clusters of 32768 bf16 tokens 24 us of scores (134 MB fetched, 5.5 TB/s), 165 us of
+// values (1.08 GB, 6.5 TB/s) and 5 us that join the parts.  64 x 32 of up to 4096 codes, most of them short and some pages absent, take 12.5, 37 and 5 us:
+// 248 MB fetched, 4.7 TB/s in all and 5.3 in the values; the scores (48 MB, 3.8 TB/s) are short stretches of many streams, bound by their look-ups.
 // Scores: a wave streams keys of its units, writes s[b][j][t] (-inf where nothing is to be attended to, whole units) and the maximum
 // and sum of exponentials of every stretch: `whole` of a stream that it took alone, else `parts` of the wave.
 // ---------------------------------------------------------------------------------------------------------
@@ -1229,7 +1231,7 @@ int unit_rows(int cache_dtype) { return cache_dtype == CHAI_F32 ? Tile<DT_F32>::
 
 }  // namespace
 
-// Waves of a launch; between 2048 and 6144 of them times differ by 3 % (one pass, which has keys and values in flight: 1024 to 4096).
+// Waves of a launch, a power of two: with 2048 times differ by 3 % (one pass, which has keys and values in flight: between 1024 and 4096).
 constexpr unsigned int kStreamWorkers = 4096, kAttendWorkers = 2048, kPagedWorkers = 4096;
 // Most waves of one stream: of dense attention and of values, whose parts are joined (1 x 52 dense heads of 8192 bf16 tokens 42.2 us, 43.5
 // with 64; 1 x 32 of 2048 15.5, 16.6 with 16), and of scores, of whose parts only two numbers are read again (4 x 4 streams of 32768 bf16
@@ -1238,21 +1240,15 @@ constexpr unsigned int kPagedParts = 32, kScoreParts = 128;
 // The parts of a head are joined by four waves, those of many heads by one each (64 x 32 heads 69.1 / 67.6 us in all, 1 x 52 25.7 / 27.7).
 constexpr long long kJoinedByOne = 512;
 
-// Whether a workgroup takes a whole head's row (one launch) or shares of all rows' units go to independent waves (two or three).  Rows /
-// shares, in us, the new token's rows written too, bf16 unless said; "to T": lengths spread evenly up to T, "few long": as their fourth power,
-// else all T:
-// * few heads, a CU's rate bounds a row: 1 x 32 in 8 of 577 tokens 9.7 / 15.9, 1024 13.5 / 15.9, 1400 16.0 / 15.8, 2048 21.6 / 15.6, of 2048 codes
-//   17.3 / 17.1, 4000 26.2 / 18.0; 1 x 52 dense of 1400 17.2 / 15.7, 2048 23.3 / 16.8; 2 x 32 of 2048 22.3 / 18.3, 4 x 32 24.1 / 24.5, to 2048
-//   22.9 / 20.0;
-// * clustered: 4 x 72 in 16 of 577 18.0 / 21.5, to 1400 21.4 / 24.8, to 2048 28.1 / 29.8, 2048 46.7 / 39.5 (two workgroups on some CUs, one on most),
-//   to 2048 codes 22.3 / 22.9; 8 x 32 in 8 of 2048 32.4 / 36.6; 16 x 32: of 577 21.3 / 28.2, 1024 32.0 / 37.2, to 2048 34.1 / 41.1, 2048 57.4 / 62.2, few
-//   long 26.1 / 24.3, to 4000 codes 38.6 / 43.7, few long to 4096 35.1 / 26.8, to 1000 fp32 33.2 / 40.9; 32 x 32: to 1024 37.2 / 40.6, 1024 58.2 / 60.6,
-//   to 2048 62.4 / 65.8, 2048 111.7 / 111.1, few long 32.5 / 35.8; beyond: 64 x 32 to 1024 codes 47.1 / 45.6, bf16 67.0 / 67.2, 1024 110.7 / 111.2, few
-//   long to 2048 codes 49.2 / 40.2;
-// * dense: 8 x 52 to 1777 35.9 / 38.2, 2048 68.1 / 72.9, 4 x 72 to 577 13.4 / 19.1, to 2048 33.5 / 36.9, 2048 60.0 / 52.6, 16 x 32 to 2048 46.0 /
-//   51.0, few long 28.6 / 31.8.
-// The rule goes by the longest row, the others' lengths are not known here; the longer it may be, the more a lone long row costs (with rows of 1 MB
-// 16 x 32, few long to 4096, 45.2 / 36.3).
+// Whether a workgroup takes a whole head's row (one launch) or shares of all rows' units go to independent waves (two or three).  The rule goes by
+// the longest row, the others' lengths are not known here.  Rows / shares around its limits, in us, the new token's rows written too, bf16 unless
+// said, rows of the stated tokens unless spread evenly "to" them:
+// * few heads, whose rows a CU's rate bounds: 1 x 32 in 8 clusters of 1024 13.5 / 15.9, 1400 16.0 / 15.8, 2048 21.6 / 15.6; 4 x 32 of 2048 24.1 / 24.5;
+// * more heads: 4 x 72 in 16 to 2048 28.1 / 29.8; 16 x 32 in 8 to 2048 34.1 / 41.1, 2048 57.4 / 62.2, to 4000 codes 38.6 / 43.7; 32 x 32 of 2048 111.7 / 111.1;
+//   dense 8 x 52 of 2048 68.1 / 72.9, 16 x 32 to 2048 46.0 / 51.0;
+// * clustered, beyond 1024: 64 x 32 to 1024 codes 47.1 / 45.6, bf16 67.0 / 67.2.
+// It loses where few rows are long, the more so the longer they may be (lengths as the fourth power: 16 x 32 to 2048 26.1 / 24.3, to 4096 codes
+// 35.1 / 26.8, with rows of 1 MB 45.2 / 36.3), and where most CUs have one workgroup of long rows and some two (4 x 72 of 2048 46.7 / 39.5, dense 60.0 / 52.6).
 static bool take_rows(int B, int H, int T_max, int cache, bool dense)
 {
     const long long heads = (long long)B * H, bytes = (long long)T_max * kHeadDim * (cache == CHAI_F32 ? 4 : (cache == CHAI_BF16 ? 2 : 1));
