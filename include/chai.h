@@ -586,6 +586,135 @@ int chai_paged_decode_step(const void *q, const void *k_new, const void *v_new, 
                            int n_pages, int page, int max_blocks, int d, int dtype, int cache_dtype, float scale,
                            float *out, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Places of new tokens: block tables and slot maps made on the device from
+ * the rows' lengths, for batches whose new tokens stand one row's behind the
+ * other's (a row that decodes has one, a prompt many).  Free pages are kept
+ * as a stack on the device; nothing comes to the host, so a recorded step can
+ * be replayed while rows grow.
+ *
+ * chai_paged_place_tokens: row b has len = seq_lens[b] positions and is to get
+ * count = counts[b] more.  Rows take the pages they need, ceil((len + count) /
+ * page) - ceil(len / page) of them, from the top of the list, in row order, a
+ * row all it needs or nothing: it gets its tokens (granted[b] = 1) if they end
+ * within the block of N tokens and within its table (and 2^31 - 1), and if it
+ * needs no page or the pages that rows 0 .. b need (those that end within
+ * both) are there: the first row that there are too few for keeps all rows
+ * behind it that need any from getting them.
+ *     counts      [B] int32  (below 0: none)
+ *     seq_lens    [B] int32  (below 0: none)
+ *     block_table [B,max_blocks] int32: entries of new pages are written
+ *     free_pages  [n_pages] int32, the first n_free[0] of them the list, not
+ *                 changed; n_free [1] int32 (taken into [0,n_pages])
+ *   written, all int32:
+ *     new_lens    [B]    len + count of rows that got their tokens, len of the
+ *                        others (may be seq_lens itself)
+ *     n_left      [1]    free pages that are left (may be n_free itself)
+ *     granted     [B]    1, or 0 for rows that got nothing
+ *     offsets     [B+1]  number of a row's first token in the block, and the
+ *                        number of all; cut to N
+ *     token_rows  [N]    row of every token, -1 behind the last one
+ *     positions   [N]    its position, 0 behind the last one
+ *     slots       [N]    page * (its page) + its place there, -1 without one
+ *                        (rows that got nothing, absent pages, behind the last)
+ *   Rows that got nothing have their tokens' numbers in the block all the
+ *   same.  The other arrays must not overlap.
+ * chai_paged_release_pages: rows keep keep[b] of their seq_lens[b] positions
+ *   (none below 0; all beyond); pages behind those go back on the list, rows
+ *   in order, a row's in order, and their entries become -1.  Entries that are
+ *   no pages are left out; pages must not stand in other rows too.
+ *     free_pages, block_table  changed;  new_lens [B], n_left [1] written (may
+ *     be seq_lens, n_free)
+ * workspace: chai_paged_place_workspace_bytes(B) (0 on invalid sizes; never
+ *   decreases), 256-byte aligned, contents need not be initialised.
+ * B = 0: no tokens (token_rows, positions, slots, n_left and offsets are not
+ * written).  B <= 4096, N <= 2^24, n_pages * page < 2^31, page a multiple of 8.
+ */
+size_t chai_paged_place_workspace_bytes(int B);
+int chai_paged_place_tokens(const int32_t *counts, const int32_t *seq_lens, int32_t *block_table, const int32_t *free_pages,
+                            const int32_t *n_free, int B, int N, int n_pages, int page, int max_blocks, int32_t *new_lens,
+                            int32_t *n_left, int32_t *granted, int32_t *offsets, int32_t *token_rows, int32_t *positions,
+                            int32_t *slots, void *workspace, size_t workspace_bytes, void *stream);
+int chai_paged_release_pages(const int32_t *keep, const int32_t *seq_lens, int32_t *block_table, int32_t *free_pages,
+                             const int32_t *n_free, int B, int n_pages, int page, int max_blocks, int32_t *new_lens,
+                             int32_t *n_left, void *stream);
+
+/*
+ * Rotary positions (Section 4 evaluates models that turn queries and keys by
+ * their positions before the scores are taken).  The first `rot` elements of
+ * a row are rot / 2 pairs; pair i of a token at position p is turned by the
+ * angle p * freq[i]:
+ *     (a, b) -> gain * (a cos - b sin, a sin + b cos)
+ *     layout CHAI_ROPE_HALVES: elements i and i + rot / 2
+ *            CHAI_ROPE_PAIRS:  elements 2 i and 2 i + 1
+ * Elements from rot on stay as they are.  Angles, turns and products are in
+ * 64 bits, rounded once to fp32 and from there to the stored type.  rot is a
+ * multiple of 16 up to d; freq [rot/2] is on the device, in 64 bits, radians
+ * per position (at most pi); a negative position turns back.
+ *
+ * chai_rotary_frequencies (HOST pointers, no GPU work): n_i = theta^(-2i/rot),
+ *   CHAI_ROPE_PLAIN   n_i
+ *   CHAI_ROPE_LINEAR  n_i / factor: positions divided by it
+ *   CHAI_ROPE_BASE    the same with theta * factor^(rot/(rot-2)) for theta:
+ *                     the slowest pair is divided, the fastest stays
+ *   CHAI_ROPE_TURNS   pairs by the turns they make over original_length
+ *                     positions (arXiv 2309.00071): up to `slow` of them
+ *                     divided by the factor, from `fast` on kept, the mean of
+ *                     both in proportion between
+ *   (factor > 0 except for PLAIN; original_length > 0 and slow < fast for
+ *   TURNS; rot > 2 for BASE; others ignored)
+ *
+ * chai_rotate_qk: a block of Tn tokens of every row.  Position of token i of
+ *   row b: positions[b][i] ([B,Tn] int32), or pos0 + i where that is NULL.
+ *     q      element (b,h,i,c) at (b*H+h)*q_head_stride + i*d + c
+ *     q_out  [B,H,Tn,d], rows of representatives written; may be q itself
+ *            (q_head_stride = Tn*d)
+ *     k      element (b,j,i,c) at (b*k+j)*k_head_stride + i*d + c: compact keys
+ *     k_out  [B,k,Tc_cap,d], rows pos0 .. pos0+Tn-1 of used slots written; k
+ *            may be those rows themselves (k_head_stride = Tc_cap*d)
+ *     (strides in elements, >= Tn*d, multiples of 8; inputs and outputs are
+ *     the same rows or do not overlap.)  q and q_out, or k and k_out, may both
+ *     be NULL.  rep_heads NULL: every head (k = H).  chai_project_qk leaves
+ *   queries and keys in these layouts.  B * Tn < 2^31.
+ */
+enum { CHAI_ROPE_HALVES = 0, CHAI_ROPE_PAIRS = 1 };
+enum { CHAI_ROPE_PLAIN = 0, CHAI_ROPE_LINEAR = 1, CHAI_ROPE_BASE = 2, CHAI_ROPE_TURNS = 3 };
+int chai_rotary_frequencies(int rot, double theta, int kind, double factor, double original_length, double slow, double fast,
+                            double *freq);
+int chai_rotate_qk(const void *q, const void *k, int64_t q_head_stride, int64_t k_head_stride, const int32_t *rep_heads,
+                   const int32_t *positions, const double *freq, int B, int H, int k_slots, int Tn, int pos0, int Tc_cap, int d,
+                   int rot, int layout, int dtype, float gain, void *q_out, void *k_out, void *stream);
+
+/*
+ * chai_paged_append_packed: N tokens one behind the other, of any rows, into
+ * pages; queries and keys are turned on the way, as by chai_rotate_qk (rot = 0:
+ * as they are; freq and positions are not read then).
+ *     q      element (n,h,c) at n*q_token_stride + h*d + c
+ *     k_new  element (n,h,c) at n*k_token_stride + h*d + c, or, k_by_slot set,
+ *            (n,j,c): keys of the representatives alone
+ *     v_new  element (n,h,c) at n*v_token_stride + h*d + c
+ *     (strides in elements, multiples of 8: parts of one row of a layer's
+ *     projections are read in place)
+ *     rep_heads  [B,k], or NULL: every head (k = H)
+ *     token_rows, positions, slots  [N] int32, as chai_paged_place_tokens
+ *            gives them: nothing of a token is read or written whose row is
+ *            outside [0,B), nor pages where its slot is outside
+ *            [0,n_pages*page).  Two tokens must not be given the same slot.
+ *     q_out  [N,H,d]: representatives' rows written; may be q itself
+ *            (q_token_stride = H*d).  q and q_out may both be NULL.
+ *   pages, scales, types as chai_paged_append_kv; 8-bit codes are those of the
+ *   turned rows of 32 bits.  With one token per row q_out is what
+ *   chai_paged_decode_attention takes.
+ * N = 0 is a no-op.  Limits as for the other calls on pages, n_pages * page <
+ * 2^31 besides; N <= 2^24, N * (H + 2k) < 2^34.
+ */
+int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new, int64_t q_token_stride,
+                             int64_t k_token_stride, int64_t v_token_stride, int k_by_slot, const int32_t *rep_heads,
+                             const int32_t *token_rows, const int32_t *positions, const int32_t *slots, const double *freq,
+                             void *q_out, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int N, int B, int H,
+                             int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype, float gain,
+                             void *stream);
+
 #ifdef __cplusplus
 }
 #endif

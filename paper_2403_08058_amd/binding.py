@@ -20,6 +20,8 @@ LIB_PATH = os.path.join(_HERE, "libchai.so")
 
 CHAI_OK = 0
 CHAI_F32, CHAI_BF16, CHAI_E4M3 = 0, 1, 2
+CHAI_ROPE_HALVES, CHAI_ROPE_PAIRS = 0, 1
+CHAI_ROPE_PLAIN, CHAI_ROPE_LINEAR, CHAI_ROPE_BASE, CHAI_ROPE_TURNS = 0, 1, 2, 3
 STATUS_NAMES = {0: "CHAI_OK", 1: "CHAI_ERR_NULL", 2: "CHAI_ERR_SHAPE", 3: "CHAI_ERR_DTYPE", 4: "CHAI_ERR_WORKSPACE",
                 5: "CHAI_ERR_UNSUPPORTED", 6: "CHAI_ERR_HIP", 7: "CHAI_ERR_ALIGN", 8: "CHAI_ERR_STATIC_LIMIT"}
 CHAI_STATIC_SCRATCH_BYTES = 32 << 20
@@ -34,7 +36,8 @@ EXPORTS = ["chai_version", "chai_status_string", "chai_score_features", "chai_as
            "chai_dense_decode_attention", "chai_prefill_workspace_bytes", "chai_prefill_attention",
            "chai_prefill_attention_timed", "chai_dense_prefill_attention", "chai_project_qk", "chai_project_qk_timed", "chai_stream_read_probe", "chai_mfma_rate_probe",
            "chai_paged_workspace_bytes", "chai_paged_append_kv", "chai_paged_gather_kv", "chai_paged_decode_attention",
-           "chai_paged_decode_step"]
+           "chai_paged_decode_step", "chai_paged_place_workspace_bytes", "chai_paged_place_tokens", "chai_paged_release_pages",
+           "chai_rotary_frequencies", "chai_rotate_qk", "chai_paged_append_packed"]
 
 
 class ChaiError(RuntimeError):
@@ -93,8 +96,16 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.chai_paged_gather_kv.argtypes = [vp] * 9 + [ci] * 10 + [vp]
     L.chai_paged_decode_attention.argtypes = [vp] * 9 + [ci] * 10 + [cf, vp, vp, sz, vp]
     L.chai_paged_decode_step.argtypes = [vp] * 11 + [ci] * 10 + [cf, vp, vp, sz, vp]
+    L.chai_paged_place_workspace_bytes.restype = sz
+    L.chai_paged_place_workspace_bytes.argtypes = [ci]
+    L.chai_paged_place_tokens.argtypes = [vp] * 5 + [ci] * 5 + [vp] * 8 + [sz, vp]
+    L.chai_paged_release_pages.argtypes = [vp] * 5 + [ci] * 4 + [vp] * 3
+    cd = ctypes.c_double
+    L.chai_rotary_frequencies.argtypes = [ci, cd, ci, cd, cd, cd, cd, vp]
+    L.chai_rotate_qk.argtypes = [vp, vp, i64, i64, vp, vp, vp] + [ci] * 10 + [cf, vp, vp, vp]
+    L.chai_paged_append_packed.argtypes = [vp] * 3 + [i64] * 3 + [ci] + [vp] * 10 + [ci] * 11 + [cf, vp]
     for fn in EXPORTS:
-        if fn not in ("chai_paged_workspace_bytes", "chai_status_string", "chai_decode_workspace_bytes", "chai_prefill_workspace_bytes",
+        if fn not in ("chai_paged_workspace_bytes", "chai_paged_place_workspace_bytes", "chai_status_string", "chai_decode_workspace_bytes", "chai_prefill_workspace_bytes",
                       "chai_decode_q8_workspace_bytes"):
             getattr(L, fn).restype = ci
     return L
@@ -500,6 +511,7 @@ def alloc_workspace(B: int, H: int, k: int, T: int, d: int, dtype: int, device="
 
 
 _I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
+_MOST_ROWS = 4096                      # rows of a call on pages
 # (type of q and new rows, type of the pages) -> their codes
 _PAGED_CODES = {(torch.float32, torch.float32): (CHAI_F32, CHAI_F32), (torch.bfloat16, torch.bfloat16): (CHAI_BF16, CHAI_BF16),
                 (torch.float32, torch.uint8): (CHAI_F32, CHAI_E4M3), (torch.bfloat16, torch.uint8): (CHAI_BF16, CHAI_E4M3)}
@@ -616,6 +628,155 @@ def chai_paged_decode_step(q, k_new, v_new, k_pages, v_pages, head_to_cluster, r
     """Cache growth + attention in one call: position seq_lens[b]-1 of every row is taken from k_new / v_new [B,H,d]."""
     return _paged_decode("chai_paged_decode_step", _lib.chai_paged_decode_step, q, (k_new, v_new), k_pages, v_pages, k_scales, v_scales,
                          head_to_cluster, rep_heads, block_table, seq_lens, T_max, scale, out, workspace, stream)
+
+
+def chai_paged_place_workspace_bytes(B: int) -> int:
+    return int(_lib.chai_paged_place_workspace_bytes(B))
+
+
+def alloc_paged_place_workspace(B: int, device="cuda") -> torch.Tensor:
+    """Device scratch of chai_paged_place_tokens; one of the most rows serves fewer."""
+    return torch.empty((max(chai_paged_place_workspace_bytes(B), 256),), dtype=torch.uint8, device=device)
+
+
+def chai_paged_place_tokens(counts, seq_lens, block_table, free_pages, n_free, page: int, new_lens, n_left, granted, offsets,
+                            token_rows, positions, slots, workspace, stream=None):
+    """Pages and places for counts[b] new tokens of every row behind its seq_lens[b] (all [B]): block_table [B,max_blocks] gets pages
+    from the top of free_pages [n_pages], n_free [1] of them; new_lens [B], n_left [1] (may be seq_lens and n_free), granted [B],
+    offsets [B+1] and the tokens' token_rows, positions, slots [N] are written.  All int32."""
+    fn = "chai_paged_place_tokens"
+    B, max_blocks = block_table.shape
+    N, n_pages = slots.shape[0], free_pages.shape[0]
+    for t, shape in ((counts, (B,)), (seq_lens, (B,)), (block_table, (B, max_blocks)), (free_pages, (n_pages,)), (n_free, (1,)),
+                     (new_lens, (B,)), (n_left, (1,)), (granted, (B,)), (offsets, (B + 1,)), (token_rows, (N,)), (positions, (N,)),
+                     (slots, (N,))):
+        if t.dtype is not _I32 or t.shape != shape:
+            _misfit(fn, f"int32 of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
+    p = _ptrs((counts, seq_lens, block_table, free_pages, n_free, new_lens, n_left, granted, offsets, token_rows, positions, slots,
+               workspace))
+    _check(fn, _lib.chai_paged_place_tokens(*p[:5], B, N, n_pages, page, max_blocks, *p[5:], workspace.nbytes, _stream(stream)))
+
+
+def chai_paged_release_pages(keep, seq_lens, block_table, free_pages, n_free, page: int, new_lens, n_left, stream=None):
+    """Rows keep keep[b] of their seq_lens[b] positions; the pages behind those go back on the list.  All int32."""
+    fn = "chai_paged_release_pages"
+    B, max_blocks = block_table.shape
+    n_pages = free_pages.shape[0]
+    for t, shape in ((keep, (B,)), (seq_lens, (B,)), (block_table, (B, max_blocks)), (free_pages, (n_pages,)), (n_free, (1,)),
+                     (new_lens, (B,)), (n_left, (1,))):
+        if t.dtype is not _I32 or t.shape != shape:
+            _misfit(fn, f"int32 of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
+    p = _ptrs((keep, seq_lens, block_table, free_pages, n_free, new_lens, n_left))
+    _check(fn, _lib.chai_paged_release_pages(*p[:5], B, n_pages, page, max_blocks, *p[5:], _stream(stream)))
+
+
+def chai_rotary_frequencies(rot: int, theta: float = 10000.0, kind: int = CHAI_ROPE_PLAIN, factor: float = 1.0,
+                            original_length: float = 0.0, slow: float = 1.0, fast: float = 32.0) -> torch.Tensor:
+    """Radians per position of the rot / 2 pairs: a host tensor in 64 bits (the calls that turn rows take it on the device)."""
+    freq = torch.empty((max(rot // 2, 0),), dtype=torch.float64)
+    _check("chai_rotary_frequencies", _lib.chai_rotary_frequencies(rot, theta, kind, factor, original_length, slow, fast,
+                                                                   freq.data_ptr() if freq.numel() else None))
+    return freq
+
+
+def _streams_of(fn, name, t):
+    """Address and stride from head to head of t [B,heads,n,d] whose rows lie one behind the other: a dense tensor, or the same
+    positions of every head of one."""
+    B, heads, n, d = t.shape
+    sb, sh, sn, sd = t.stride()
+    if not t.is_cuda:
+        raise ValueError("libchai takes device tensors")
+    if B * heads * n == 0:
+        return t.data_ptr(), n * d
+    if heads == 1:
+        sh = sb if B > 1 else n * d
+    if sd != 1 or (n > 1 and sn != d) or (B > 1 and sb != heads * sh):
+        _misfit(fn, f"{name} {tuple(t.shape)} with strides {t.stride()}: rows of a head must lie one behind the other, heads equally far apart")
+    return t.data_ptr(), sh
+
+
+def _freq_of(fn, freq):
+    if freq is None:
+        return None, 0
+    if freq.dtype is not torch.float64 or freq.dim() != 1:
+        _misfit(fn, f"frequencies in 64 bits expected, got {freq.dtype} {tuple(freq.shape)}")
+    return _ptr(freq), 2 * freq.shape[0]
+
+
+def chai_rotate_qk(q, k, rep_heads, freq, q_out, k_out, pos0: int, positions=None, layout: int = CHAI_ROPE_HALVES, gain: float = 1.0,
+                   stream=None):
+    """Queries q [B,H,Tn,d] of the representatives -> their rows of q_out (may be q), compact keys k [B,k,Tn,d] -> rows pos0.. of
+    k_out [B,k,Tc_cap,d] (k may be a view of those), turned by positions [B,Tn] int32 (None: pos0 on) times freq [rot/2] (64 bits).
+    q and q_out, or k and k_out, may both be None; rep_heads [B,k], or None for every head (k = H)."""
+    fn = "chai_rotate_qk"
+    some = q if q is not None else k
+    if some is None or (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        _misfit(fn, "queries or keys, or both, with what they are written to")
+    B, heads, Tn, d = some.shape
+    dtype = some.dtype
+    code = dtype_code(some)
+    slots = k.shape[1] if k is not None else rep_heads.shape[1] if rep_heads is not None else heads
+    H = q.shape[1] if q is not None else slots      # (of keys alone: heads are not looked at beyond whether a slot has one)
+    if q is not None and (q.shape != (B, H, Tn, d) or q_out.shape != q.shape or q_out.dtype is not dtype or q.dtype is not dtype):
+        _misfit(fn, f"q {tuple(q.shape)} {q.dtype} and q_out {tuple(q_out.shape)} {q_out.dtype} do not fit together")
+    Tc_cap = k_out.shape[2] if k is not None else pos0 + Tn
+    if k is not None and (k.shape != (B, slots, Tn, d) or k.dtype is not dtype or k_out.shape != (B, slots, Tc_cap, d)
+                          or k_out.dtype is not dtype):
+        _misfit(fn, f"k {tuple(k.shape)} {k.dtype} and k_out {tuple(k_out.shape)} {k_out.dtype} do not fit together")
+    if (rep_heads is not None and (rep_heads.dtype is not _I32 or rep_heads.shape != (B, slots))) \
+            or (positions is not None and (positions.dtype is not _I32 or positions.shape != (B, Tn))):
+        _misfit(fn, "int32 maps and positions for every row expected")
+    qp, qs = _streams_of(fn, "q", q) if q is not None else (None, 0)
+    kp, ks = _streams_of(fn, "k", k) if k is not None else (None, 0)
+    fp, rot = _freq_of(fn, freq)
+    _check(fn, _lib.chai_rotate_qk(qp, kp, qs, ks, _ptr(rep_heads), _ptr(positions), fp, B, H, slots, Tn, pos0, Tc_cap, d, rot, layout,
+                                   code, gain, _ptr(q_out), _ptr(k_out), _stream(stream)))
+    return q_out, k_out
+
+
+def _tokens_of(fn, name, t, heads, d):
+    """Address and stride from token to token of t [N,heads,d], a dense tensor or a part of wider rows."""
+    N = t.shape[0]
+    if t.shape != (N, heads, d):
+        _misfit(fn, f"{name} {tuple(t.shape)}: [tokens,{heads},{d}] expected")
+    if not t.is_cuda:
+        raise ValueError("libchai takes device tensors")
+    sn, sh, sd = t.stride()
+    if N and (sd != 1 or (heads > 1 and sh != d)):
+        _misfit(fn, f"{name} with strides {t.stride()}: heads of a token must lie one behind the other")
+    return t.data_ptr(), sn if N > 1 else heads * d
+
+
+def chai_paged_append_packed(q, k_new, v_new, rep_heads, token_rows, positions, slots, freq, q_out, k_pages, v_pages, k_scales=None,
+                             v_scales=None, layout: int = CHAI_ROPE_HALVES, gain: float = 1.0, k_by_slot: Optional[bool] = None,
+                             stream=None):
+    """N tokens one behind the other: keys k_new [N,H,d] (or [N,k,d], k_by_slot: the representatives' alone; None: by the shape) and
+    values v_new [N,H,d] into their slots of the pages, queries q [N,H,d] of the representatives -> q_out [N,H,d] (may be q; both
+    may be None).  Queries and keys are turned by positions times freq [rot/2] (64 bits; None: as they are).  token_rows, positions,
+    slots [N] int32 as chai_paged_place_tokens gives them; rep_heads [B,k], or None for every head (k = H)."""
+    fn = "chai_paged_append_packed"
+    n_pages, k, page, d = k_pages.shape
+    N, H, _ = v_new.shape
+    dtype = k_new.dtype
+    code, pages = _paged_types(fn, dtype, k_pages, v_pages, k_scales, v_scales, n_pages, H, k, page, d)
+    if k_by_slot is None:
+        k_by_slot = k_new.shape[1] != H
+    if v_new.dtype is not dtype or (q is None) != (q_out is None) or (q is not None and (q.dtype is not dtype or q_out.dtype is not dtype
+                                                                                         or q_out.shape != (N, H, d))):
+        _misfit(fn, "queries, keys and values of one type, and q_out [N,H,d] beside q, expected")
+    if (rep_heads is not None and (rep_heads.dtype is not _I32 or rep_heads.shape[1:] != (k,))) or k_new.shape[0] != N \
+            or any(t is not None and (t.dtype is not _I32 or t.shape != (N,)) for t in (token_rows, positions, slots)):
+        _misfit(fn, "int32 maps for every row, and rows, positions and slots for every token, expected")
+    B = rep_heads.shape[0] if rep_heads is not None else _MOST_ROWS      # (without maps a row is only a number that is not below 0)
+    qp, qs = _tokens_of(fn, "q", q, H, d) if q is not None else (None, 0)
+    kp, ks = _tokens_of(fn, "k_new", k_new, k if k_by_slot else H, d)
+    vp, vs = _tokens_of(fn, "v_new", v_new, H, d)
+    fp, rot = _freq_of(fn, freq)
+    p = _ptrs((rep_heads, token_rows, positions, slots))
+    o = _ptrs((q_out, k_pages, v_pages, k_scales, v_scales))
+    _check(fn, _lib.chai_paged_append_packed(qp, kp, vp, qs, ks, vs, int(k_by_slot), *p, fp, *o, N, B, H, k, n_pages, page, d, rot, layout,
+                                             code, pages, gain, _stream(stream)))
+    return q_out
 
 
 class _Binding(types.ModuleType):

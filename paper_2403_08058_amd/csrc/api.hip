@@ -2,6 +2,7 @@
 // allocates, synchronises or reads device memory.
 #include "chai_internal.h"
 
+#include <cmath>
 #include <mutex>
 
 using namespace chai;
@@ -685,6 +686,197 @@ int chai_paged_decode_step(const void *q, const void *k_new, const void *v_new, 
     if (B == 0) return CHAI_OK;
     return hip_status(launch_paged_attention(sh, pg, q, k_new, v_new, dtype, cache_dtype, head_to_cluster, rep_heads, scale, out,
                                              workspace, plan, static_cast<hipStream_t>(stream)));
+}
+
+static bool check_place(int B, int n_pages, int page, int max_blocks, int *st, PlaceShape *sh)
+{
+    *st = CHAI_OK;
+    if (B < 0 || n_pages < 1 || page < 8 || page % 8 != 0 || max_blocks < 1) *st = CHAI_ERR_SHAPE;
+    else if (B > kMaxPagedBatch || page > kMaxPagedTokens || (long long)n_pages * page > 0x7fffffffll) *st = CHAI_ERR_UNSUPPORTED;
+    if (*st != CHAI_OK) return false;
+    PagedShape div;
+    div.page = page;
+    set_page_division(&div);
+    sh->B = B;
+    sh->n_pages = n_pages;
+    sh->page = page;
+    sh->max_blocks = max_blocks;
+    sh->div_mul = div.div_mul;
+    sh->div_shift = div.div_shift;
+    return true;
+}
+
+size_t chai_paged_place_workspace_bytes(int B)
+{
+    if (B < 0 || B > kMaxPagedBatch) return 0;
+    return B == 0 ? 256 : place_workspace_bytes(B);
+}
+
+int chai_paged_place_tokens(const int32_t *counts, const int32_t *seq_lens, int32_t *block_table, const int32_t *free_pages,
+                            const int32_t *n_free, int B, int N, int n_pages, int page, int max_blocks, int32_t *new_lens,
+                            int32_t *n_left, int32_t *granted, int32_t *offsets, int32_t *token_rows, int32_t *positions,
+                            int32_t *slots, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (B != 0 && (!counts || !seq_lens || !block_table || !free_pages || !n_free || !new_lens || !n_left || !granted || !offsets ||
+                   (N != 0 && (!token_rows || !positions || !slots))))
+        return CHAI_ERR_NULL;
+    if (N < 0) return CHAI_ERR_SHAPE;
+    PlaceShape sh;
+    int st;
+    if (!check_place(B, n_pages, page, max_blocks, &st, &sh)) return st;
+    if (N > kMaxPagedTokens) return CHAI_ERR_UNSUPPORTED;
+    sh.N = N;
+    if (B > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < place_workspace_bytes(B)))
+        return CHAI_ERR_WORKSPACE;
+    if (B == 0) return CHAI_OK;
+    const PlaceIn in{counts, seq_lens, free_pages, n_free};
+    const PlaceOut out{block_table, new_lens, n_left, granted, offsets, token_rows, positions, slots};
+    return hip_status(launch_place_tokens(sh, in, out, workspace, static_cast<hipStream_t>(stream)));
+}
+
+int chai_paged_release_pages(const int32_t *keep, const int32_t *seq_lens, int32_t *block_table, int32_t *free_pages,
+                             const int32_t *n_free, int B, int n_pages, int page, int max_blocks, int32_t *new_lens,
+                             int32_t *n_left, void *stream)
+{
+    if (B != 0 && (!keep || !seq_lens || !block_table || !free_pages || !n_free || !new_lens || !n_left)) return CHAI_ERR_NULL;
+    PlaceShape sh;
+    int st;
+    if (!check_place(B, n_pages, page, max_blocks, &st, &sh)) return st;
+    if (B == 0) return CHAI_OK;
+    return hip_status(launch_release_pages(sh, keep, seq_lens, block_table, free_pages, n_free, new_lens, n_left,
+                                           static_cast<hipStream_t>(stream)));
+}
+
+int chai_rotary_frequencies(int rot, double theta, int kind, double factor, double original_length, double slow, double fast,
+                            double *freq)
+{
+    if (!freq) return CHAI_ERR_NULL;
+    if (rot < 2 || rot % 2 != 0 || rot > kHeadDim || kind < CHAI_ROPE_PLAIN || kind > CHAI_ROPE_TURNS || !(theta > 0.0) || !std::isfinite(theta))
+        return CHAI_ERR_SHAPE;
+    if (kind != CHAI_ROPE_PLAIN && (!(factor > 0.0) || !std::isfinite(factor))) return CHAI_ERR_SHAPE;
+    if (kind == CHAI_ROPE_BASE && rot == 2) return CHAI_ERR_SHAPE;
+    if (kind == CHAI_ROPE_TURNS && (!(original_length > 0.0) || !(slow < fast) || !std::isfinite(original_length) || !std::isfinite(slow) || !std::isfinite(fast)))
+        return CHAI_ERR_SHAPE;
+    const double base = kind == CHAI_ROPE_BASE ? theta * std::pow(factor, (double)rot / (rot - 2)) : theta;
+    for (int i = 0; i < rot / 2; ++i) {
+        const double n = std::pow(base, -2.0 * i / rot);
+        if (kind == CHAI_ROPE_LINEAR) {
+            freq[i] = n / factor;
+        } else if (kind == CHAI_ROPE_TURNS) {
+            const double turns = original_length * n / 6.283185307179586476925, at = (turns - slow) / (fast - slow);
+            const double kept = at < 0.0 ? 0.0 : at > 1.0 ? 1.0 : at;
+            freq[i] = kept * n + (1.0 - kept) * n / factor;
+        } else {
+            freq[i] = n;
+        }
+    }
+    return CHAI_OK;
+}
+
+// What is common to rows that are turned.
+static int check_turn(int rot, int layout, int dtype, int d, const void *freq)
+{
+    if (bad_dtype(dtype)) return CHAI_ERR_DTYPE;
+    if (rot < 0 || d < 1 || rot > d || (layout != CHAI_ROPE_HALVES && layout != CHAI_ROPE_PAIRS)) return CHAI_ERR_SHAPE;
+    if (d != kHeadDim || rot % 16 != 0) return CHAI_ERR_UNSUPPORTED;
+    if (rot != 0 && !freq) return CHAI_ERR_NULL;
+    return (reinterpret_cast<uintptr_t>(freq) & 7u) != 0 ? CHAI_ERR_ALIGN : CHAI_OK;
+}
+
+int chai_rotate_qk(const void *q, const void *k, int64_t q_head_stride, int64_t k_head_stride, const int32_t *rep_heads,
+                   const int32_t *positions, const double *freq, int B, int H, int k_slots, int Tn, int pos0, int Tc_cap, int d,
+                   int rot, int layout, int dtype, float gain, void *q_out, void *k_out, void *stream)
+{
+    if (B != 0 && Tn != 0 && ((!q != !q_out) || (!k != !k_out) || (!q && !k))) return CHAI_ERR_NULL;
+    const int st = check_turn(rot, layout, dtype, d, freq);
+    if (st != CHAI_OK) return st;
+    if (B < 0 || H < 1 || k_slots < 1 || k_slots > H || (!rep_heads && k_slots != H && B != 0) || Tn < 0 || rot < 1) return CHAI_ERR_SHAPE;
+    if (q && (q_head_stride < (int64_t)Tn * d || (q_head_stride & 7))) return CHAI_ERR_SHAPE;
+    if (k && (pos0 < 0 || (long long)pos0 + Tn > Tc_cap || k_head_stride < (int64_t)Tn * d || (k_head_stride & 7))) return CHAI_ERR_SHAPE;
+    // in place: every row onto itself (one head of one row alone has no stride)
+    if (q && q == q_out && q_head_stride != (int64_t)Tn * d && (long long)B * H > 1) return CHAI_ERR_SHAPE;
+    if (k && static_cast<const char *>(k) == static_cast<char *>(k_out) + (int64_t)pos0 * row_bytes_of(dtype) && k_head_stride != (int64_t)Tc_cap * d &&
+        (long long)B * k_slots > 1)
+        return CHAI_ERR_SHAPE;
+    if ((long long)B * Tn > 0x7fffffffll || 2ll * k_slots > kMaxGridYZ || (long long)pos0 + Tn > 0x7fffffffll) return CHAI_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return CHAI_ERR_ALIGN;
+    if (B == 0 || Tn == 0) return CHAI_OK;
+    TurnShape sh;
+    sh.rep = rep_heads;
+    sh.positions = positions;
+    sh.freq = freq;
+    sh.B = B;
+    sh.H = H;
+    sh.k = k_slots;
+    sh.rot = rot;
+    sh.gain = (double)gain;
+    sh.Tn = Tn;
+    sh.pos0 = pos0;
+    sh.Tc_cap = Tc_cap;
+    sh.N = B * Tn;
+    TurnRows rows;
+    rows.q = static_cast<const char *>(q);
+    rows.k = static_cast<const char *>(k);
+    rows.q_stride = q_head_stride;
+    rows.k_stride = k_head_stride;
+    rows.q_out = static_cast<char *>(q_out);
+    rows.k_out = static_cast<char *>(k_out);
+    return hip_status(launch_rotate(sh, rows, layout, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new, int64_t q_token_stride,
+                             int64_t k_token_stride, int64_t v_token_stride, int k_by_slot, const int32_t *rep_heads,
+                             const int32_t *token_rows, const int32_t *positions, const int32_t *slots, const double *freq,
+                             void *q_out, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int N, int B, int H,
+                             int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype, float gain,
+                             void *stream)
+{
+    if (N != 0 && (!k_new || !v_new || !token_rows || !slots || (rot != 0 && !positions) || (!q != !q_out))) return CHAI_ERR_NULL;
+    PagedShape ps;
+    PagedPages pg;
+    // (no table: slots say where rows go)
+    int st = check_pages(k_pages, v_pages, k_scales, v_scales, slots ? slots : reinterpret_cast<const int32_t *>(k_pages), B, H, k,
+                         rep_heads != nullptr, n_pages, page, 1, d, dtype, cache_dtype, &ps, &pg);
+    if (st == CHAI_OK) st = check_turn(rot, layout, dtype, d, freq);
+    if (st != CHAI_OK) return st;
+    const int64_t heads = (int64_t)H * d, keys = k_by_slot ? (int64_t)k * d : heads;
+    if (N < 0 || (N != 0 && B == 0)) return CHAI_ERR_SHAPE;
+    if (N != 0 && (k_token_stride < keys || v_token_stride < heads || (k_token_stride & 7) || (v_token_stride & 7))) return CHAI_ERR_SHAPE;
+    if (N != 0 && q && (q_token_stride < heads || (q_token_stride & 7) || (q == q_out && q_token_stride != heads))) return CHAI_ERR_SHAPE;
+    if (N > kMaxPagedTokens || (long long)n_pages * page > 0x7fffffffll || (long long)N * ((long long)H + 2ll * k) >= (1ll << 34))
+        return CHAI_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out)) return CHAI_ERR_ALIGN;
+    if (N == 0) return CHAI_OK;
+    TurnShape sh;
+    sh.rep = rep_heads;
+    sh.positions = positions;
+    sh.freq = freq;
+    sh.B = B;
+    sh.H = H;
+    sh.k = k;
+    sh.rot = rot;
+    sh.gain = (double)gain;
+    sh.rows = token_rows;
+    sh.slots = slots;
+    sh.N = N;
+    sh.by_slot = k_by_slot != 0;
+    sh.n_pages = n_pages;
+    sh.page = page;
+    sh.div_mul = ps.div_mul;
+    sh.div_shift = ps.div_shift;
+    TurnRows rows;
+    rows.q = static_cast<const char *>(q);
+    rows.k = static_cast<const char *>(k_new);
+    rows.v = static_cast<const char *>(v_new);
+    rows.q_stride = q_token_stride;
+    rows.k_stride = k_token_stride;
+    rows.v_stride = v_token_stride;
+    rows.q_out = static_cast<char *>(q_out);
+    rows.k_out = static_cast<char *>(k_pages);
+    rows.v_out = static_cast<char *>(v_pages);
+    rows.k_scales = k_scales;
+    rows.v_scales = v_scales;
+    return hip_status(launch_append_packed(sh, rows, layout, dtype, cache_dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -166,6 +166,46 @@ int launch_paged_append(const PagedShape &sh, const PagedPages &pg, const void *
 int launch_paged_gather(const PagedShape &sh, const PagedPages &pg, const int32_t *start, const int32_t *count, void *k_out, void *v_out,
                         int Tn, int dtype, int cache_dtype, hipStream_t stream);
 
+// Places of new tokens (chai_paged_place_tokens): all pointers on the device.
+struct PlaceShape {
+    int B = 0, N = 0, n_pages = 0, page = 0, max_blocks = 0;
+    int div_shift = 0;                   // n / page without a division
+    unsigned int div_mul = 0;
+};
+struct PlaceIn {
+    const int32_t *counts = nullptr, *lens = nullptr, *free_pages = nullptr, *n_free = nullptr;
+};
+struct PlaceOut {
+    int32_t *table = nullptr, *new_lens = nullptr, *n_left = nullptr, *granted = nullptr, *offsets = nullptr, *token_rows = nullptr,
+            *positions = nullptr, *slots = nullptr;
+};
+constexpr int kPlaceOneRows = 1024, kPlaceOneTokens = 2048;      // up to so many of both: one launch of one workgroup
+size_t place_workspace_bytes(int B);
+int launch_place_tokens(const PlaceShape &sh, const PlaceIn &in, const PlaceOut &out, void *workspace, hipStream_t stream);
+int launch_release_pages(const PlaceShape &sh, const int32_t *keep, const int32_t *lens, int32_t *table, int32_t *free_pages,
+                         const int32_t *n_free, int32_t *new_lens, int32_t *n_left, hipStream_t stream);
+
+// Rows turned by their positions: blocks of tokens of a contiguous cache, or tokens one behind the other on their way into pages.
+struct TurnShape {
+    const int32_t *rep = nullptr;        // [B,k], or NULL: every head (k = H)
+    const int32_t *positions = nullptr;  // of every token, or NULL (blocks): pos0 + its number
+    const double *freq = nullptr;        // [rot / 2] radians per position
+    int B = 0, H = 0, k = 0, rot = 0;
+    double gain = 1.0;
+    int Tn = 0, pos0 = 0, Tc_cap = 0;    // blocks: n = b * Tn + i
+    const int32_t *rows = nullptr, *slots = nullptr;     // packed: of every token
+    int N = 0, by_slot = 0, n_pages = 0, page = 0, div_shift = 0;
+    unsigned int div_mul = 0;
+};
+struct TurnRows {
+    const char *q = nullptr, *k = nullptr, *v = nullptr;
+    long long q_stride = 0, k_stride = 0, v_stride = 0;  // elements from head to head (blocks) or token to token (packed)
+    char *q_out = nullptr, *k_out = nullptr, *v_out = nullptr;       // (k_out, v_out: caches or pages)
+    float *k_scales = nullptr, *v_scales = nullptr;
+};
+int launch_rotate(const TurnShape &sh, const TurnRows &rows, int layout, int dtype, hipStream_t stream);
+int launch_append_packed(const TurnShape &sh, const TurnRows &rows, int layout, int dtype, int cache_dtype, hipStream_t stream);
+
 // 32 x 32 x 16 products alone: `rounds` rounds of 8 of them per wave on operands taken from buf; flops of one launch
 int launch_mfma_probe(const void *buf, size_t bytes, int rounds, float *sink, const KernelEvents &ev, hipStream_t stream);
 double mfma_probe_flops(int rounds);

@@ -1,0 +1,271 @@
+// Places of new tokens: which rows of a batch get their new tokens, which pages of a list of free ones they take for them, and where
+// every token of the batch, one row's behind the other's, then stands.  All on the device: lengths, tables and the list never come to
+// the host, so that a recorded step can be replayed while rows grow.
+//
+//   row b:    have = ceil(len / page) pages, need = ceil((len + count) / page) - have more, granted iff its tokens end within the block
+//             of N tokens and within its table, and need = 0 or need[0] + .. + need[b] <= n_free (over the rows that end within both)
+//   pages:    the list is a stack; the rows take from its top, in row order
+//   token i:  position len + i in page position / page of its row, slot = page number * page + position % page
+//
+// Two sums over the rows (tokens and pages), both capped, so that no number of tokens overflows them: min(a + b, cap) is associative.
+#include "chai_internal.h"
+
+#include <hip/hip_ext.h>
+
+namespace chai {
+
+namespace {
+
+constexpr int kPlaceBlock = 256;
+constexpr int kPlaceWaves = kPlaceBlock / 64;
+
+__device__ __forceinline__ unsigned int capped(unsigned int a, unsigned int b, unsigned int cap) { return min(a + b, cap); }
+
+// position / page, as the attention kernels find it
+__device__ __forceinline__ int block_at(const PlaceShape &sh, unsigned int pos) { return (int)((__umulhi(pos, sh.div_mul) + pos) >> sh.div_shift); }
+__device__ __forceinline__ int blocks_of(const PlaceShape &sh, unsigned int n) { return n == 0u ? 0 : block_at(sh, n - 1u) + 1; }
+
+// What the tokens of a row have to know of it.
+struct PlacedRow {
+    int first;        // number of its first token in the block
+    int len;          // positions before the call
+    int have;         // its pages before the call, or -1: it got none of what it asked for
+    int top;          // its i-th new page is free_pages[top - 1 - i]
+};
+
+// inclusive sum over the workgroup, capped; `sums` [kPlaceWaves] is free again after the call's barrier and one more
+__device__ __forceinline__ unsigned int block_scan(unsigned int x, unsigned int cap, unsigned int *sums)
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned int other = (unsigned int)__shfl_up((int)x, o);
+        if (lane >= o) x = capped(x, other, cap);
+    }
+    if (lane == 63) sums[w] = x;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < kPlaceWaves; ++v)
+        if (v < w) x = capped(x, sums[v], cap);
+    return x;
+}
+
+// Which rows get their tokens; one workgroup.  rows: [B] in LDS or in the workspace; total (in LDS or NULL): tokens of all.  Everything that may be written in place
+// (new_lens over seq_lens, n_left over n_free) has been read by every thread before the first barrier.
+__device__ __forceinline__ void place_rows(const PlaceShape &sh, const PlaceIn &in, const PlaceOut &out, PlacedRow *rows, int *total)
+{
+    __shared__ unsigned int sums[2][kPlaceWaves], taken;
+    const int tid = threadIdx.x, span = (sh.B + kPlaceBlock - 1) / kPlaceBlock;
+    const unsigned int most_tokens = (unsigned int)sh.N + 1u, most_pages = (unsigned int)sh.n_pages + 1u;
+    const unsigned int n_free = (unsigned int)min(max(in.n_free[0], 0), sh.n_pages);
+    const long long reach = min((long long)sh.max_blocks * sh.page, 0x7fffffffll);
+    if (tid == 0) taken = 0u;
+
+    // (the first of a thread's rows, all it has where there are few, is asked for once)
+    const int b0 = min(tid * span, sh.B), b1 = min(b0 + span, sh.B);
+    const int count0 = b0 < b1 ? in.counts[b0] : 0, len0 = b0 < b1 ? in.lens[b0] : 0;
+    auto count_of = [&](int b) { return min((unsigned int)max(b == b0 ? count0 : in.counts[b], 0), most_tokens); };
+    auto len_of = [&](int b) { return max(b == b0 ? len0 : in.lens[b], 0); };
+    unsigned int tokens = 0u;
+    for (int b = b0; b < b1; ++b) tokens = capped(tokens, count_of(b), most_tokens);
+    const unsigned int tokens_upto = block_scan(tokens, most_tokens, sums[0]);
+    // what came before this thread's rows: with a cap it cannot be had by subtraction
+    unsigned int tokens_before = (unsigned int)__shfl_up((int)tokens_upto, 1);
+    if ((tid & 63) == 0) {
+        tokens_before = 0u;
+        for (int v = 0; v < tid >> 6; ++v) tokens_before = capped(tokens_before, sums[0][v], most_tokens);
+    }
+    auto need_of = [&](unsigned int end, int len, unsigned int count, bool &fits) {
+        fits = end <= (unsigned int)sh.N && (long long)len + count <= reach;
+        return fits ? (unsigned int)(blocks_of(sh, (unsigned int)len + count) - blocks_of(sh, (unsigned int)len)) : 0u;
+    };
+    unsigned int pages = 0u, end = tokens_before;
+    for (int b = b0; b < b1; ++b) {
+        const unsigned int count = count_of(b);
+        bool fits;
+        end = capped(end, count, most_tokens);
+        pages = capped(pages, need_of(end, len_of(b), count, fits), most_pages);
+    }
+    const unsigned int pages_upto = block_scan(pages, most_pages, sums[1]);
+    unsigned int pages_end = (unsigned int)__shfl_up((int)pages_upto, 1);
+    if ((tid & 63) == 0) {
+        pages_end = 0u;
+        for (int v = 0; v < tid >> 6; ++v) pages_end = capped(pages_end, sums[1][v], most_pages);
+    }
+    end = tokens_before;
+    unsigned int last = 0u;
+    for (int b = b0; b < b1; ++b) {
+        const unsigned int count = count_of(b), first = end, before = pages_end;
+        const int len = len_of(b);
+        bool fits;
+        end = capped(end, count, most_tokens);
+        const unsigned int need = need_of(end, len, count, fits);
+        pages_end = capped(pages_end, need, most_pages);
+        const bool granted = fits && (need == 0u || pages_end <= n_free);
+        if (granted && need != 0u) last = pages_end;
+        rows[b] = PlacedRow{(int)min(first, (unsigned int)sh.N), len, granted ? blocks_of(sh, (unsigned int)len) : -1,
+                            granted ? (int)(n_free - min(before, n_free)) : 0};
+        out.offsets[b] = (int)min(first, (unsigned int)sh.N);
+        out.granted[b] = granted ? 1 : 0;
+        out.new_lens[b] = granted ? len + (int)count : len;
+    }
+    if (last != 0u) atomicMax(&taken, last);
+    if (tid == kPlaceBlock - 1) {
+        out.offsets[sh.B] = (int)min(tokens_upto, (unsigned int)sh.N);
+        if (total != nullptr) *total = (int)min(tokens_upto, (unsigned int)sh.N);
+    }
+    __syncthreads();
+    if (tid == 0) out.n_left[0] = (int)(n_free - taken);
+}
+
+// Token n: its row (the last one that begins at or before it: rows without tokens begin where the next one does), position and slot;
+// the first token of a page that its row took enters it in the table.
+__device__ __forceinline__ void place_token(const PlaceShape &sh, const PlaceIn &in, const PlaceOut &out, const PlacedRow *rows, int n, int total)
+{
+    int b = -1, pos = 0, slot = -1;
+    if (n < total) {
+        int lo = 0, hi = sh.B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (rows[mid].first <= n) lo = mid;
+            else hi = mid - 1;
+        }
+        b = lo;
+        const PlacedRow r = rows[b];
+        const unsigned int at = (unsigned int)r.len + (unsigned int)(n - r.first);
+        pos = (int)at;
+        if (r.have >= 0) {
+            const int block = block_at(sh, at), place = (int)at - block * sh.page;
+            int32_t *entry = out.table + (size_t)b * sh.max_blocks + block;
+            int p;
+            if (block >= r.have) {
+                p = in.free_pages[r.top - 1 - (block - r.have)];
+                if (place == 0) *entry = p;
+            } else {
+                p = *entry;
+            }
+            if ((unsigned int)p < (unsigned int)sh.n_pages) slot = p * sh.page + place;
+        }
+    }
+    out.token_rows[n] = b;
+    out.positions[n] = pos;
+    out.slots[n] = slot;
+}
+
+// One workgroup for everything.
+__global__ __launch_bounds__(kPlaceBlock) void place_all_kernel(PlaceShape sh, PlaceIn in, PlaceOut out)
+{
+    __shared__ PlacedRow rows[kPlaceOneRows];
+    __shared__ int total;
+    place_rows(sh, in, out, rows, &total);
+    for (int n = threadIdx.x; n < sh.N; n += kPlaceBlock) place_token(sh, in, out, rows, n, total);
+}
+
+__global__ __launch_bounds__(kPlaceBlock) void place_rows_kernel(PlaceShape sh, PlaceIn in, PlaceOut out, PlacedRow *rows)
+{
+    place_rows(sh, in, out, rows, nullptr);
+}
+
+__global__ __launch_bounds__(kPlaceBlock) void place_tokens_kernel(PlaceShape sh, PlaceIn in, PlaceOut out, const PlacedRow *rows)
+{
+    const int n = blockIdx.x * kPlaceBlock + threadIdx.x;
+    if (n < sh.N) place_token(sh, in, out, rows, n, out.offsets[sh.B]);
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Pages of rows that end, or lose their last positions, go back on the list: those behind the kept positions that are pages, rows in
+// order, a row's in order.  One workgroup: rows write behind one another.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kReleaseBlock = 1024;
+
+__global__ __launch_bounds__(kReleaseBlock) void release_kernel(PlaceShape sh, const int32_t *__restrict__ keep, const int32_t *lens, int32_t *table,
+                                                                int32_t *free_pages, const int32_t *n_free, int32_t *new_lens, int32_t *n_left)
+{
+    __shared__ int from[kMaxPagedBatch];                 // pages of a row that go back, then where its first one goes
+    __shared__ int sums[kReleaseBlock / 64];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int top = min(max(n_free[0], 0), sh.n_pages);
+    auto bounds = [&](int b, int &lo, int &hi) {
+        const int len = max(lens[b], 0), kept = min(max(keep[b], 0), len);
+        lo = min(blocks_of(sh, (unsigned int)kept), sh.max_blocks);
+        hi = min(blocks_of(sh, (unsigned int)len), sh.max_blocks);
+        return kept;
+    };
+    for (int b = w; b < sh.B; b += kReleaseBlock / 64) {
+        int lo, hi, n = 0;
+        bounds(b, lo, hi);
+        for (int i = lo; i < hi; i += 64) {
+            const int p = i + lane < hi ? table[(size_t)b * sh.max_blocks + i + lane] : -1;
+            n += __popcll(__ballot((unsigned int)p < (unsigned int)sh.n_pages));
+        }
+        if (lane == 0) from[b] = n;
+    }
+    __syncthreads();
+    // (at most n_pages go back in a table of pages that are in use once; a sum that a broken table makes larger is cut there)
+    const int span = (sh.B + kReleaseBlock - 1) / kReleaseBlock, b0 = min(tid * span, sh.B), b1 = min(b0 + span, sh.B);
+    const unsigned int cap = (unsigned int)sh.n_pages + 1u;
+    unsigned int mine = 0u;
+    for (int b = b0; b < b1; ++b) mine = capped(mine, (unsigned int)from[b], cap);
+    unsigned int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned int other = (unsigned int)__shfl_up((int)upto, o);
+        if (lane >= o) upto = capped(upto, other, cap);
+    }
+    if (lane == 63) sums[w] = (int)upto;
+    unsigned int before = (unsigned int)__shfl_up((int)upto, 1);
+    if (lane == 0) before = 0u;
+    __syncthreads();
+    for (int v = 0; v < w; ++v) before = capped(before, (unsigned int)sums[v], cap);
+    for (int b = b0; b < b1; ++b) {
+        const unsigned int n = (unsigned int)from[b];
+        from[b] = (int)before;
+        before = capped(before, n, cap);
+    }
+    __syncthreads();
+    for (int b = w; b < sh.B; b += kReleaseBlock / 64) {
+        int lo, hi;
+        bounds(b, lo, hi);
+        long long at = (long long)top + from[b];
+        for (int i = lo; i < hi; i += 64) {
+            int32_t *entry = table + (size_t)b * sh.max_blocks + i + lane;
+            const int p = i + lane < hi ? *entry : -1;
+            const bool page = (unsigned int)p < (unsigned int)sh.n_pages;
+            const unsigned long long votes = __ballot(page);
+            const long long to = at + __popcll(votes & ((1ull << lane) - 1ull));
+            if (page && to < sh.n_pages) free_pages[to] = p;
+            if (i + lane < hi) *entry = -1;
+            at += __popcll(votes);
+        }
+    }
+    __syncthreads();
+    for (int b = tid; b < sh.B; b += kReleaseBlock) {
+        int lo, hi;
+        new_lens[b] = bounds(b, lo, hi);
+    }
+    if (tid == kReleaseBlock - 1) n_left[0] = (int)min((long long)top + before, (long long)sh.n_pages);
+}
+
+}  // namespace
+
+size_t place_workspace_bytes(int B) { return ((size_t)B * sizeof(PlacedRow) + 255) / 256 * 256; }
+
+int launch_place_tokens(const PlaceShape &sh, const PlaceIn &in, const PlaceOut &out, void *workspace, hipStream_t stream)
+{
+    if (sh.B <= kPlaceOneRows && sh.N <= kPlaceOneTokens)
+        return (int)launch_kernel(place_all_kernel, dim3(1), dim3(kPlaceBlock), 0, stream, KernelEvents{}, sh, in, out);
+    PlacedRow *rows = static_cast<PlacedRow *>(workspace);
+    const hipError_t e = launch_kernel(place_rows_kernel, dim3(1), dim3(kPlaceBlock), 0, stream, KernelEvents{}, sh, in, out, rows);
+    if (e != hipSuccess || sh.N == 0) return (int)e;
+    return (int)launch_kernel(place_tokens_kernel, dim3((unsigned int)((sh.N + kPlaceBlock - 1) / kPlaceBlock)), dim3(kPlaceBlock), 0, stream,
+                              KernelEvents{}, sh, in, out, rows);
+}
+
+int launch_release_pages(const PlaceShape &sh, const int32_t *keep, const int32_t *lens, int32_t *table, int32_t *free_pages,
+                         const int32_t *n_free, int32_t *new_lens, int32_t *n_left, hipStream_t stream)
+{
+    return (int)launch_kernel(release_kernel, dim3(1), dim3(kReleaseBlock), 0, stream, KernelEvents{}, sh, keep, lens, table, free_pages, n_free,
+                              new_lens, n_left);
+}
+
+}  // namespace chai
