@@ -715,6 +715,34 @@ int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new
                              int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype, float gain,
                              void *stream);
 
+/*
+ * chai_project_qk with a low-rank adapter of every row's own beside the shared
+ * weights, as servers of many tuned models keep them (row b, a =
+ * adapter_ids[b], s_a its factor, slot j with r = rep_heads[b][j] >= 0):
+ *   q_out[b][r][i][:]            = x[b][i] . w_q[r]^T + s_a (x[b][i] . a_q[a]^T) . b_q[a][r]^T
+ *   k_compact[b][j][pos0 + i][:] = the same with w_k, a_k, b_k
+ * Products accumulate in fp32; (s_a x a^T) is held in 16 bits of mantissa (two
+ * bf16), their sum in fp32, and that is rounded once to bf16.
+ *
+ *   adapter_ids   [B] int32 on the device; a row whose id is outside
+ *                 [0,n_adapters) has no adapter
+ *   a_q, a_k      [n_adapters,R,D] bf16
+ *   b_q, b_k      [n_adapters,H*d,R] bf16 (a_q and b_q may both be NULL:
+ *                 adapters of the keys alone; or a_k and b_k)
+ *   adapter_scale [n_adapters] fp32, or NULL: 1
+ *   workspace     chai_project_adapted_workspace_bytes(B,Tn,R) bytes (0 on
+ *                 invalid sizes; never decreases), 256-byte aligned, contents
+ *                 need not be initialised.  Two calls that run concurrently
+ *                 need separate workspaces.
+ * R is a multiple of 8 up to 128 (adapters of a smaller rank: zeros behind it);
+ * the other arguments, limits and errors as chai_project_qk.
+ */
+size_t chai_project_adapted_workspace_bytes(int B, int Tn, int R);
+int chai_project_qk_adapted(const void *x, const void *w_q, const void *w_k, const int32_t *rep_heads, const int32_t *adapter_ids,
+                            const void *a_q, const void *b_q, const void *a_k, const void *b_k, const float *adapter_scale,
+                            int n_adapters, int R, int B, int H, int k, int Tn, int D, int d, int dtype, void *q_out,
+                            void *k_compact, int pos0, int Tc_cap, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

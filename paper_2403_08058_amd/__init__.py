@@ -8,7 +8,7 @@ import importlib
 
 _BINDING_NAMES = ("CHAI_BF16", "CHAI_E4M3", "CHAI_F32", "CHAI_OK", "CHAI_ROPE_BASE", "CHAI_ROPE_HALVES", "CHAI_ROPE_LINEAR",
                   "CHAI_ROPE_PAIRS", "CHAI_ROPE_PLAIN", "CHAI_ROPE_TURNS", "EXPORTS", "LIB_PATH", "ChaiError",
-                  "alloc_paged_place_workspace", "alloc_paged_workspace", "alloc_workspace", "lib")
+                  "alloc_adapted_workspace", "alloc_paged_place_workspace", "alloc_paged_workspace", "alloc_workspace", "lib")
 
 
 def __getattr__(name):

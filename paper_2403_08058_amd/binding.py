@@ -37,7 +37,8 @@ EXPORTS = ["chai_version", "chai_status_string", "chai_score_features", "chai_as
            "chai_prefill_attention_timed", "chai_dense_prefill_attention", "chai_project_qk", "chai_project_qk_timed", "chai_stream_read_probe", "chai_mfma_rate_probe",
            "chai_paged_workspace_bytes", "chai_paged_append_kv", "chai_paged_gather_kv", "chai_paged_decode_attention",
            "chai_paged_decode_step", "chai_paged_place_workspace_bytes", "chai_paged_place_tokens", "chai_paged_release_pages",
-           "chai_rotary_frequencies", "chai_rotate_qk", "chai_paged_append_packed"]
+           "chai_rotary_frequencies", "chai_rotate_qk", "chai_paged_append_packed", "chai_project_adapted_workspace_bytes",
+           "chai_project_qk_adapted"]
 
 
 class ChaiError(RuntimeError):
@@ -104,8 +105,11 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.chai_rotary_frequencies.argtypes = [ci, cd, ci, cd, cd, cd, cd, vp]
     L.chai_rotate_qk.argtypes = [vp, vp, i64, i64, vp, vp, vp] + [ci] * 10 + [cf, vp, vp, vp]
     L.chai_paged_append_packed.argtypes = [vp] * 3 + [i64] * 3 + [ci] + [vp] * 10 + [ci] * 11 + [cf, vp]
+    L.chai_project_adapted_workspace_bytes.restype = sz
+    L.chai_project_adapted_workspace_bytes.argtypes = [ci] * 3
+    L.chai_project_qk_adapted.argtypes = [vp] * 10 + [ci] * 9 + [vp, vp, ci, ci, vp, sz, vp]
     for fn in EXPORTS:
-        if fn not in ("chai_paged_workspace_bytes", "chai_paged_place_workspace_bytes", "chai_status_string", "chai_decode_workspace_bytes", "chai_prefill_workspace_bytes",
+        if fn not in ("chai_project_adapted_workspace_bytes", "chai_paged_workspace_bytes", "chai_paged_place_workspace_bytes", "chai_status_string", "chai_decode_workspace_bytes", "chai_prefill_workspace_bytes",
                       "chai_decode_q8_workspace_bytes"):
             getattr(L, fn).restype = ci
     return L
@@ -777,6 +781,40 @@ def chai_paged_append_packed(q, k_new, v_new, rep_heads, token_rows, positions, 
     _check(fn, _lib.chai_paged_append_packed(qp, kp, vp, qs, ks, vs, int(k_by_slot), *p, fp, *o, N, B, H, k, n_pages, page, d, rot, layout,
                                              code, pages, gain, _stream(stream)))
     return q_out
+
+
+def chai_project_adapted_workspace_bytes(B: int, Tn: int, R: int) -> int:
+    return int(_lib.chai_project_adapted_workspace_bytes(B, Tn, R))
+
+
+def alloc_adapted_workspace(B: int, Tn: int, R: int, device="cuda") -> torch.Tensor:
+    """Device scratch of chai_project_qk_adapted; one of the largest sizes serves all smaller calls."""
+    return torch.empty((max(chai_project_adapted_workspace_bytes(B, Tn, R), 256),), dtype=torch.uint8, device=device)
+
+
+def chai_project_qk_adapted(x, w_q, w_k, rep_heads, adapter_ids, a_q, b_q, a_k, b_k, adapter_scale, q_out, k_compact, pos0: int,
+                            workspace, stream=None):
+    """chai_project_qk with row b's adapter adapter_ids[b] (int32; outside [0,n): none) beside the weights: a_q, a_k [n,R,D], b_q, b_k
+    [n,H*d,R] (bf16; of queries or keys both None: none of those), factors adapter_scale [n] fp32 (None: 1)."""
+    fn = "chai_project_qk_adapted"
+    B, Tn, D = x.shape
+    H, d = q_out.shape[1], q_out.shape[3]
+    k, Tc_cap = k_compact.shape[1], k_compact.shape[2]
+    a = a_q if a_q is not None else a_k
+    if a is None or (a_q is None) != (b_q is None) or (a_k is None) != (b_k is None):
+        _misfit(fn, "adapters of queries or keys, or both, each of two parts")
+    n, R = a.shape[0], a.shape[1]
+    dtype = x.dtype
+    for t, shape in ((x, (B, Tn, D)), (w_q, (H * d, D)), (w_k, (H * d, D)), (a_q, (n, R, D)), (a_k, (n, R, D)), (b_q, (n, H * d, R)),
+                     (b_k, (n, H * d, R)), (q_out, (B, H, Tn, d)), (k_compact, (B, k, Tc_cap, d))):
+        if t is not None and (t.shape != shape or t.dtype is not dtype):
+            _misfit(fn, f"{dtype} of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
+    if rep_heads.shape != (B, k) or rep_heads.dtype is not _I32 or adapter_ids.shape != (B,) or adapter_ids.dtype is not _I32 \
+            or (adapter_scale is not None and (adapter_scale.shape != (n,) or adapter_scale.dtype is not _F32)):
+        _misfit(fn, "int32 maps and adapters for every row, fp32 factors for every adapter expected")
+    p = _ptrs((x, w_q, w_k, rep_heads, adapter_ids, a_q, b_q, a_k, b_k, adapter_scale, q_out, k_compact, workspace))
+    _check(fn, _lib.chai_project_qk_adapted(*p[:10], n, R, B, H, k, Tn, D, d, dtype_code(x), p[10], p[11], pos0, Tc_cap, p[12],
+                                            workspace.nbytes, _stream(stream)))
 
 
 class _Binding(types.ModuleType):

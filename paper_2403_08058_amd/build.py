@@ -32,6 +32,7 @@ SOURCES = {
     "prefill.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-mfma-vgpr-form", "-mllvm", "-structurizecfg-skip-uniform-regions",
                     "-mllvm", "-align-all-nofallthru-blocks=6"],
     "project.hip": [],
+    "adapter.hip": [],
     # bit-exact k-means: no fused multiply-add, no reassociation
     "kmeans.hip": ["-ffp-contract=off", "-fno-fast-math"],
 }

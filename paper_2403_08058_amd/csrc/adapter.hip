@@ -1,0 +1,204 @@
+// The first half of a low-rank adapter: t = s_a x A_a^T of every token, a = the adapter of the token's row.  The projections add the second
+// half, t B_a^T, to what they sum up (project.hip).
+//
+//   x [B,Tn,D], A [n,R,D] bf16, queries' and keys' apart;  t [B,Tn][2][chunks][32] bf16: of sixteen ranks the upper 8 bits of t, then what
+//   those leave, again rounded to 8 bits: t to 2^-17 of itself.  (In 8 bits alone it would be the largest error of the call, 2^-9 of the
+//   adapter's part in every sum; the second product is a hundredth of the first, twice its depth costs nothing.)
+//
+// A workgroup takes the ranks of U units of 8 (of queries, then of keys) for 8 XT tokens of one row.  As in the projections of few tokens,
+// its waves deal the contraction out in blocks of 64 elements and stream their blocks, ranks and tokens, through rings of their own in LDS,
+// without a barrier before the sums of all waves are added in wave order.
+#include "chai_internal.h"
+
+#include <hip/hip_ext.h>
+
+#include <type_traits>
+#include <utility>
+
+namespace chai {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+union Frag {
+    u32x4 raw;
+    bf16x8 bf;
+};
+
+template <typename F, int... I>
+__device__ __forceinline__ void unroll_seq(F &&f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unroll(F &&f)
+{
+    unroll_seq(f, std::make_integer_sequence<int, N>{});
+}
+
+constexpr int kAdWaveBytes = 20 * 1024;              // ring of a wave
+constexpr int kAdMostAhead = 8;
+
+template <int U, int XT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void adapter_down_kernel(const char *__restrict__ x, const int32_t *__restrict__ ids,
+                                                                  const char *__restrict__ a_q, const char *__restrict__ a_k,
+                                                                  const float *__restrict__ scales, int n, int R, int Tn, int D, int tiles,
+                                                                  int groups, unsigned int items, char *__restrict__ t)
+{
+    constexpr int NB = (U + 1) / 2, TT = (XT + 1) / 2, kLoads = U + XT, kBytes = kLoads * 1024;
+    constexpr int N = kAdWaveBytes / kBytes < kAdMostAhead ? kAdWaveBytes / kBytes : kAdMostAhead;       // blocks of a ring
+    static_assert(N >= 2 && NB * TT * 1024 <= kAdWaveBytes, "a block ahead; the sums fit");
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // items: (row, tile of tokens, group of ranks), the groups of a tile, which read the same tokens, on one XCD
+    const unsigned int local = blockIdx.x >> 3, item = (local / (unsigned int)groups * 8u + (blockIdx.x & 7u)) * (unsigned int)groups + local % (unsigned int)groups;
+    if (item >= items) return;
+    const int group = (int)(item % (unsigned int)groups), tile = (int)(item / (unsigned int)groups), b = tile / tiles, c0 = (tile - b * tiles) * 8 * XT;
+    const int a = ids[b];
+    if ((unsigned int)a >= (unsigned int)n) return;      // (t of these rows is not read)
+    const int each = R / 8, first = a_q == nullptr ? each : 0, total = (a_q != nullptr ? each : 0) + (a_k != nullptr ? each : 0);
+    const int u0 = group * U;                            // units of the group: first + u0 .., each of queries (below `each`) or keys
+    const unsigned int row_bytes = (unsigned int)D * 2u;
+    const int col = lane & 15, g = lane >> 4, r8 = lane >> 3;
+    // piece p of row r of eight lands in slot p ^ (r >> 1), with 4 on top in every other group of eight rows: 16 rows read at one
+    // piece touch 16 different 16-byte bank groups
+    const int piece[2] = {((lane & 7) ^ (r8 >> 1)) * 16, ((lane & 7) ^ (4 + (r8 >> 1))) * 16};
+    char *const ring = lds + w * kAdWaveBytes;
+    unsigned int aoff[U], xoff[XT];
+    bool key[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int u = first + min(u0 + i, total - 1);    // (units past the end repeat the last one, unused)
+        key[i] = u >= each;
+        aoff[i] = (unsigned int)((u - (key[i] ? each : 0)) * 8 + r8) * row_bytes + piece[i & 1];
+    }
+#pragma unroll
+    for (int i = 0; i < XT; ++i) xoff[i] = (unsigned int)min(c0 + 8 * i + r8, Tn - 1) * row_bytes + piece[i & 1];
+    const int n_mine = (D / 64 - w + WAVES - 1) / WAVES;                 // blocks of this wave: w, w + WAVES, ..
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto base = [&](const char *from, size_t at) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from + at), 0, -1, 0x00020000); };
+    const auto x_rs = base(x, (size_t)b * Tn * row_bytes);
+    const auto q_rs = base(a_q != nullptr ? a_q : a_k, (size_t)a * R * row_bytes);
+    const auto k_rs = base(a_k != nullptr ? a_k : a_q, (size_t)a * R * row_bytes);
+#endif
+    auto fetch = [&](int s, int at) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const unsigned int off = (unsigned int)(w + s * WAVES) * 128u;
+        auto load = [&](__amdgpu_buffer_rsrc_t rs, unsigned int from, int i) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(ring + at * kBytes + i * 1024), 16, (int)from, 0, 0, 0);
+        };
+#pragma unroll
+        for (int i = 0; i < U; ++i) load(key[i] ? k_rs : q_rs, aoff[i] + off, i);
+#pragma unroll
+        for (int i = 0; i < XT; ++i) load(x_rs, xoff[i] + off, U + i);
+#endif
+    };
+    // all requests but those of the `younger` last blocks have landed
+    auto landed = [&](int younger) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        if (younger >= N - 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((N - 1) * kLoads) : "memory");
+        else
+            unroll<N - 1>([&](auto m) {
+                if (younger == m.value) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(m.value * kLoads) : "memory");
+            });
+#endif
+    };
+    f32x4 acc[NB][TT];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < TT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < N - 1; ++s)
+        if (s < n_mine) fetch(s, s);
+    int at = 0;
+    for (int s = 0; s < n_mine; ++s) {
+        if (s + N - 1 < n_mine) fetch(s + N - 1, at == 0 ? N - 1 : at - 1);
+        landed(n_mine - 1 - s);
+        const char *from = ring + at * kBytes;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            // (rows past an odd number of units are of no rank or token; of one unit the row itself is read again)
+            const int slot = ((4 * i + g) ^ ((col >> 1) & 7)) << 4, slot8 = ((4 * i + g) ^ ((col & 7) >> 1)) << 4;
+            Frag fa[NB], fx[TT];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) fa[j].raw = *reinterpret_cast<const u32x4 *>(from + (j * 16 + (U == 1 ? col & 7 : col)) * 128 + (U == 1 ? slot8 : slot));
+#pragma unroll
+            for (int j = 0; j < TT; ++j) fx[j].raw = *reinterpret_cast<const u32x4 *>(from + (U * 8 + j * 16 + (XT == 1 ? col & 7 : col)) * 128 + (XT == 1 ? slot8 : slot));
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < TT; ++e) acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[j].bf, fx[e].bf, acc[j][e], 0, 0, 0);
+        }
+        at = at == N - 1 ? 0 : at + 1;
+    }
+    __syncthreads();
+    f32x4 *const red = reinterpret_cast<f32x4 *>(lds);   // [wave][NB][TT][lane]
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < TT; ++j) red[((w * NB + i) * TT + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    // lane l holds ranks 16 i + 4*(l/16) .. +3 of the group, of token l%16
+    const float scale = scales != nullptr ? scales[a] : 1.f;
+    for (int out = w; out < NB * TT; out += WAVES) {
+        const int i = out / TT, j = out % TT, tok = c0 + j * 16 + col, u = u0 + 2 * i + (g >> 1);
+        if (tok >= Tn || tok >= c0 + 8 * XT || 2 * i + (g >> 1) >= U || u >= total) continue;
+        f32x4 sum = red[(i * TT + j) * 64 + lane];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v) sum += red[((v * NB + i) * TT + j) * 64 + lane];
+        const int part = first + u >= each ? 1 : 0, rank = (first + u - part * each) * 8 + (g & 1) * 4;
+        bf16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float y = scale * sum[e];
+            hi[e] = (__bf16)y;
+            const float rest = y - (float)hi[e];         // (an infinity's is NaN)
+            lo[e] = (__bf16)(rest - rest == 0.f ? rest : 0.f);
+            if (fabsf(y) < __builtin_huge_valf() && rest - rest != 0.f) {        // the largest of 32 bits round up to infinity: cut
+                const float cut = __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+                hi[e] = (__bf16)cut;
+                lo[e] = (__bf16)(y - cut);
+            }
+        }
+        char *to = t + (((size_t)b * Tn + tok) * 2 + part) * (size_t)((R + 15) / 16 * 64) + rank / 16 * 64 + rank % 16 * 2;
+        *reinterpret_cast<bf16x4 *>(to) = hi;
+        *reinterpret_cast<bf16x4 *>(to + 32) = lo;
+    }
+}
+
+template <int U, int XT, int WAVES>
+int launch_down(const char *x, const int32_t *ids, const char *a_q, const char *a_k, const float *scales, int n, int R, int B, int Tn, int D,
+                char *t, hipStream_t stream)
+{
+    const int total = R / 8 * ((a_q ? 1 : 0) + (a_k ? 1 : 0)), groups = (total + U - 1) / U, tiles = (Tn + 8 * XT - 1) / (8 * XT);
+    const long long n_tiles = (long long)B * tiles, items = n_tiles * groups, grid = (n_tiles + 7) / 8 * 8 * groups;
+    if (grid > 0x7fffffffll) return (int)hipErrorInvalidConfiguration;
+    static DeviceFlags lds_allowed;
+    const size_t lds = (size_t)WAVES * kAdWaveBytes;
+    const auto kernel = adapter_down_kernel<U, XT, WAVES>;
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds, lds_allowed);
+    if (e != hipSuccess) return (int)e;
+    return (int)launch_kernel(kernel, dim3((unsigned int)grid), dim3(WAVES * 64), lds, stream, KernelEvents{}, x, ids, a_q, a_k, scales, n, R, Tn, D,
+                              tiles, groups, (unsigned int)items, t);
+}
+
+}  // namespace
+
+size_t adapter_workspace_bytes(int B, int Tn, int R) { return ((size_t)B * Tn * 2 * ((R + 15) / 16) * 64 + 255) / 256 * 256; }
+
+int launch_adapter_down(const void *x_, const int32_t *ids, const void *a_q_, const void *a_k_, const float *scales, int n, int R, int B, int Tn,
+                        int D, void *t_, hipStream_t stream)
+{
+    const char *x = static_cast<const char *>(x_), *a_q = static_cast<const char *>(a_q_), *a_k = static_cast<const char *>(a_k_);
+    char *t = static_cast<char *>(t_);
+    if (Tn <= 8) return launch_down<1, 1, 8>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
+    if (Tn <= 64) return launch_down<2, 2, 8>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
+    return launch_down<4, 4, 4>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
+}
+
+}  // namespace chai

@@ -466,9 +466,8 @@ int chai_dense_decode_attention(const void *q, const void *k_cache, const void *
                                     plan, true, static_cast<hipStream_t>(stream)));
 }
 
-int chai_project_qk_timed(const void *x, const void *w_q, const void *w_k, const int32_t *rep_heads, int B, int H, int k,
-                          int Tn, int D, int d, int dtype, void *q_out, void *k_compact, int pos0, int Tc_cap,
-                          void *stream, void *start_event, void *stop_event)
+static int check_project(const void *x, const void *w_q, const void *w_k, const int32_t *rep_heads, int B, int H, int k, int Tn, int D,
+                         int d, int dtype, const void *q_out, const void *k_compact, int pos0, int Tc_cap)
 {
     if (!x || !w_q || !w_k || !rep_heads || !q_out || !k_compact) return CHAI_ERR_NULL;
     if (bad_dtype(dtype)) return CHAI_ERR_DTYPE;
@@ -479,6 +478,15 @@ int chai_project_qk_timed(const void *x, const void *w_q, const void *w_k, const
         return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(x) || !aligned16(w_q) || !aligned16(w_k) || !aligned16(q_out) || !aligned16(k_compact))
         return CHAI_ERR_ALIGN;
+    return CHAI_OK;
+}
+
+int chai_project_qk_timed(const void *x, const void *w_q, const void *w_k, const int32_t *rep_heads, int B, int H, int k,
+                          int Tn, int D, int d, int dtype, void *q_out, void *k_compact, int pos0, int Tc_cap,
+                          void *stream, void *start_event, void *stop_event)
+{
+    const int st = check_project(x, w_q, w_k, rep_heads, B, H, k, Tn, D, d, dtype, q_out, k_compact, pos0, Tc_cap);
+    if (st != CHAI_OK) return st;
     if (B == 0) return CHAI_OK;
     KernelEvents ev;
     ev.start = static_cast<hipEvent_t>(start_event);
@@ -492,6 +500,39 @@ int chai_project_qk(const void *x, const void *w_q, const void *w_k, const int32
 {
     return chai_project_qk_timed(x, w_q, w_k, rep_heads, B, H, k, Tn, D, d, dtype, q_out, k_compact, pos0, Tc_cap, stream,
                                  nullptr, nullptr);
+}
+
+size_t chai_project_adapted_workspace_bytes(int B, int Tn, int R)
+{
+    if (B < 0 || Tn < 1 || R < 8 || R % 8 != 0 || R > kMaxAdapterRank) return 0;
+    return B == 0 ? 256 : adapter_workspace_bytes(B, Tn, R);
+}
+
+int chai_project_qk_adapted(const void *x, const void *w_q, const void *w_k, const int32_t *rep_heads, const int32_t *adapter_ids,
+                            const void *a_q, const void *b_q, const void *a_k, const void *b_k, const float *adapter_scale,
+                            int n_adapters, int R, int B, int H, int k, int Tn, int D, int d, int dtype, void *q_out,
+                            void *k_compact, int pos0, int Tc_cap, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!adapter_ids || !a_q != !b_q || !a_k != !b_k || (!a_q && !a_k)) return CHAI_ERR_NULL;
+    int st = check_project(x, w_q, w_k, rep_heads, B, H, k, Tn, D, d, dtype, q_out, k_compact, pos0, Tc_cap);
+    if (st != CHAI_OK) return st;
+    if (n_adapters < 1 || R < 1) return CHAI_ERR_SHAPE;
+    if (R % 8 != 0 || R > kMaxAdapterRank) return CHAI_ERR_UNSUPPORTED;
+    if (!aligned16(a_q) || !aligned16(b_q) || !aligned16(a_k) || !aligned16(b_k)) return CHAI_ERR_ALIGN;
+    if (B > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < adapter_workspace_bytes(B, Tn, R)))
+        return CHAI_ERR_WORKSPACE;
+    if (B == 0) return CHAI_OK;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    st = hip_status(launch_adapter_down(x, adapter_ids, a_q, a_k, adapter_scale, n_adapters, R, B, Tn, D, workspace, s));
+    if (st != CHAI_OK) return st;
+    AdapterUse use;
+    use.t = static_cast<const char *>(workspace);
+    use.b_q = static_cast<const char *>(b_q);
+    use.b_k = static_cast<const char *>(b_k);
+    use.ids = adapter_ids;
+    use.n = n_adapters;
+    use.R = R;
+    return hip_status(launch_project_qk_adapted(x, w_q, w_k, rep_heads, B, H, k, Tn, D, q_out, k_compact, pos0, Tc_cap, use, s));
 }
 
 size_t chai_prefill_workspace_bytes(int B, int H, int k, int n_keys)

@@ -58,6 +58,87 @@ __device__ __forceinline__ void unroll(F &&f)
     unroll_seq(f, std::make_integer_sequence<int, N>{});
 }
 
+// Low-rank adapters of the rows' own (chai_project_qk_adapted): the kernels below add t B_a^T to a token's products, where t = s_a x A_a^T
+// [R] of the token, made before (adapter.hip), is held as two bf16, t = hi + lo to 2^-17 of it (16 bits of 24: the product's sum is
+// rounded to 8), sixteen ranks' hi and their lo one behind the other: a chunk of 32 is a product's depth, and meets the sixteen columns
+// of B_a twice.  NoAdapters: the kernels as they are without.
+struct NoAdapters {
+    static constexpr bool any = false;
+};
+struct Adapters : AdapterUse {
+    static constexpr bool any = true;
+    __device__ __forceinline__ int of(int b) const              // adapter of row b, -1: none
+    {
+        const int id = ids[b];
+        return (unsigned int)id < (unsigned int)n ? id : -1;
+    }
+    // lane group g's eight ranks of chunk c
+    __device__ __forceinline__ bool inside(int c, int g) const { return c * 16 + (g & 1) * 8 < R; }
+    __device__ __forceinline__ const char *token(size_t token, int part) const { return t + (token * 2 + part) * (size_t)(chunks() * 64); }
+    __device__ __forceinline__ const char *column(int part, int a, int H, int head, int f) const
+    {
+        return (part == 0 ? b_q : b_k) + (((size_t)a * H + head) * kHeadDim + f) * (size_t)(R * 2);
+    }
+    __device__ __forceinline__ u32x4 token_piece(const char *row, int c, int g) const
+    {
+        return inside(c, g) ? *reinterpret_cast<const u32x4 *>(row + c * 64 + g * 16) : u32x4{0u, 0u, 0u, 0u};
+    }
+    __device__ __forceinline__ u32x4 column_piece(const char *row, int c, int g) const
+    {
+        return inside(c, g) ? *reinterpret_cast<const u32x4 *>(row + c * 32 + (g & 1) * 16) : u32x4{0u, 0u, 0u, 0u};
+    }
+};
+
+// The adapters' part of NB x TT tiles of 16 features x 16 tokens (lane: feature or token lane % 16, eight ranks of four): features f0 ..
+// of head's 256, of which n_cols are wanted; token tok[t] of row b[t].  The tokens may be of rows with different adapters: one after the
+// other is multiplied with all of them, and kept where it is the token's own (what another's columns or ranks hold, infinities and NaN
+// among it, reaches nobody else).  WAVES waves with sums of their own deal (adapter, part, chunk) out among themselves.
+template <int WAVES, int NB, int TT>
+__device__ __forceinline__ void add_adapters(const Adapters &ad, f32x4 (&acc)[NB][TT], const int (&b)[TT], const int (&tok)[TT], int Tn, int H,
+                                             int head, int f0, int n_cols, int w, int lane)
+{
+    const int col = lane & 15, g = lane >> 4;
+    int id[TT];
+    unsigned long long left[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        id[t] = ad.of(b[t]);
+        left[t] = __ballot(id[t] >= 0);
+    }
+    int turn = 0;
+    for (;;) {
+        int a = -1;
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+            if (a < 0 && left[t] != 0ull) a = __builtin_amdgcn_readlane(id[t], __ffsll((long long)left[t]) - 1);
+        if (a < 0) break;
+#pragma unroll
+        for (int t = 0; t < TT; ++t) left[t] &= ~__ballot(id[t] == a);
+        for (int part = 0; part < 2; ++part) {
+            const int lo = max(f0, part * kHeadDim), hi = min(f0 + n_cols, (part + 1) * kHeadDim);
+            if ((part == 0 ? ad.b_q : ad.b_k) == nullptr || lo >= hi) continue;
+            for (int c = 0; c < ad.chunks(); ++c) {
+                if (turn++ % WAVES != w) continue;
+                Frag x[TT], y[NB];
+#pragma unroll
+                for (int t = 0; t < TT; ++t) x[t].raw = ad.token_piece(ad.token((size_t)b[t] * Tn + tok[t], part), c, g);
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+                    y[n].raw = ad.column_piece(ad.column(part, a, H, head, min(max(f0 + n * 16 + col, lo), hi - 1) - part * kHeadDim), c, g);
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int t = 0; t < TT; ++t) {
+                        const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n].bf, x[t].bf, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                        const bool own = id[t] == a && (f0 + n * 16 + g * 4) / kHeadDim == part;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[n][t][e] = own ? acc[n][t][e] + d[e] : acc[n][t][e];
+                    }
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------------------------------
 // Prompts.  A tile is 256 tokens x 256 columns, the 128 query and the 128 key columns of one representative, which share the
 // activations.  Four waves, one per SIMD, own 128 x 128 of it each (all 256 accumulation registers): 16 products of 16 x 16 x 32
@@ -81,11 +162,12 @@ __device__ __forceinline__ void unroll(F &&f)
 // One workgroup per CU takes several (batch row, token tile, slot) items one after the other.  Items are numbered slot first and
 // dealt to the XCDs in contiguous ranges: the slots of a token tile read the same activations and find them in L2.
 // ---------------------------------------------------------------------------------------------------------
+template <typename A>
 __global__ __launch_bounds__(kJBlock, 1) void project_kernel(const char *__restrict__ x, const char *__restrict__ w_q,
                                                              const char *__restrict__ w_k,
                                                              const int32_t *__restrict__ rep, int H, int k, int Tn, int D,
                                                              int n_mt, unsigned n_items, char *__restrict__ q_out,
-                                                             char *__restrict__ k_compact, int pos0, int Tc_cap)
+                                                             char *__restrict__ k_compact, int pos0, int Tc_cap, A ad)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -234,6 +316,30 @@ __global__ __launch_bounds__(kJBlock, 1) void project_kernel(const char *__restr
         stage(std::true_type{});
         for (int s = 1; s < n_steps; ++s) stage(std::false_type{});
 
+        // The row's adapter: fragments straight from memory, into the places that the next tile's second half will take.
+        if constexpr (A::any) {
+            const int id = __builtin_amdgcn_readfirstlane(ad.of(now.b));
+            if (id >= 0 && (wn == 0 ? ad.b_q : ad.b_k) != nullptr) {
+                for (int c = 0; c < ad.chunks(); ++c) {
+                    int l2 = lane;
+#if defined(__HIP_DEVICE_COMPILE__)
+                    asm volatile("" : "+v"(l2));     // addresses are made here, not kept in registers all the time
+#endif
+                    const int r2 = l2 & 15, g2 = l2 >> 4;
+                    const char *cols = ad.column(wn, id, H, now.head, r2);
+                    unroll<8>([&](auto nb) { fa[1][decltype(nb)::value].raw = ad.column_piece(cols + decltype(nb)::value * 16 * (size_t)(ad.R * 2), c, g2); });
+                    unroll<8>([&](auto tb) {
+                        const int tok = min(now.t0 + wm * 128 + decltype(tb)::value * 16 + r2, Tn - 1);
+                        fb[1][decltype(tb)::value].raw = ad.token_piece(ad.token((size_t)now.b * Tn + tok, wn), c, g2);
+                    });
+                    unroll<64>([&](auto nc) {
+                        constexpr int n = decltype(nc)::value, nb = n >> 3, tb = (nb & 1) ? 7 - (n & 7) : n & 7;
+                        acc[nb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][nb].bf, fb[1][tb].bf, acc[nb][tb], 0, 0, 0);
+                    });
+                }
+            }
+        }
+
         // D[4*g + v][r]: this lane's token is t0 + wm*128 + tb*16 + r, its features nb*16 + 4*g .. +3.
         // 32 tokens at a time through LDS (piece p of token row R in slot p ^ (R & 15)), so that whole rows are stored.
         char *const strip = lds + 2 * kJStageBytes + w * kJOutBytes;
@@ -322,12 +428,13 @@ constexpr int kJrWaves = 8, kJrBlocks = 4;
 constexpr int kJrTokens = 8;                 // tokens of all rows up to which this kernel is faster than 64-token tiles
 constexpr int kJrParts = kJCol / 16;                 // workgroups per head
 
+template <typename A>
 __global__ __launch_bounds__(kJrWaves * 64) void project_rows_kernel(const char *__restrict__ x,
                                                                      const char *__restrict__ w_q,
                                                                      const char *__restrict__ w_k,
                                                                      const int32_t *__restrict__ rep, int B, int H, int k,
                                                                      int Tn, int D, char *__restrict__ q_out,
-                                                                     char *__restrict__ k_compact, int pos0, int Tc_cap)
+                                                                     char *__restrict__ k_compact, int pos0, int Tc_cap, A ad)
 {
     __shared__ int slots[kJtMaxSlots];
     __shared__ int wave_slots[kJrWaves];
@@ -362,6 +469,12 @@ __global__ __launch_bounds__(kJrWaves * 64) void project_rows_kernel(const char 
         Block bl[kJrBlocks];
 #pragma unroll
         for (int u = 0; u < kJrBlocks; ++u) request(bl[u], w + u * kJrWaves);
+        if constexpr (A::any) {
+            f32x4 tile[1][1] = {{acc}};
+            const int bt[1] = {sl / k}, tt[1] = {tok};
+            add_adapters<kJrWaves>(ad, tile, bt, tt, Tn, H, head, f0, 16, w, lane);
+            acc = tile[0][0];
+        }
         for (int b0 = w; b0 < n_blk; b0 += kJrBlocks * kJrWaves) {
 #pragma unroll
             for (int u = 0; u < kJrBlocks; ++u) {
@@ -428,12 +541,12 @@ __device__ __forceinline__ unsigned wave_or(unsigned x)
                       __builtin_amdgcn_readlane((int)z, 47) | __builtin_amdgcn_readlane((int)z, 63));
 }
 
-template <int MOST>
+template <int MOST, typename A>
 __global__ __launch_bounds__(kJsWaves * 64) void project_stream_kernel(const char *__restrict__ x, const char *__restrict__ w_q,
                                                                        const char *__restrict__ w_k,
                                                                        const int32_t *__restrict__ rep, int B, int H, int k,
                                                                        int Tn, int D, char *__restrict__ q_out,
-                                                                       char *__restrict__ k_compact, int pos0, int Tc_cap)
+                                                                       char *__restrict__ k_compact, int pos0, int Tc_cap, A ad)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -576,6 +689,17 @@ __global__ __launch_bounds__(kJsWaves * 64) void project_stream_kernel(const cha
 #pragma unroll
         for (int s = 0; s < R - 1; ++s)
             if (s < n_mine) fetch(s, s);
+        if constexpr (A::any) {                      // while those are on their way
+            int bt[TT], tt[TT];
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const int it = min(c0 + t * 16 + col, n_items - 1);  // (beyond this pass' tokens: of no pair that is listed)
+                const int sl = __shfl(listed, it < min(n_items, c0 + 8 * XT) ? it / Tn - c0 / Tn : 0);
+                bt[t] = sl / k;
+                tt[t] = it % Tn;
+            }
+            add_adapters<kJsWaves>(ad, acc, bt, tt, Tn, H, head, f0, U * 8, w, lane);
+        }
         int at = 0;
         for (int s = 0; s < n_mine; ++s) {
             if (s + R - 1 < n_mine) fetch(s + R - 1, at == 0 ? R - 1 : at - 1);
@@ -664,11 +788,11 @@ constexpr size_t kJtLdsBytes = (size_t)kJtTeams * kJtStages * jt_stage_bytes(2);
 
 // One tile: tokens c0 .. c0+63 of the n_items tokens of `head` (listed in slots), columns f0 .. f0 + 64*NB - 1 of its
 // 128 query (0..127) and 128 key (128..255) columns.
-template <int NB>
+template <int NB, typename A>
 __device__ __forceinline__ void project_tile(const char *__restrict__ x, const char *__restrict__ w_q,
                                              const char *__restrict__ w_k, int H, int k, int Tn, int D,
                                              char *__restrict__ q_out, char *__restrict__ k_compact, int pos0, int Tc_cap,
-                                             char *lds, const int *slots, int head, int n_items, int c0, int f0)
+                                             char *lds, const int *slots, int head, int n_items, int c0, int f0, const A &ad)
 {
     constexpr int kStageBytes = jt_stage_bytes(NB);
     constexpr int kLoads = kStageBytes / 1024 / kJtWaves;                // direct loads per wave and stage: 2 + 2*NB
@@ -735,6 +859,36 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
     const int sw = (r >> 1) & 7;                     // fragments start on multiples of 16 rows
     if (my_steps > 0) stage(0, 0);
     if (my_steps > 1) stage(1, 1);
+    if constexpr (A::any) {
+        // As add_adapters, with tiles of 32 features x 32 tokens: hi and lo are a product each.  The teams deal (adapter, chunk) out.
+        const int item = min(c0 + wm * 32 + r, n_items - 1), row = slots[item / Tn] / k, tok = item % Tn, part = f0 < kHeadDim ? 0 : 1;
+        const int id = (part == 0 ? ad.b_q : ad.b_k) != nullptr ? ad.of(row) : -1;
+        const char *const trow = ad.token((size_t)row * Tn + tok, part);
+        int turn = 0;
+        for (unsigned long long left = __ballot(id >= 0); left != 0ull;) {
+            const int a = __builtin_amdgcn_readlane(id, __ffsll((long long)left) - 1);
+            left &= ~__ballot(id == a);
+            for (int c = 0; c < ad.chunks(); ++c) {
+                if ((turn++ & (kJtTeams - 1)) != team) continue;
+                Frag t[2], col[NB];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) t[i].raw = ad.token_piece(trow, c, 2 * i + hl);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                    col[nb].raw = ad.column_piece(ad.column(part, a, H, head, (f0 & (kHeadDim - 1)) + wn * 32 * NB + nb * 32 + r), c, hl);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    f32x16 d;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) d[e] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col[nb].bf, t[i].bf, d, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[nb][e] = id == a ? acc[nb][e] + d[e] : acc[nb][e];
+                }
+            }
+        }
+    }
     int buf = 0;
     for (int s = 0; s < (n_steps + 1) / 2; ++s) {    // both teams: the same number of barriers
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -793,11 +947,12 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
     }
 }
 
+template <typename A>
 __global__ __launch_bounds__(kJtBlock) void project_tile_kernel(const char *__restrict__ x, const char *__restrict__ w_q,
                                                                 const char *__restrict__ w_k,
                                                                 const int32_t *__restrict__ rep, int B, int H, int k,
                                                                 int Tn, int D, char *__restrict__ q_out,
-                                                                char *__restrict__ k_compact, int pos0, int Tc_cap)
+                                                                char *__restrict__ k_compact, int pos0, int Tc_cap, A ad)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     __shared__ int slots[kJtMaxSlots];
@@ -842,9 +997,9 @@ __global__ __launch_bounds__(kJtBlock) void project_tile_kernel(const char *__re
     const int head = mine[0], c0 = mine[1] * kJtTok;
     const int n_items = list_slots<kJtWaves * kJtTeams>(rep, B * k, head, H, slots, wave_sum) * Tn;
     if (parts == 4)
-        project_tile<1>(x, w_q, w_k, H, k, Tn, D, q_out, k_compact, pos0, Tc_cap, lds, slots, head, n_items, c0, item % 4 * 64);
+        project_tile<1>(x, w_q, w_k, H, k, Tn, D, q_out, k_compact, pos0, Tc_cap, lds, slots, head, n_items, c0, item % 4 * 64, ad);
     else
-        project_tile<2>(x, w_q, w_k, H, k, Tn, D, q_out, k_compact, pos0, Tc_cap, lds, slots, head, n_items, c0, item % 2 * 128);
+        project_tile<2>(x, w_q, w_k, H, k, Tn, D, q_out, k_compact, pos0, Tc_cap, lds, slots, head, n_items, c0, item % 2 * 128, ad);
 }
 
 // Measurement aid: 32 x 32 x 16 products alone, the prefill kernels' shape (16 x 16 x 32 ones, project_kernel's, reach a sixth
@@ -954,9 +1109,9 @@ static bool project_streams(int B, int H, int k, int Tn, int D)
     return tokens <= 32 ? std::any_of(std::begin(to32), std::end(to32), within) : std::any_of(std::begin(to64), std::end(to64), within);
 }
 
-int launch_project_qk(const void *x, const void *w_q, const void *w_k, const int32_t *rep, int B, int H, int k, int Tn,
-                      int D, void *q_out, void *k_compact, int pos0, int Tc_cap, const KernelEvents &ev,
-                      hipStream_t stream)
+template <typename A>
+static int launch_project(const void *x, const void *w_q, const void *w_k, const int32_t *rep, int B, int H, int k, int Tn, int D,
+                          void *q_out, void *k_compact, int pos0, int Tc_cap, const A &ad, const KernelEvents &ev, hipStream_t stream)
 {
     const char *xc = static_cast<const char *>(x), *wq = static_cast<const char *>(w_q), *wk = static_cast<const char *>(w_k);
     char *qo = static_cast<char *>(q_out), *ko = static_cast<char *>(k_compact);
@@ -985,16 +1140,16 @@ int launch_project_qk(const void *x, const void *w_q, const void *w_k, const int
         const int heads = H < B * k ? H : B * k, most = heads * ((kJsUnits + kJsMaxUnits - 3) / (kJsMaxUnits - 2));
         const bool few = heads <= kJCus / (kJsUnits / kJsFewUnits);
         const int n_wg = few ? kJCus : (most > 2 * kJCus ? most : 2 * kJCus);
-        auto *kernel = few ? project_stream_kernel<kJsFewUnits> : project_stream_kernel<kJsMaxUnits>;
+        auto *kernel = few ? project_stream_kernel<kJsFewUnits, A> : project_stream_kernel<kJsMaxUnits, A>;
         static DeviceFlags lds_allowed[2];
         const hipError_t attr = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kJsLdsBytes, lds_allowed[few ? 1 : 0]);
         if (attr != hipSuccess) return (int)attr;
         return (int)launch_kernel(kernel, dim3((unsigned int)n_wg), dim3(kJsWaves * 64), kJsLdsBytes, stream, ev, xc, wq, wk, rep, B, H, k, Tn,
-                                  D, qo, ko, pos0, Tc_cap);
+                                  D, qo, ko, pos0, Tc_cap, ad);
     }
     if (listed && (long long)B * Tn <= kJrTokens && H <= 0x7fffffff / kJrParts)
-        return (int)launch_kernel(project_rows_kernel, dim3((unsigned int)H * kJrParts), dim3(kJrWaves * 64), 0, stream, ev,
-                                  xc, wq, wk, rep, B, H, k, Tn, D, qo, ko, pos0, Tc_cap);
+        return (int)launch_kernel(project_rows_kernel<A>, dim3((unsigned int)H * kJrParts), dim3(kJrWaves * 64), 0, stream, ev,
+                                  xc, wq, wk, rep, B, H, k, Tn, D, qo, ko, pos0, Tc_cap, ad);
     // (the tile kernel addresses the activations and one head's weights with 32-bit byte offsets below 2 GiB)
     const long long n_large = (long long)B * k * ((Tn + kJTok - 1) / kJTok);
     const bool one_round = n_large <= 150 && D < 8192;
@@ -1002,25 +1157,40 @@ int launch_project_qk(const void *x, const void *w_q, const void *w_k, const int
     if (listed && items <= most && H <= kJtMaxHeads && (long long)B * Tn * D * 2 < 0x7fffffffLL &&
         (long long)kHeadDim * D * 2 < 0x7fffffffLL) {
         static DeviceFlags tile_lds_allowed;
-        const hipError_t attr = allow_dynamic_lds(reinterpret_cast<const void *>(&project_tile_kernel), kJtLdsBytes,
+        const hipError_t attr = allow_dynamic_lds(reinterpret_cast<const void *>(&project_tile_kernel<A>), kJtLdsBytes,
                                                   tile_lds_allowed);
         if (attr != hipSuccess) return (int)attr;
         // an upper bound of the tiles: the heads' tokens rounded up to whole tiles
         const long long tiles = items / kJtTok + (H < B * k ? H : B * k);
         long long n_wg = 2 * tiles;
         if (n_wg < kJtNarrow) n_wg = 4 * tiles < kJtNarrow ? 4 * tiles : kJtNarrow;
-        return (int)launch_kernel(project_tile_kernel, dim3((unsigned int)((n_wg + 7) / 8 * 8)), dim3(kJtBlock), kJtLdsBytes,
-                                  stream, ev, xc, wq, wk, rep, B, H, k, Tn, D, qo, ko, pos0, Tc_cap);
+        return (int)launch_kernel(project_tile_kernel<A>, dim3((unsigned int)((n_wg + 7) / 8 * 8)), dim3(kJtBlock), kJtLdsBytes,
+                                  stream, ev, xc, wq, wk, rep, B, H, k, Tn, D, qo, ko, pos0, Tc_cap, ad);
     }
     static DeviceFlags lds_allowed;
-    const hipError_t attr = allow_dynamic_lds(reinterpret_cast<const void *>(&project_kernel), kJLdsBytes, lds_allowed);
+    const hipError_t attr = allow_dynamic_lds(reinterpret_cast<const void *>(&project_kernel<A>), kJLdsBytes, lds_allowed);
     if (attr != hipSuccess) return (int)attr;
     const int n_mt = (Tn + kJTok - 1) / kJTok;
     if ((long long)n_mt * k * B > 0x7fffffffLL) return (int)hipErrorInvalidConfiguration;
     const unsigned int n_items = (unsigned int)n_mt * k * B;
     const bool one_each = n_items < kJCus || D < 2 * kJStep;    // (loads run two stages ahead, at most one item)
-    return (int)launch_kernel(project_kernel, dim3(one_each ? (n_items + 7) / 8 * 8 : kJCus), dim3(kJBlock), kJLdsBytes,
-                              stream, ev, xc, wq, wk, rep, H, k, Tn, D, n_mt, n_items, qo, ko, pos0, Tc_cap);
+    return (int)launch_kernel(project_kernel<A>, dim3(one_each ? (n_items + 7) / 8 * 8 : kJCus), dim3(kJBlock), kJLdsBytes,
+                              stream, ev, xc, wq, wk, rep, H, k, Tn, D, n_mt, n_items, qo, ko, pos0, Tc_cap, ad);
+}
+
+int launch_project_qk(const void *x, const void *w_q, const void *w_k, const int32_t *rep, int B, int H, int k, int Tn,
+                      int D, void *q_out, void *k_compact, int pos0, int Tc_cap, const KernelEvents &ev,
+                      hipStream_t stream)
+{
+    return launch_project(x, w_q, w_k, rep, B, H, k, Tn, D, q_out, k_compact, pos0, Tc_cap, NoAdapters{}, ev, stream);
+}
+
+int launch_project_qk_adapted(const void *x, const void *w_q, const void *w_k, const int32_t *rep, int B, int H, int k, int Tn, int D,
+                              void *q_out, void *k_compact, int pos0, int Tc_cap, const AdapterUse &use, hipStream_t stream)
+{
+    Adapters ad;
+    static_cast<AdapterUse &>(ad) = use;
+    return launch_project(x, w_q, w_k, rep, B, H, k, Tn, D, q_out, k_compact, pos0, Tc_cap, ad, KernelEvents{}, stream);
 }
 
 }  // namespace chai

@@ -1,0 +1,197 @@
+"""Projections with a low-rank adapter of every row's own, against products in 64 bits.
+
+Tolerance.  Products of bf16 are exact in fp32; sums of n of them in fp32 are held to 3e-6 of the sum of magnitudes (50 * 2^-24, the bar of
+the projections without adapters, which the sums along the width are).  t = s x A^T carries that error times |B|, is multiplied by the factor
+and held as two bf16: 2^-24 + 2^-17 of it (the second part is the rest of the first, at most 2^-8 of t, rounded to 2^-9 of itself).  The
+result is rounded to bf16 once: half a step of it."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_2403_08058_amd as C
+from adapted_cases import CASES, RANKS
+
+D_HEAD = 128
+BF16 = torch.bfloat16
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+
+
+class Inputs:
+    def __init__(self, seed, B, H, k, Tn, D, R, n, parts="qk", pos0=0, cap=None):
+        g = np.random.default_rng(seed)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(seed)
+        new = lambda std, *s: torch.randn(s, generator=gen, device="cuda").mul_(std).to(BF16)  # noqa: E731
+        self.sizes = (B, H, k, Tn, D, R, n)
+        self.pos0, self.cap = pos0, cap or pos0 + Tn
+        self.x, self.w = new(1.0, B, Tn, D), {p: new(D ** -0.5, H * D_HEAD, D) for p in "qk"}
+        self.a = {p: new(D ** -0.5, n, R, D) if p in parts else None for p in "qk"}
+        self.b = {p: new(R ** -0.5, n, H * D_HEAD, R) if p in parts else None for p in "qk"}
+        self.rep = np.stack([g.permutation(H)[:k] for _ in range(B)])
+        self.rep[g.random((B, k)) < 0.15] = -1
+        self.ids = g.integers(-1, n, B)
+        self.scale = torch.from_numpy(g.uniform(0.25, 2.0, n).astype(np.float32)).cuda()
+
+    def run(self, plain=False, scale=True, stream=None, out=None, workspace=None):
+        B, H, k, Tn, D, R, n = self.sizes
+        q, kc = out or (torch.full((B, H, Tn, D_HEAD), 7.0, dtype=BF16, device="cuda"), torch.full((B, k, self.cap, D_HEAD), 9.0, dtype=BF16, device="cuda"))
+        if plain:
+            C.chai_project_qk(self.x, self.w["q"], self.w["k"], dev(self.rep), q, kc, self.pos0)
+        else:
+            if workspace is None:
+                workspace = C.alloc_adapted_workspace(B, Tn, R)
+                workspace.fill_(0xFF)
+            C.chai_project_qk_adapted(self.x, self.w["q"], self.w["k"], dev(self.rep), dev(self.ids), self.a["q"], self.b["q"], self.a["k"],
+                                      self.b["k"], self.scale if scale else None, q, kc, self.pos0, workspace, stream=stream)
+        torch.cuda.synchronize()
+        return q, kc
+
+    def check(self, q, kc, rows=None, scale=True, bits=None):
+        """Against 64 bits; rows whose slots are checked (None: all).  What must not be written is not."""
+        B, H, k, Tn, D, R, n = self.sizes
+        nearest = total = 0
+        for b in range(B):
+            used = self.rep[b][self.rep[b] >= 0]
+            others = np.setdiff1d(np.arange(H), used)
+            assert bool((q[b, others] == 7.0).all()), "rows of other heads"
+            assert bool((kc[b, self.rep[b] < 0] == 9.0).all()), "slots without a cluster"
+            assert bool((kc[b, :, :self.pos0] == 9.0).all()) and bool((kc[b, :, self.pos0 + Tn:] == 9.0).all())
+            if rows is not None and b not in rows:
+                continue
+            x = self.x[b].double()
+            a = int(self.ids[b])
+            for p in "qk":
+                t = mag_t = None
+                if self.a[p] is not None and 0 <= a < n:
+                    s = float(self.scale[a]) if scale else 1.0
+                    down = self.a[p][a].double().t().contiguous()
+                    t, mag_t = s * (x @ down), s * (x.abs() @ down.abs())
+                for j in range(k):
+                    r = int(self.rep[b, j])
+                    if r < 0:
+                        continue
+                    cols = slice(r * D_HEAD, (r + 1) * D_HEAD)
+                    w = self.w[p][cols].double().t().contiguous()
+                    want, allowed = x @ w, 3e-6 * (x.abs() @ w.abs())
+                    if t is not None:
+                        up = self.b[p][a, cols].double().t().contiguous()
+                        want = want + t @ up
+                        allowed = allowed + (3e-6 * mag_t) @ up.abs() + (2.0 ** -17 + 2.0 ** -24 + 3e-6) * (t.abs() @ up.abs())
+                    step = 2.0 ** (torch.floor(torch.log2(want.abs().clamp(min=2.0 ** -126))) - 8)
+                    got = (q[b, r] if p == "q" else kc[b, j, self.pos0:self.pos0 + Tn]).double()
+                    off = (got - want).abs()
+                    assert bool((off <= step + allowed).all()), (b, j, p, float((off / (step + allowed)).max()))
+                    nearest += int((off <= step * (1 + 1e-9)).sum())
+                    total += off.numel()
+        # most are the nearest; the others lie where an error of 2^-17 of the adapter's part decides
+        assert total == 0 or nearest / total > 0.98
+
+
+ALL = [(kernel, *c, R) for kernel, cases in CASES.items() for i, c in enumerate(cases) for R in (RANKS if i == 0 else [16, 128])]
+
+
+@pytest.mark.parametrize("kernel,B,H,k,Tn,D,R", ALL)
+def test_every_kernel(kernel, B, H, k, Tn, D, R):
+    print(f"[adapted] {kernel} {B} x {Tn} tokens, {k} of {H}, width {D}, rank {R}", flush=True)
+    x = Inputs(B * 3 + Tn + R, B, H, k, Tn, D, R, n=max(2, B * 2 // 3), pos0=3)
+    if B > 3:
+        x.rep[2, :] = x.rep[3, :]                          # rows of one head with adapters of their own
+        x.ids[2], x.ids[3] = 0, 1
+    q, kc = x.run()
+    x.check(q, kc, rows=range(B) if B <= 16 else [0, 2, 3, B // 2, B - 1])
+    plain_q, plain_k = x.run(plain=True)
+    bare = np.flatnonzero(x.ids < 0)                       # without an adapter: the projections' own bits
+    assert torch.equal(q[bare], plain_q[bare]) and torch.equal(kc[bare], plain_k[bare])
+
+
+@pytest.mark.parametrize("kernel", CASES)
+@pytest.mark.parametrize("parts", ["q", "k"])
+def test_one_part_alone(kernel, parts):
+    B, H, k, Tn, D = CASES[kernel][1]
+    x = Inputs(77, B, H, k, Tn, D, 24, n=3, parts=parts)
+    q, kc = x.run(scale=False)
+    x.check(q, kc, rows=[0, B - 1], scale=False)
+    plain_q, plain_k = x.run(plain=True)
+    assert torch.equal(kc, plain_k) if parts == "q" else torch.equal(q, plain_q)
+
+
+@pytest.mark.parametrize("kernel", CASES)
+def test_ids_outside_are_no_adapters(kernel):
+    B, H, k, Tn, D = CASES[kernel][1]
+    x = Inputs(78, B, H, k, Tn, D, 16, n=2)
+    x.ids[:] = [[-1, 2, 1 << 30, -(1 << 31)][b % 4] for b in range(B)]
+    for got, want in zip(x.run(), x.run(plain=True)):
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("kernel", CASES)
+def test_what_one_adapter_holds_reaches_no_other_row(kernel):
+    """Infinities and NaN in one adapter and in one row's activations: the other rows keep their bits."""
+    B, H, k, Tn, D = next(c for c in CASES[kernel] if c[0] > 1)
+    x = Inputs(79, B, H, k, Tn, D, 24, n=3)
+    x.rep[:] = x.rep[0]
+    x.ids[:] = [[0, 1, 2][b % 3] for b in range(B)]
+    clean = x.run()
+    x.a["q"][1, 3, 5], x.b["q"][1, :, 7], x.b["k"][1, :, 0] = float("nan"), float("inf"), float("nan")
+    dirty = x.run()
+    keep = [b for b in range(B) if x.ids[b] != 1]
+    for a, b in zip(clean, dirty):
+        assert torch.equal(a[keep], b[keep])
+    bad = [b for b in range(B) if x.ids[b] == 1]
+    used = x.rep[0][x.rep[0] >= 0]
+    assert bool(torch.isnan(dirty[0][bad][:, used].float()).all())
+
+
+@pytest.mark.parametrize("kernel", ["rows", "stream", "tile"])
+def test_a_head_in_several_slots(kernel):
+    B, H, k, Tn, D = next(c for c in CASES[kernel] if c[2] > 2)
+    x = Inputs(80, B, H, k, Tn, D, 16, n=2)
+    x.rep[:, 1] = x.rep[:, 0] = 1
+    q, kc = x.run()
+    x.check(q, kc, rows=[0, B - 1])
+    assert torch.equal(kc[:, 0], kc[:, 1])
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_drawn_sizes(seed):
+    g = np.random.default_rng(500 + seed)
+    B, H = int(g.integers(1, 20)), int(g.integers(1, 40))
+    k, Tn = int(g.integers(1, H + 1)), int(g.integers(1, 90))
+    D, R = 64 * int(g.integers(1, 40)), 8 * int(g.integers(1, 17))
+    print(f"[adapted] drawn {B} x {Tn}, {k} of {H}, width {D}, rank {R}", flush=True)
+    x = Inputs(seed, B, H, k, Tn, D, R, n=int(g.integers(1, 2 * B + 1)), pos0=int(g.integers(0, 5)), cap=Tn + 9)
+    q, kc = x.run()
+    x.check(q, kc, rows=[0, B // 2, B - 1])
+
+
+@pytest.mark.parametrize("kernel", CASES)
+def test_recorded_and_on_another_stream(kernel):
+    B, H, k, Tn, D = CASES[kernel][1]
+    x = Inputs(81, B, H, k, Tn, D, 16, n=3)
+    want = x.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for a, b in zip(x.run(stream=side), want):
+        assert torch.equal(a, b)
+    q, kc = torch.full_like(want[0], 7.0), torch.full_like(want[1], 9.0)
+    ws, rep, ids = C.alloc_adapted_workspace(B, Tn, 16), dev(x.rep), dev(x.ids)
+    call = lambda: C.chai_project_qk_adapted(x.x, x.w["q"], x.w["k"], rep, ids, x.a["q"], x.b["q"], x.a["k"], x.b["k"], x.scale, q, kc, 0, ws)  # noqa: E731
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    g = np.random.default_rng(82)
+    for _ in range(3):
+        ids.copy_(dev(g.integers(-1, 3, B)))
+        x.x.mul_(-1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = q.clone(), kc.clone()
+        ws.fill_(0xFF)
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], q) and torch.equal(got[1], kc)
