@@ -79,13 +79,21 @@ struct Adapters : AdapterUse {
     {
         return (part == 0 ? b_q : b_k) + (((size_t)a * H + head) * kHeadDim + f) * (size_t)(R * 2);
     }
+    // (ranks behind the last one: 0, read elsewhere; without branches, whose masks would cost registers)
+    __device__ __forceinline__ u32x4 only(bool in, u32x4 x) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = in ? x[e] : 0u;
+        return x;
+    }
     __device__ __forceinline__ u32x4 token_piece(const char *row, int c, int g) const
     {
-        return inside(c, g) ? *reinterpret_cast<const u32x4 *>(row + c * 64 + g * 16) : u32x4{0u, 0u, 0u, 0u};
+        return only(inside(c, g), *reinterpret_cast<const u32x4 *>(row + c * 64 + g * 16));
     }
     __device__ __forceinline__ u32x4 column_piece(const char *row, int c, int g) const
     {
-        return inside(c, g) ? *reinterpret_cast<const u32x4 *>(row + c * 32 + (g & 1) * 16) : u32x4{0u, 0u, 0u, 0u};
+        const bool in = inside(c, g);
+        return only(in, *reinterpret_cast<const u32x4 *>(row + c * 32 + (in ? (g & 1) * 16 : 0)));
     }
 };
 
@@ -162,12 +170,14 @@ __device__ __forceinline__ void add_adapters(const Adapters &ad, f32x4 (&acc)[NB
 // One workgroup per CU takes several (batch row, token tile, slot) items one after the other.  Items are numbered slot first and
 // dealt to the XCDs in contiguous ranges: the slots of a token tile read the same activations and find them in L2.
 // ---------------------------------------------------------------------------------------------------------
+// `given`, the first argument, is read from where the arguments lie when a tile needs it: kept in registers from the kernel's start, its
+// ten words put others away inside the loop over stages, whose reading back waits for every load under way (16 rows x 2043 tokens 974 us).
 template <typename A>
-__global__ __launch_bounds__(kJBlock, 1) void project_kernel(const char *__restrict__ x, const char *__restrict__ w_q,
+__global__ __launch_bounds__(kJBlock, 1) void project_kernel(A given, const char *__restrict__ x, const char *__restrict__ w_q,
                                                              const char *__restrict__ w_k,
                                                              const int32_t *__restrict__ rep, int H, int k, int Tn, int D,
                                                              int n_mt, unsigned n_items, char *__restrict__ q_out,
-                                                             char *__restrict__ k_compact, int pos0, int Tc_cap, A ad)
+                                                             char *__restrict__ k_compact, int pos0, int Tc_cap)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -318,6 +328,13 @@ __global__ __launch_bounds__(kJBlock, 1) void project_kernel(const char *__restr
 
         // The row's adapter: fragments straight from memory, into the places that the next tile's second half will take.
         if constexpr (A::any) {
+#if defined(__HIP_DEVICE_COMPILE__)
+            const auto *arguments = __builtin_amdgcn_kernarg_segment_ptr();
+            asm volatile("" : "+s"(arguments));
+            const A ad = *(const __attribute__((address_space(4))) A *)arguments;
+#else
+            const A ad = given;
+#endif
             const int id = __builtin_amdgcn_readfirstlane(ad.of(now.b));
             if (id >= 0 && (wn == 0 ? ad.b_q : ad.b_k) != nullptr) {
                 for (int c = 0; c < ad.chunks(); ++c) {
@@ -353,6 +370,15 @@ __global__ __launch_bounds__(kJBlock, 1) void project_kernel(const char *__restr
 #endif
         const int wr = l & 15, wp = l >> 5, wh = (l >> 4 & 1) * 8, rd = l >> 4, rp = l & 15;
         unroll<4>([&](auto tc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+            // The sums of these tokens leave the accumulation registers here and not before: all at once they would take the registers of
+            // addresses, which would then be read back inside the loop over stages (see `given`).
+            if constexpr (A::any)
+                unroll<16>([&](auto i) {
+                    f32x4 &sum = acc[decltype(i)::value & 7][2 * decltype(tc)::value + (decltype(i)::value >> 3)];
+                    asm volatile("" : "+a"(sum));
+                });
+#endif
 #pragma unroll
             for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
@@ -1175,7 +1201,7 @@ static int launch_project(const void *x, const void *w_q, const void *w_k, const
     const unsigned int n_items = (unsigned int)n_mt * k * B;
     const bool one_each = n_items < kJCus || D < 2 * kJStep;    // (loads run two stages ahead, at most one item)
     return (int)launch_kernel(project_kernel<A>, dim3(one_each ? (n_items + 7) / 8 * 8 : kJCus), dim3(kJBlock), kJLdsBytes,
-                              stream, ev, xc, wq, wk, rep, H, k, Tn, D, n_mt, n_items, qo, ko, pos0, Tc_cap, ad);
+                              stream, ev, ad, xc, wq, wk, rep, H, k, Tn, D, n_mt, n_items, qo, ko, pos0, Tc_cap);
 }
 
 int launch_project_qk(const void *x, const void *w_q, const void *w_k, const int32_t *rep, int B, int H, int k, int Tn,
