@@ -40,7 +40,7 @@ __device__ __forceinline__ void unroll(F &&f)
     unroll_seq(f, std::make_integer_sequence<int, N>{});
 }
 
-constexpr int kAdWaveBytes = 20 * 1024;              // ring of a wave
+constexpr int wave_bytes(int waves) { return waves > 8 ? 10 * 1024 : 20 * 1024; }      // ring of a wave
 constexpr int kAdMostAhead = 8;
 
 template <int U, int XT, int WAVES>
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(WAVES * 64) void adapter_down_kernel(const char *__
                                                                   const float *__restrict__ scales, int n, int R, int Tn, int D, int tiles,
                                                                   int groups, unsigned int items, char *__restrict__ t)
 {
-    constexpr int NB = (U + 1) / 2, TT = (XT + 1) / 2, kLoads = U + XT, kBytes = kLoads * 1024;
+    constexpr int NB = (U + 1) / 2, TT = (XT + 1) / 2, kLoads = U + XT, kBytes = kLoads * 1024, kAdWaveBytes = wave_bytes(WAVES);
     constexpr int N = kAdWaveBytes / kBytes < kAdMostAhead ? kAdWaveBytes / kBytes : kAdMostAhead;       // blocks of a ring
     static_assert(N >= 2 && NB * TT * 1024 <= kAdWaveBytes, "a block ahead; the sums fit");
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -179,7 +179,7 @@ int launch_down(const char *x, const int32_t *ids, const char *a_q, const char *
     const long long n_tiles = (long long)B * tiles, items = n_tiles * groups, grid = (n_tiles + 7) / 8 * 8 * groups;
     if (grid > 0x7fffffffll) return (int)hipErrorInvalidConfiguration;
     static DeviceFlags lds_allowed;
-    const size_t lds = (size_t)WAVES * kAdWaveBytes;
+    const size_t lds = (size_t)WAVES * wave_bytes(WAVES);
     const auto kernel = adapter_down_kernel<U, XT, WAVES>;
     const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds, lds_allowed);
     if (e != hipSuccess) return (int)e;
@@ -196,8 +196,12 @@ int launch_adapter_down(const void *x_, const int32_t *ids, const void *a_q_, co
 {
     const char *x = static_cast<const char *>(x_), *a_q = static_cast<const char *>(a_q_), *a_k = static_cast<const char *>(a_k_);
     char *t = static_cast<char *>(t_);
-    if (Tn <= 8) return launch_down<1, 1, 8>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
-    if (Tn <= 64) return launch_down<2, 2, 8>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
+    // Few tokens of a row: as many workgroups as there are eights of ranks and tokens, of sixteen waves (8 rows x 37 tokens, width 9216, rank 8
+    // of queries alone, with the projections 84.7 us; eight waves of 16 ranks x 16 tokens 87.4), while that is a round of the chip (4 x 50 tokens,
+    // rank 64, with 448 of them 31.4, sixteen tokens each 27.4).
+    const long long eights = (long long)B * ((Tn + 7) / 8) * (R / 8) * ((a_q ? 1 : 0) + (a_k ? 1 : 0));
+    if (Tn <= 8 || (Tn <= 64 && eights <= 256)) return launch_down<1, 1, 16>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
+    if (Tn <= 64) return launch_down<1, 2, 16>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
     return launch_down<4, 4, 4>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
 }
 

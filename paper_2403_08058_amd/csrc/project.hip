@@ -97,52 +97,72 @@ struct Adapters : AdapterUse {
     }
 };
 
+// The different adapters among the lanes' (-1: none) in lanes 0, 1, .. of the result, in order of their first lanes; n of them, at most 64.
+template <int TT>
+__device__ __forceinline__ int list_adapters(const int (&id)[TT], int lane, int &n)
+{
+    int list = -1;
+    n = 0;
+    unsigned long long left[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) left[t] = __ballot(id[t] >= 0);
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+        while (left[t] != 0ull) {
+            const int a = __builtin_amdgcn_readlane(id[t], __ffsll((long long)left[t]) - 1);
+#pragma unroll
+            for (int o = t; o < TT; ++o) left[o] &= ~__ballot(id[o] == a);
+            list = lane == n ? a : list;
+            ++n;
+        }
+    return list;
+}
+
 // The adapters' part of NB x TT tiles of 16 features x 16 tokens (lane: feature or token lane % 16, eight ranks of four): features f0 ..
-// of head's 256, of which n_cols are wanted; token tok[t] of row b[t].  The tokens may be of rows with different adapters: one after the
-// other is multiplied with all of them, and kept where it is the token's own (what another's columns or ranks hold, infinities and NaN
-// among it, reaches nobody else).  WAVES waves with sums of their own deal (adapter, part, chunk) out among themselves.
+// of head's 256, of which n_cols are wanted; token tok[t] of row b[t].  The tokens may be of rows with different adapters: every one of
+// those is multiplied with all of them, and kept where it is the token's own (what another's columns or ranks hold, infinities and NaN
+// among it, reaches nobody else).  WAVES waves with sums of their own deal (part, chunk, adapter) out among themselves.  (64 rows x 1 token
+// with 64 adapters of rank 16 26.6 us, 17.2 of them without adapters and 6 their first half; 16 x 1 with rank 64 21.8, 14.1 and 4.5.  The
+// columns of two or four adapters asked for at once: 28.1 and 27.9, 23.2 and 26.5.)
 template <int WAVES, int NB, int TT>
 __device__ __forceinline__ void add_adapters(const Adapters &ad, f32x4 (&acc)[NB][TT], const int (&b)[TT], const int (&tok)[TT], int Tn, int H,
                                              int head, int f0, int n_cols, int w, int lane)
 {
     const int col = lane & 15, g = lane >> 4;
-    int id[TT];
-    unsigned long long left[TT];
+    int id[TT], n_list;
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        id[t] = ad.of(b[t]);
-        left[t] = __ballot(id[t] >= 0);
-    }
-    int turn = 0;
-    for (;;) {
-        int a = -1;
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-            if (a < 0 && left[t] != 0ull) a = __builtin_amdgcn_readlane(id[t], __ffsll((long long)left[t]) - 1);
-        if (a < 0) break;
-#pragma unroll
-        for (int t = 0; t < TT; ++t) left[t] &= ~__ballot(id[t] == a);
-        for (int part = 0; part < 2; ++part) {
-            const int lo = max(f0, part * kHeadDim), hi = min(f0 + n_cols, (part + 1) * kHeadDim);
-            if ((part == 0 ? ad.b_q : ad.b_k) == nullptr || lo >= hi) continue;
-            for (int c = 0; c < ad.chunks(); ++c) {
-                if (turn++ % WAVES != w) continue;
-                Frag x[TT], y[NB];
+    for (int t = 0; t < TT; ++t) id[t] = ad.of(b[t]);
+    const int list = list_adapters<TT>(id, lane, n_list);
+    int first = w;                                       // the wave's next adapter of the list, for this part and chunk
+    for (int part = 0; part < 2; ++part) {
+        const int lo = max(f0, part * kHeadDim), hi = min(f0 + n_cols, (part + 1) * kHeadDim);
+        if ((part == 0 ? ad.b_q : ad.b_k) == nullptr || lo >= hi) continue;
+        for (int c = 0; c < ad.chunks(); ++c) {
+            int i = first;
+            if (i < n_list) {
+                Frag x[TT];
 #pragma unroll
                 for (int t = 0; t < TT; ++t) x[t].raw = ad.token_piece(ad.token((size_t)b[t] * Tn + tok[t], part), c, g);
+                for (; i < n_list; i += WAVES) {
+                    const int a = __builtin_amdgcn_readlane(list, i);
+                    Frag y[NB];
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
-                    y[n].raw = ad.column_piece(ad.column(part, a, H, head, min(max(f0 + n * 16 + col, lo), hi - 1) - part * kHeadDim), c, g);
+                    for (int n = 0; n < NB; ++n)
+                        y[n].raw = ad.column_piece(ad.column(part, a, H, head, min(max(f0 + n * 16 + col, lo), hi - 1) - part * kHeadDim), c, g);
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
+                    for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int t = 0; t < TT; ++t) {
-                        const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n].bf, x[t].bf, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                        const bool own = id[t] == a && (f0 + n * 16 + g * 4) / kHeadDim == part;
+                        for (int t = 0; t < TT; ++t) {
+                            const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n].bf, x[t].bf, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                            const bool own = id[t] == a && (f0 + n * 16 + g * 4) / kHeadDim == part;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[n][t][e] = own ? acc[n][t][e] + d[e] : acc[n][t][e];
-                    }
+                            for (int e = 0; e < 4; ++e) acc[n][t][e] = own ? acc[n][t][e] + d[e] : acc[n][t][e];
+                        }
+                }
             }
+            // the next part or chunk goes on with the wave behind the one that took the list's last
+            first -= n_list;
+            first = first < 0 ? (first & (WAVES - 1)) : first;
         }
     }
 }
@@ -886,33 +906,39 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
     if (my_steps > 0) stage(0, 0);
     if (my_steps > 1) stage(1, 1);
     if constexpr (A::any) {
-        // As add_adapters, with tiles of 32 features x 32 tokens: hi and lo are a product each.  The teams deal (adapter, chunk) out.
+        // As add_adapters, with tiles of 32 features x 32 tokens: hi and lo are a product each.  The teams deal (chunk, adapter) out.
         const int item = min(c0 + wm * 32 + r, n_items - 1), row = slots[item / Tn] / k, tok = item % Tn, part = f0 < kHeadDim ? 0 : 1;
-        const int id = (part == 0 ? ad.b_q : ad.b_k) != nullptr ? ad.of(row) : -1;
+        const int id[1] = {(part == 0 ? ad.b_q : ad.b_k) != nullptr ? ad.of(row) : -1};
+        int n_list;
+        const int list = list_adapters<1>(id, lane, n_list);
         const char *const trow = ad.token((size_t)row * Tn + tok, part);
-        int turn = 0;
-        for (unsigned long long left = __ballot(id >= 0); left != 0ull;) {
-            const int a = __builtin_amdgcn_readlane(id, __ffsll((long long)left) - 1);
-            left &= ~__ballot(id == a);
-            for (int c = 0; c < ad.chunks(); ++c) {
-                if ((turn++ & (kJtTeams - 1)) != team) continue;
-                Frag t[2], col[NB];
+        const int f = (f0 & (kHeadDim - 1)) + wn * 32 * NB + r;
+        int first_of = team;
+        for (int c = 0; c < ad.chunks(); ++c) {
+            int i = first_of;
+            if (i < n_list) {
+                Frag t[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) t[i].raw = ad.token_piece(trow, c, 2 * i + hl);
+                for (int e = 0; e < 2; ++e) t[e].raw = ad.token_piece(trow, c, 2 * e + hl);
+                for (; i < n_list; i += kJtTeams) {
+                    const int a = __builtin_amdgcn_readlane(list, i);
+                    Frag col[NB];
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-                    col[nb].raw = ad.column_piece(ad.column(part, a, H, head, (f0 & (kHeadDim - 1)) + wn * 32 * NB + nb * 32 + r), c, hl);
+                    for (int nb = 0; nb < NB; ++nb) col[nb].raw = ad.column_piece(ad.column(part, a, H, head, f + nb * 32), c, hl);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    f32x16 d;
+                    for (int nb = 0; nb < NB; ++nb) {
+                        f32x16 d;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) d[e] = 0.f;
+                        for (int e = 0; e < 16; ++e) d[e] = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col[nb].bf, t[i].bf, d, 0, 0, 0);
+                        for (int e = 0; e < 2; ++e) d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col[nb].bf, t[e].bf, d, 0, 0, 0);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[nb][e] = id == a ? acc[nb][e] + d[e] : acc[nb][e];
+                        for (int e = 0; e < 16; ++e) acc[nb][e] = id[0] == a ? acc[nb][e] + d[e] : acc[nb][e];
+                    }
                 }
             }
+            first_of -= n_list;
+            first_of = first_of < 0 ? (first_of & (kJtTeams - 1)) : first_of;
         }
     }
     int buf = 0;
