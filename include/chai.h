@@ -689,31 +689,34 @@ int chai_rotate_qk(const void *q, const void *k, int64_t q_head_stride, int64_t 
  * chai_paged_append_packed: N tokens one behind the other, of any rows, into
  * pages; queries and keys are turned on the way, as by chai_rotate_qk (rot = 0:
  * as they are; freq and positions are not read then).
- *     q      element (n,h,c) at n*q_token_stride + h*d + c
- *     k_new  element (n,h,c) at n*k_token_stride + h*d + c, or, k_by_slot set,
- *            (n,j,c): keys of the representatives alone
- *     v_new  element (n,h,c) at n*v_token_stride + h*d + c
- *     (strides in elements, multiples of 8: parts of one row of a layer's
- *     projections are read in place)
+ *     q      element (n,h,c) at n*q_token_stride + h*q_head_stride + c
+ *     k_new  element (n,h,c) at n*k_token_stride + h*k_head_stride + c, or,
+ *            k_by_slot set, (n,j,c): keys of the representatives alone
+ *     v_new  element (n,h,c) at n*v_token_stride + h*v_head_stride + c
+ *     q_out  element (n,h,c) at n*out_token_stride + h*out_head_stride + c:
+ *            representatives' rows written; may be q itself, with its strides.
+ *            q and q_out may both be NULL.
+ *     (strides in elements, multiples of 8, >= d: parts of one row of a layer's
+ *     projections are read in place, and so is a block [heads,N,d] of one row,
+ *     as chai_project_qk leaves it; rows of a tensor must not overlap)
  *     rep_heads  [B,k], or NULL: every head (k = H)
  *     token_rows, positions, slots  [N] int32, as chai_paged_place_tokens
  *            gives them: nothing of a token is read or written whose row is
  *            outside [0,B), nor pages where its slot is outside
  *            [0,n_pages*page).  Two tokens must not be given the same slot.
- *     q_out  [N,H,d]: representatives' rows written; may be q itself
- *            (q_token_stride = H*d).  q and q_out may both be NULL.
  *   pages, scales, types as chai_paged_append_kv; 8-bit codes are those of the
- *   turned rows of 32 bits.  With one token per row q_out is what
- *   chai_paged_decode_attention takes.
+ *   turned rows of 32 bits.  With one token per row a dense q_out [N,H,d] is
+ *   what chai_paged_decode_attention takes.
  * N = 0 is a no-op.  Limits as for the other calls on pages, n_pages * page <
  * 2^31 besides; N <= 2^24, N * (H + 2k) < 2^34.
  */
-int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new, int64_t q_token_stride,
-                             int64_t k_token_stride, int64_t v_token_stride, int k_by_slot, const int32_t *rep_heads,
-                             const int32_t *token_rows, const int32_t *positions, const int32_t *slots, const double *freq,
-                             void *q_out, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int N, int B, int H,
-                             int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype, float gain,
-                             void *stream);
+int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new, int64_t q_token_stride, int64_t q_head_stride,
+                             int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                             int k_by_slot, const int32_t *rep_heads, const int32_t *token_rows, const int32_t *positions,
+                             const int32_t *slots, const double *freq, void *q_out, int64_t out_token_stride,
+                             int64_t out_head_stride, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int N,
+                             int B, int H, int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype,
+                             float gain, void *stream);
 
 /*
  * chai_project_qk with a low-rank adapter of every row's own beside the shared

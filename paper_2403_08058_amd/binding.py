@@ -104,7 +104,7 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     cd = ctypes.c_double
     L.chai_rotary_frequencies.argtypes = [ci, cd, ci, cd, cd, cd, cd, vp]
     L.chai_rotate_qk.argtypes = [vp, vp, i64, i64, vp, vp, vp] + [ci] * 10 + [cf, vp, vp, vp]
-    L.chai_paged_append_packed.argtypes = [vp] * 3 + [i64] * 3 + [ci] + [vp] * 10 + [ci] * 11 + [cf, vp]
+    L.chai_paged_append_packed.argtypes = [vp] * 3 + [i64] * 6 + [ci] + [vp] * 6 + [i64] * 2 + [vp] * 4 + [ci] * 11 + [cf, vp]
     L.chai_project_adapted_workspace_bytes.restype = sz
     L.chai_project_adapted_workspace_bytes.argtypes = [ci] * 3
     L.chai_project_qk_adapted.argtypes = [vp] * 10 + [ci] * 9 + [vp, vp, ci, ci, vp, sz, vp]
@@ -738,17 +738,16 @@ def chai_rotate_qk(q, k, rep_heads, freq, q_out, k_out, pos0: int, positions=Non
     return q_out, k_out
 
 
-def _tokens_of(fn, name, t, heads, d):
-    """Address and stride from token to token of t [N,heads,d], a dense tensor or a part of wider rows."""
-    N = t.shape[0]
-    if t.shape != (N, heads, d):
-        _misfit(fn, f"{name} {tuple(t.shape)}: [tokens,{heads},{d}] expected")
+def _tokens_of(fn, name, t, N, heads, d, dtype):
+    """Address and strides from token to token and head to head of t [N,heads,d], dense or a view."""
+    if t.shape != (N, heads, d) or t.dtype is not dtype:
+        _misfit(fn, f"{name}: {dtype} of shape {(N, heads, d)} expected, got {t.dtype} {tuple(t.shape)}")
     if not t.is_cuda:
         raise ValueError("libchai takes device tensors")
-    sn, sh, sd = t.stride()
-    if N and (sd != 1 or (heads > 1 and sh != d)):
-        _misfit(fn, f"{name} with strides {t.stride()}: heads of a token must lie one behind the other")
-    return t.data_ptr(), sn if N > 1 else heads * d
+    token, head, one = t.stride()
+    if one != 1:
+        _misfit(fn, f"{name} with strides {t.stride()}: elements of a row must lie one behind the other")
+    return t.data_ptr(), token, head
 
 
 def chai_paged_append_packed(q, k_new, v_new, rep_heads, token_rows, positions, slots, freq, q_out, k_pages, v_pages, k_scales=None,
@@ -757,7 +756,8 @@ def chai_paged_append_packed(q, k_new, v_new, rep_heads, token_rows, positions, 
     """N tokens one behind the other: keys k_new [N,H,d] (or [N,k,d], k_by_slot: the representatives' alone; None: by the shape) and
     values v_new [N,H,d] into their slots of the pages, queries q [N,H,d] of the representatives -> q_out [N,H,d] (may be q; both
     may be None).  Queries and keys are turned by positions times freq [rot/2] (64 bits; None: as they are).  token_rows, positions,
-    slots [N] int32 as chai_paged_place_tokens gives them; rep_heads [B,k], or None for every head (k = H)."""
+    slots [N] int32 as chai_paged_place_tokens gives them; rep_heads [B,k], or None for every head (k = H).  Queries, keys and values may
+    be views (parts of wider rows, or a row's block [heads,N,d] transposed)."""
     fn = "chai_paged_append_packed"
     n_pages, k, page, d = k_pages.shape
     N, H, _ = v_new.shape
@@ -765,21 +765,22 @@ def chai_paged_append_packed(q, k_new, v_new, rep_heads, token_rows, positions, 
     code, pages = _paged_types(fn, dtype, k_pages, v_pages, k_scales, v_scales, n_pages, H, k, page, d)
     if k_by_slot is None:
         k_by_slot = k_new.shape[1] != H
-    if v_new.dtype is not dtype or (q is None) != (q_out is None) or (q is not None and (q.dtype is not dtype or q_out.dtype is not dtype
-                                                                                         or q_out.shape != (N, H, d))):
-        _misfit(fn, "queries, keys and values of one type, and q_out [N,H,d] beside q, expected")
-    if (rep_heads is not None and (rep_heads.dtype is not _I32 or rep_heads.shape[1:] != (k,))) or k_new.shape[0] != N \
-            or any(t is not None and (t.dtype is not _I32 or t.shape != (N,)) for t in (token_rows, positions, slots)):
-        _misfit(fn, "int32 maps for every row, and rows, positions and slots for every token, expected")
+    if (q is None) != (q_out is None):
+        _misfit(fn, "queries with what they are written to")
+    if rep_heads is not None and (rep_heads.dtype is not _I32 or rep_heads.shape[1:] != (k,)):
+        _misfit(fn, f"int32 maps [rows,{k}] expected, got {rep_heads.dtype} {tuple(rep_heads.shape)}")
+    for t in (token_rows, slots) if positions is None else (token_rows, slots, positions):
+        if t.dtype is not _I32 or t.shape != (N,):
+            _misfit(fn, f"int32 rows, positions and slots of {N} tokens expected, got {t.dtype} {tuple(t.shape)}")
     B = rep_heads.shape[0] if rep_heads is not None else _MOST_ROWS      # (without maps a row is only a number that is not below 0)
-    qp, qs = _tokens_of(fn, "q", q, H, d) if q is not None else (None, 0)
-    kp, ks = _tokens_of(fn, "k_new", k_new, k if k_by_slot else H, d)
-    vp, vs = _tokens_of(fn, "v_new", v_new, H, d)
+    qp, qt, qh = _tokens_of(fn, "q", q, N, H, d, dtype) if q is not None else (None, 0, 0)
+    op, ot, oh = _tokens_of(fn, "q_out", q_out, N, H, d, dtype) if q is not None else (None, 0, 0)
+    kp, kt, kh = _tokens_of(fn, "k_new", k_new, N, k if k_by_slot else H, d, dtype)
+    vp, vt, vh = _tokens_of(fn, "v_new", v_new, N, H, d, dtype)
     fp, rot = _freq_of(fn, freq)
-    p = _ptrs((rep_heads, token_rows, positions, slots))
-    o = _ptrs((q_out, k_pages, v_pages, k_scales, v_scales))
-    _check(fn, _lib.chai_paged_append_packed(qp, kp, vp, qs, ks, vs, int(k_by_slot), *p, fp, *o, N, B, H, k, n_pages, page, d, rot, layout,
-                                             code, pages, gain, _stream(stream)))
+    p = _ptrs((rep_heads, token_rows, positions, slots, k_pages, v_pages, k_scales, v_scales))
+    _check(fn, _lib.chai_paged_append_packed(qp, kp, vp, qt, qh, kt, kh, vt, vh, k_by_slot, *p[:4], fp, op, ot, oh, *p[4:], N, B, H, k, n_pages,
+                                             page, d, rot, layout, code, pages, gain, _stream(stream)))
     return q_out
 
 

@@ -865,12 +865,13 @@ int chai_rotate_qk(const void *q, const void *k, int64_t q_head_stride, int64_t 
     return hip_status(launch_rotate(sh, rows, layout, dtype, static_cast<hipStream_t>(stream)));
 }
 
-int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new, int64_t q_token_stride,
-                             int64_t k_token_stride, int64_t v_token_stride, int k_by_slot, const int32_t *rep_heads,
-                             const int32_t *token_rows, const int32_t *positions, const int32_t *slots, const double *freq,
-                             void *q_out, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int N, int B, int H,
-                             int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype, float gain,
-                             void *stream)
+int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new, int64_t q_token_stride, int64_t q_head_stride,
+                             int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                             int k_by_slot, const int32_t *rep_heads, const int32_t *token_rows, const int32_t *positions,
+                             const int32_t *slots, const double *freq, void *q_out, int64_t out_token_stride,
+                             int64_t out_head_stride, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int N,
+                             int B, int H, int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype,
+                             float gain, void *stream)
 {
     if (N != 0 && (!k_new || !v_new || !token_rows || !slots || (rot != 0 && !positions) || (!q != !q_out))) return CHAI_ERR_NULL;
     PagedShape ps;
@@ -880,10 +881,17 @@ int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new
                          rep_heads != nullptr, n_pages, page, 1, d, dtype, cache_dtype, &ps, &pg);
     if (st == CHAI_OK) st = check_turn(rot, layout, dtype, d, freq);
     if (st != CHAI_OK) return st;
-    const int64_t heads = (int64_t)H * d, keys = k_by_slot ? (int64_t)k * d : heads;
     if (N < 0 || (N != 0 && B == 0)) return CHAI_ERR_SHAPE;
-    if (N != 0 && (k_token_stride < keys || v_token_stride < heads || (k_token_stride & 7) || (v_token_stride & 7))) return CHAI_ERR_SHAPE;
-    if (N != 0 && q && (q_token_stride < heads || (q_token_stride & 7) || (q == q_out && q_token_stride != heads))) return CHAI_ERR_SHAPE;
+    // Rows of a tensor lie apart: the heads of a token within its step, or the tokens of a head.  (A stride over one row is not looked
+    // at; products of the others and numbers of rows fit 64 bits.)
+    auto apart = [&](int64_t token, int64_t head, int64_t heads) {
+        auto step = [&](int64_t n, int64_t stride) { return n <= 1 || (stride >= d && stride <= ((int64_t)1 << 38) && (stride & 7) == 0); };
+        return step(N, token) && step(heads, head) && (N <= 1 || heads <= 1 || token >= head * (heads - 1) + d || head >= token * (N - 1) + d);
+    };
+    if (N != 0 && (!apart(k_token_stride, k_head_stride, k_by_slot ? k : H) || !apart(v_token_stride, v_head_stride, H))) return CHAI_ERR_SHAPE;
+    if (N != 0 && q && (!apart(q_token_stride, q_head_stride, H) || !apart(out_token_stride, out_head_stride, H) ||
+                        (q == q_out && (q_token_stride != out_token_stride || q_head_stride != out_head_stride))))
+        return CHAI_ERR_SHAPE;
     if (N > kMaxPagedTokens || (long long)n_pages * page > 0x7fffffffll || (long long)N * ((long long)H + 2ll * k) >= (1ll << 34))
         return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out)) return CHAI_ERR_ALIGN;
@@ -912,6 +920,11 @@ int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new
     rows.q_stride = q_token_stride;
     rows.k_stride = k_token_stride;
     rows.v_stride = v_token_stride;
+    rows.out_stride = out_token_stride;
+    rows.q_head = q_head_stride;
+    rows.k_head = k_head_stride;
+    rows.v_head = v_head_stride;
+    rows.out_head = out_head_stride;
     rows.q_out = static_cast<char *>(q_out);
     rows.k_out = static_cast<char *>(k_pages);
     rows.v_out = static_cast<char *>(v_pages);

@@ -215,6 +215,7 @@ struct TurnShape {
 struct TurnRows {
     const char *q = nullptr, *k = nullptr, *v = nullptr;
     long long q_stride = 0, k_stride = 0, v_stride = 0;  // elements from head to head (blocks) or token to token (packed)
+    long long out_stride = 0, q_head = 0, k_head = 0, v_head = 0, out_head = 0;          // packed: of q_out; from head to head
     char *q_out = nullptr, *k_out = nullptr, *v_out = nullptr;       // (k_out, v_out: caches or pages)
     float *k_scales = nullptr, *v_scales = nullptr;
 };

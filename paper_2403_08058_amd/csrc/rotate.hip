@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kBlock, 7) void turn_kernel(TurnShape sh, TurnRows 
         if (s >= turned) {
             if (!placed) return;
             const int h = s - turned;
-            from = rw.v + ((long long)n * rw.v_stride + h * kHeadDim) * kBytes;
+            from = rw.v + (n * rw.v_stride + h * rw.v_head) * kBytes;
             r.to = in_pages(rw.v_out, sh.H, h);
         } else {
             const bool key = s >= q_streams;
@@ -245,11 +245,11 @@ __global__ __launch_bounds__(kBlock, 7) void turn_kernel(TurnShape sh, TurnRows 
                     for (int o = 0; o < j; ++o)
                         if (min(rep[o], sh.H - 1) == h) return;
                 }
-                from = rw.q + (PACKED ? (long long)n * rw.q_stride + h * kHeadDim : ((long long)b * sh.H + h) * rw.q_stride + (long long)number * kHeadDim) * kBytes;
-                r.to = rw.q_out + (PACKED ? (long long)n * sh.H + h : ((long long)b * sh.H + h) * sh.Tn + number) * kRow;
+                from = rw.q + (PACKED ? n * rw.q_stride + h * rw.q_head : ((long long)b * sh.H + h) * rw.q_stride + (long long)number * kHeadDim) * kBytes;
+                r.to = rw.q_out + (PACKED ? (n * rw.out_stride + h * rw.out_head) * kBytes : (((long long)b * sh.H + h) * sh.Tn + number) * kRow);
             } else if constexpr (PACKED) {
                 if (!placed) return;
-                from = rw.k + ((long long)n * rw.k_stride + (sh.by_slot ? j : h) * kHeadDim) * kBytes;
+                from = rw.k + (n * rw.k_stride + (sh.by_slot ? j : h) * rw.k_head) * kBytes;
                 r.to = in_pages(rw.k_out, sh.k, j);
             } else {
                 from = rw.k + (((long long)b * sh.k + j) * rw.k_stride + (long long)number * kHeadDim) * kBytes;

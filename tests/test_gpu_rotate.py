@@ -277,6 +277,24 @@ def test_packed(layout, rot, cache, B, H, k, N, page, by_slot, dense, wide):
         assert want_scales[i] is None or torch.equal(s["scales"][i], want_scales[i])
 
 
+@pytest.mark.parametrize("cache", ["bf16", "e4m3_f32"])
+@pytest.mark.parametrize("by_slot", [False, True])
+def test_packed_views_of_a_block(cache, by_slot):
+    """A row's blocks [heads,N,128] as the projections leave them, queries turned in place, against the same tokens dense."""
+    B, H, k, N = 1, 6, 3, 37
+    s, t = (packed_case(41, B, H, k, N, 16, cache, by_slot) for _ in range(2))
+    freq = C.chai_rotary_frequencies(96).cuda()
+    views = {n: s[n].transpose(0, 1).contiguous().transpose(0, 1) for n in ("q", "k_new", "v_new")}
+    args = (dev(s["rep"]), dev(s["rows"]), dev(s["pos"]), dev(s["slots"]), freq)
+    s["q_out"].copy_(s["q"])
+    C.chai_paged_append_packed(s["q"], s["k_new"], s["v_new"], *args, s["q_out"], *s["pages"], *s["scales"], k_by_slot=by_slot)
+    C.chai_paged_append_packed(views["q"], views["k_new"], views["v_new"], *args, views["q"], *t["pages"], *t["scales"], k_by_slot=by_slot)
+    torch.cuda.synchronize()
+    assert torch.equal(views["q"], s["q_out"])
+    for i in range(2):
+        assert torch.equal(s["pages"][i], t["pages"][i]) and (s["scales"][i] is None or torch.equal(s["scales"][i], t["scales"][i]))
+
+
 def test_packed_queries_in_place_and_without_queries():
     s, t, u = (packed_case(21, 3, 6, 3, 40, 16, "bf16", False) for _ in range(3))
     freq = C.chai_rotary_frequencies(128).cuda()

@@ -39,8 +39,9 @@ def rotate(**kw):
 
 def packed(**kw):
     return call("chai_paged_append_packed", (
-        ("q", FAKE), ("k_new", FAKE), ("v_new", FAKE), ("q_stride", 32 * 128), ("k_stride", 32 * 128), ("v_stride", 32 * 128),
-        ("k_by_slot", 0), ("rep", FAKE), ("rows", FAKE), ("positions", FAKE), ("slots", FAKE), ("freq", FAKE), ("q_out", 2 * FAKE),
+        ("q", FAKE), ("k_new", FAKE), ("v_new", FAKE), ("q_stride", 32 * 128), ("q_head", 128), ("k_stride", 32 * 128), ("k_head", 128),
+        ("v_stride", 32 * 128), ("v_head", 128), ("k_by_slot", 0), ("rep", FAKE), ("rows", FAKE), ("positions", FAKE), ("slots", FAKE),
+        ("freq", FAKE), ("q_out", 2 * FAKE), ("out_stride", 32 * 128), ("out_head", 128),
         ("k_pages", FAKE), ("v_pages", FAKE), ("k_scales", None), ("v_scales", None), ("N", 5), ("B", 2), ("H", 32), ("k", 8),
         ("n_pages", 40), ("page", 16), ("d", 128), ("rot", 128), ("layout", 0), ("dtype", 1), ("cache_dtype", 1), ("gain", 1.0),
         ("stream", None)), **kw)
@@ -93,10 +94,14 @@ def test_packed_tokens():
     assert packed(dtype=2) == DTYPE and packed(cache_dtype=0) == DTYPE and packed(cache_dtype=2) == NULL
     assert packed(N=-1) == SHAPE and packed(B=0) == SHAPE and packed(k=33) == SHAPE and packed(page=20) == SHAPE
     assert packed(k_stride=8 * 128) == SHAPE and packed(v_stride=32 * 128 - 8) == SHAPE and packed(q_stride=32 * 128 + 4) == SHAPE
-    assert packed(q_out=FAKE, q_stride=33 * 128) == SHAPE
+    assert packed(q_out=FAKE, q_stride=33 * 128) == SHAPE and packed(q_out=FAKE, q_head=256, q_stride=64 * 128) == SHAPE
+    assert packed(v_head=64) == SHAPE and packed(k_head=132) == SHAPE and packed(out_head=0) == SHAPE and packed(v_stride=-128, v_head=640) == SHAPE
+    assert packed(v_stride=1 << 41) == SHAPE
+    # rows of one head one behind the other: five tokens of 128 elements, no fewer
+    assert packed(v_stride=128, v_head=5 * 128 - 8) == SHAPE and packed(k_stride=128, k_head=4 * 128) == SHAPE
     assert packed(rot=136) == SHAPE and packed(layout=-1) == SHAPE and packed(rot=40) == UNSUPPORTED and packed(d=64, rot=64) == UNSUPPORTED
     assert packed(N=(1 << 24) + 1) == UNSUPPORTED and packed(n_pages=1 << 27, H=1, k=1) == UNSUPPORTED and packed(B=4097) == UNSUPPORTED
-    assert packed(N=1 << 24, H=1000, k=1000, q_stride=128000, k_stride=128000, v_stride=128000) == UNSUPPORTED
+    assert packed(N=1 << 24, H=1000, k=1000, q_stride=128000, k_stride=128000, v_stride=128000, out_stride=128000) == UNSUPPORTED
     assert packed(k_new=FAKE + 2) == ALIGN and packed(k_pages=FAKE + 8) == ALIGN and packed(q_out=FAKE + 8) == ALIGN
     assert packed(N=0) == 0 and packed(N=0, B=0, k_new=None, v_new=None, rows=None, positions=None, slots=None) == 0
 
