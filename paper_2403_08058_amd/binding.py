@@ -651,14 +651,14 @@ def chai_paged_place_tokens(counts, seq_lens, block_table, free_pages, n_free, p
     fn = "chai_paged_place_tokens"
     B, max_blocks = block_table.shape
     N, n_pages = slots.shape[0], free_pages.shape[0]
-    for t, shape in ((counts, (B,)), (seq_lens, (B,)), (block_table, (B, max_blocks)), (free_pages, (n_pages,)), (n_free, (1,)),
-                     (new_lens, (B,)), (n_left, (1,)), (granted, (B,)), (offsets, (B + 1,)), (token_rows, (N,)), (positions, (N,)),
-                     (slots, (N,))):
-        if t.dtype is not _I32 or t.shape != shape:
-            _misfit(fn, f"int32 of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
-    p = _ptrs((counts, seq_lens, block_table, free_pages, n_free, new_lens, n_left, granted, offsets, token_rows, positions, slots,
-               workspace))
-    _check(fn, _lib.chai_paged_place_tokens(*p[:5], B, N, n_pages, page, max_blocks, *p[5:], workspace.nbytes, _stream(stream)))
+    ints = (counts, seq_lens, block_table, free_pages, n_free, new_lens, n_left, granted, offsets, token_rows, positions, slots)
+    # (bytes are asked for in one word, shapes in tuples: only where something does not fit)
+    if [t.nbytes for t in ints] != [4 * B, 4 * B, 4 * B * max_blocks, 4 * n_pages, 4, 4 * B, 4, 4 * B, 4 * B + 4, 4 * N, 4 * N, 4 * N] \
+            or any([t.dtype is not _I32 for t in ints]):
+        _misfit(fn, f"int32 arrays of {B} rows, {max_blocks} blocks, {n_pages} pages and {N} tokens expected, got "
+                    f"{[(t.dtype, tuple(t.shape)) for t in ints]}")
+    p = _ptrs(ints)
+    _check(fn, _lib.chai_paged_place_tokens(*p[:5], B, N, n_pages, page, max_blocks, *p[5:], _ptr(workspace), workspace.nbytes, _stream(stream)))
 
 
 def chai_paged_release_pages(keep, seq_lens, block_table, free_pages, n_free, page: int, new_lens, n_left, stream=None):
@@ -683,17 +683,16 @@ def chai_rotary_frequencies(rot: int, theta: float = 10000.0, kind: int = CHAI_R
     return freq
 
 
-def _streams_of(fn, name, t):
+def _streams_of(fn, name, t, B, heads, n, d):
     """Address and stride from head to head of t [B,heads,n,d] whose rows lie one behind the other: a dense tensor, or the same
     positions of every head of one."""
-    B, heads, n, d = t.shape
-    sb, sh, sn, sd = t.stride()
     if not t.is_cuda:
         raise ValueError("libchai takes device tensors")
-    if B * heads * n == 0:
+    if t.is_contiguous():
         return t.data_ptr(), n * d
+    sb, sh, sn, sd = t.stride()
     if heads == 1:
-        sh = sb if B > 1 else n * d
+        sh = sb
     if sd != 1 or (n > 1 and sn != d) or (B > 1 and sb != heads * sh):
         _misfit(fn, f"{name} {tuple(t.shape)} with strides {t.stride()}: rows of a head must lie one behind the other, heads equally far apart")
     return t.data_ptr(), sh
@@ -713,40 +712,47 @@ def chai_rotate_qk(q, k, rep_heads, freq, q_out, k_out, pos0: int, positions=Non
     k_out [B,k,Tc_cap,d] (k may be a view of those), turned by positions [B,Tn] int32 (None: pos0 on) times freq [rot/2] (64 bits).
     q and q_out, or k and k_out, may both be None; rep_heads [B,k], or None for every head (k = H)."""
     fn = "chai_rotate_qk"
-    some = q if q is not None else k
-    if some is None or (q is None) != (q_out is None) or (k is None) != (k_out is None):
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         _misfit(fn, "queries or keys, or both, with what they are written to")
-    B, heads, Tn, d = some.shape
-    dtype = some.dtype
-    code = dtype_code(some)
-    slots = k.shape[1] if k is not None else rep_heads.shape[1] if rep_heads is not None else heads
-    H = q.shape[1] if q is not None else slots      # (of keys alone: heads are not looked at beyond whether a slot has one)
-    if q is not None and (q.shape != (B, H, Tn, d) or q_out.shape != q.shape or q_out.dtype is not dtype or q.dtype is not dtype):
-        _misfit(fn, f"q {tuple(q.shape)} {q.dtype} and q_out {tuple(q_out.shape)} {q_out.dtype} do not fit together")
-    Tc_cap = k_out.shape[2] if k is not None else pos0 + Tn
-    if k is not None and (k.shape != (B, slots, Tn, d) or k.dtype is not dtype or k_out.shape != (B, slots, Tc_cap, d)
-                          or k_out.dtype is not dtype):
-        _misfit(fn, f"k {tuple(k.shape)} {k.dtype} and k_out {tuple(k_out.shape)} {k_out.dtype} do not fit together")
+    qp = kp = None
+    qs = ks = 0
+    if q is not None:
+        shape = q.shape
+        B, H, Tn, d = shape
+        dtype = q.dtype
+        if q_out.shape != shape or q_out.dtype is not dtype:
+            _misfit(fn, f"q {tuple(shape)} {dtype} and q_out {tuple(q_out.shape)} {q_out.dtype} do not fit together")
+        qp, qs = _streams_of(fn, "q", q, B, H, Tn, d)
+    if k is not None:
+        shape = k.shape
+        rows, slots, n, width = shape
+        kind = k.dtype
+        if q is None:
+            B, H, Tn, d, dtype = rows, slots, n, width, kind         # (of keys alone: heads are not looked at beyond whether a slot has one)
+        Tc_cap = k_out.shape[2]
+        if rows != B or n != Tn or width != d or kind is not dtype or k_out.dtype is not dtype or k_out.shape != (B, slots, Tc_cap, d):
+            _misfit(fn, f"k {tuple(shape)} {kind} and k_out {tuple(k_out.shape)} {k_out.dtype} do not fit together")
+        kp, ks = _streams_of(fn, "k", k, B, slots, Tn, d)
+    else:
+        slots, Tc_cap = H if rep_heads is None else rep_heads.shape[1], pos0 + Tn
     if (rep_heads is not None and (rep_heads.dtype is not _I32 or rep_heads.shape != (B, slots))) \
             or (positions is not None and (positions.dtype is not _I32 or positions.shape != (B, Tn))):
         _misfit(fn, "int32 maps and positions for every row expected")
-    qp, qs = _streams_of(fn, "q", q) if q is not None else (None, 0)
-    kp, ks = _streams_of(fn, "k", k) if k is not None else (None, 0)
     fp, rot = _freq_of(fn, freq)
-    _check(fn, _lib.chai_rotate_qk(qp, kp, qs, ks, _ptr(rep_heads), _ptr(positions), fp, B, H, slots, Tn, pos0, Tc_cap, d, rot, layout,
-                                   code, gain, _ptr(q_out), _ptr(k_out), _stream(stream)))
+    code = CHAI_BF16 if dtype is torch.bfloat16 else dtype_code(q if q is not None else k)
+    p = _ptrs((rep_heads, positions, q_out, k_out))
+    _check(fn, _lib.chai_rotate_qk(qp, kp, qs, ks, p[0], p[1], fp, B, H, slots, Tn, pos0, Tc_cap, d, rot, layout, code, gain, p[2], p[3],
+                                   _stream(stream)))
     return q_out, k_out
 
 
-def _tokens_of(fn, name, t, N, heads, d, dtype):
+def _tokens_of(fn, name, t, shape, dtype):
     """Address and strides from token to token and head to head of t [N,heads,d], dense or a view."""
-    if t.shape != (N, heads, d) or t.dtype is not dtype:
-        _misfit(fn, f"{name}: {dtype} of shape {(N, heads, d)} expected, got {t.dtype} {tuple(t.shape)}")
+    token, head, one = t.stride()
+    if t.shape != shape or t.dtype is not dtype or one != 1:
+        _misfit(fn, f"{name}: {dtype} of shape {shape} with rows in one piece expected, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
     if not t.is_cuda:
         raise ValueError("libchai takes device tensors")
-    token, head, one = t.stride()
-    if one != 1:
-        _misfit(fn, f"{name} with strides {t.stride()}: elements of a row must lie one behind the other")
     return t.data_ptr(), token, head
 
 
@@ -760,23 +766,29 @@ def chai_paged_append_packed(q, k_new, v_new, rep_heads, token_rows, positions, 
     be views (parts of wider rows, or a row's block [heads,N,d] transposed)."""
     fn = "chai_paged_append_packed"
     n_pages, k, page, d = k_pages.shape
-    N, H, _ = v_new.shape
+    shape = v_new.shape
+    N, H, _ = shape
     dtype = k_new.dtype
     code, pages = _paged_types(fn, dtype, k_pages, v_pages, k_scales, v_scales, n_pages, H, k, page, d)
-    if k_by_slot is None:
-        k_by_slot = k_new.shape[1] != H
     if (q is None) != (q_out is None):
         _misfit(fn, "queries with what they are written to")
-    if rep_heads is not None and (rep_heads.dtype is not _I32 or rep_heads.shape[1:] != (k,)):
-        _misfit(fn, f"int32 maps [rows,{k}] expected, got {rep_heads.dtype} {tuple(rep_heads.shape)}")
-    for t in (token_rows, slots) if positions is None else (token_rows, slots, positions):
-        if t.dtype is not _I32 or t.shape != (N,):
-            _misfit(fn, f"int32 rows, positions and slots of {N} tokens expected, got {t.dtype} {tuple(t.shape)}")
-    B = rep_heads.shape[0] if rep_heads is not None else _MOST_ROWS      # (without maps a row is only a number that is not below 0)
-    qp, qt, qh = _tokens_of(fn, "q", q, N, H, d, dtype) if q is not None else (None, 0, 0)
-    op, ot, oh = _tokens_of(fn, "q_out", q_out, N, H, d, dtype) if q is not None else (None, 0, 0)
-    kp, kt, kh = _tokens_of(fn, "k_new", k_new, N, k if k_by_slot else H, d, dtype)
-    vp, vt, vh = _tokens_of(fn, "v_new", v_new, N, H, d, dtype)
+    if k_by_slot is None:
+        k_by_slot = k_new.shape[1] != H
+    B = _MOST_ROWS                                         # (without maps a row is only a number that is not below 0)
+    if rep_heads is not None:
+        B = rep_heads.shape[0]
+        if rep_heads.dtype is not _I32 or rep_heads.shape != (B, k):
+            _misfit(fn, f"int32 maps [rows,{k}] expected, got {rep_heads.dtype} {tuple(rep_heads.shape)}")
+    if token_rows.dtype is not _I32 or token_rows.nbytes != 4 * N or slots.dtype is not _I32 or slots.nbytes != 4 * N \
+            or (positions is not None and (positions.dtype is not _I32 or positions.nbytes != 4 * N)):
+        _misfit(fn, f"int32 rows, positions and slots of {N} tokens expected")
+    qp = op = None
+    qt = qh = ot = oh = 0
+    if q is not None:
+        qp, qt, qh = _tokens_of(fn, "q", q, shape, dtype)
+        op, ot, oh = (qp, qt, qh) if q_out is q else _tokens_of(fn, "q_out", q_out, shape, dtype)
+    kp, kt, kh = _tokens_of(fn, "k_new", k_new, (N, k, d) if k_by_slot else shape, dtype)
+    vp, vt, vh = _tokens_of(fn, "v_new", v_new, (N, H, d), dtype)
     fp, rot = _freq_of(fn, freq)
     p = _ptrs((rep_heads, token_rows, positions, slots, k_pages, v_pages, k_scales, v_scales))
     _check(fn, _lib.chai_paged_append_packed(qp, kp, vp, qt, qh, kt, kh, vt, vh, k_by_slot, *p[:4], fp, op, ot, oh, *p[4:], N, B, H, k, n_pages,
@@ -806,12 +818,14 @@ def chai_project_qk_adapted(x, w_q, w_k, rep_heads, adapter_ids, a_q, b_q, a_k, 
         _misfit(fn, "adapters of queries or keys, or both, each of two parts")
     n, R = a.shape[0], a.shape[1]
     dtype = x.dtype
-    for t, shape in ((x, (B, Tn, D)), (w_q, (H * d, D)), (w_k, (H * d, D)), (a_q, (n, R, D)), (a_k, (n, R, D)), (b_q, (n, H * d, R)),
-                     (b_k, (n, H * d, R)), (q_out, (B, H, Tn, d)), (k_compact, (B, k, Tc_cap, d))):
-        if t is not None and (t.shape != shape or t.dtype is not dtype):
-            _misfit(fn, f"{dtype} of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
-    if rep_heads.shape != (B, k) or rep_heads.dtype is not _I32 or adapter_ids.shape != (B,) or adapter_ids.dtype is not _I32 \
-            or (adapter_scale is not None and (adapter_scale.shape != (n,) or adapter_scale.dtype is not _F32)):
+    weights, down, up = (H * d, D), (n, R, D), (n, H * d, R)
+    if w_q.shape != weights or w_k.shape != weights or q_out.shape != (B, H, Tn, d) or k_compact.shape != (B, k, Tc_cap, d) \
+            or w_q.dtype is not dtype or w_k.dtype is not dtype or q_out.dtype is not dtype or k_compact.dtype is not dtype \
+            or (a_q is not None and (a_q.shape != down or b_q.shape != up or a_q.dtype is not dtype or b_q.dtype is not dtype)) \
+            or (a_k is not None and (a_k.shape != down or b_k.shape != up or a_k.dtype is not dtype or b_k.dtype is not dtype)):
+        _misfit(fn, f"{dtype} expected: weights {weights}, adapters {down} and {up}, q_out {(B, H, Tn, d)}, k_compact {(B, k, Tc_cap, d)}")
+    if rep_heads.shape != (B, k) or rep_heads.dtype is not _I32 or adapter_ids.nbytes != 4 * B or adapter_ids.dtype is not _I32 \
+            or (adapter_scale is not None and (adapter_scale.nbytes != 4 * n or adapter_scale.dtype is not _F32)):
         _misfit(fn, "int32 maps and adapters for every row, fp32 factors for every adapter expected")
     p = _ptrs((x, w_q, w_k, rep_heads, adapter_ids, a_q, b_q, a_k, b_k, adapter_scale, q_out, k_compact, workspace))
     _check(fn, _lib.chai_project_qk_adapted(*p[:10], n, R, B, H, k, Tn, D, d, dtype_code(x), p[10], p[11], pos0, Tc_cap, p[12],

@@ -196,13 +196,21 @@ int launch_adapter_down(const void *x_, const int32_t *ids, const void *a_q_, co
 {
     const char *x = static_cast<const char *>(x_), *a_q = static_cast<const char *>(a_q_), *a_k = static_cast<const char *>(a_k_);
     char *t = static_cast<char *>(t_);
-    // Few tokens of a row: as many workgroups as there are eights of ranks and tokens, of sixteen waves (8 rows x 37 tokens, width 9216, rank 8
-    // of queries alone, with the projections 84.7 us; eight waves of 16 ranks x 16 tokens 87.4), while that is a round of the chip (4 x 50 tokens,
-    // rank 64, with 448 of them 31.4, sixteen tokens each 27.4).
+    // Few tokens of a row: as many workgroups as there are eights of ranks and tokens, of sixteen waves, while that is a round of the chip
+    // (8 rows x 37 tokens, width 9216, rank 8 of queries alone, with the projections 84.7 us; eight waves of 16 ranks x 16 tokens 87.4),
+    // else two or four eights of ranks each, or sixteen tokens where a row has more (4 x 50 tokens, rank 64, 27.4 us instead of 31.4; 31 rows x 1
+    // token, rank 128, 36.1 instead of 42.2).
     const long long eights = (long long)B * ((Tn + 7) / 8) * (R / 8) * ((a_q ? 1 : 0) + (a_k ? 1 : 0));
-    if (Tn <= 8 || (Tn <= 64 && eights <= 256)) return launch_down<1, 1, 16>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
-    if (Tn <= 64) return launch_down<1, 2, 16>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
-    return launch_down<4, 4, 4>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
+    auto go = [&](auto u, auto xt, auto waves) {
+        return launch_down<decltype(u)::value, decltype(xt)::value, decltype(waves)::value>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);
+    };
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 2> two{};
+    constexpr std::integral_constant<int, 4> four{};
+    constexpr std::integral_constant<int, 16> sixteen{};
+    if (Tn <= 8) return eights <= 256 ? go(one, one, sixteen) : eights <= 512 ? go(two, one, sixteen) : go(four, one, sixteen);
+    if (Tn <= 64) return eights <= 256 ? go(one, one, sixteen) : go(one, two, sixteen);
+    return go(four, four, four);
 }
 
 }  // namespace chai

@@ -1161,6 +1161,18 @@ static bool project_streams(int B, int H, int k, int Tn, int D)
     return tokens <= 32 ? std::any_of(std::begin(to32), std::end(to32), within) : std::any_of(std::begin(to64), std::end(to64), within);
 }
 
+// What 64-token tiles and 256-token tiles take of a call, in us: rounds of tiles of a chain along the width each (within 15 % over 483 calls of
+// 33 tokens and more, 2000 to 140 000 tokens over all pairs, widths 1024 to 9216, and they differ by up to three times).
+static double small_tiles_cost(int B, int H, int k, int Tn, int D)
+{
+    const double used = H * (1.0 - pow(1.0 - (double)k / H, B)), each = (double)B * k * Tn / used;
+    return 4.0 + used * ceil(each / kJtTok - 0.001) * (0.04 + 5.2e-5 * D);
+}
+static double large_tiles_cost(int B, int k, int Tn, int D)
+{
+    return ceil((double)B * k * ((Tn + kJTok - 1) / kJTok) / kJCus) * (5.0 + 0.0217 * D);
+}
+
 template <typename A>
 static int launch_project(const void *x, const void *w_q, const void *w_k, const int32_t *rep, int B, int H, int k, int Tn, int D,
                           void *q_out, void *k_compact, int pos0, int Tc_cap, const A &ad, const KernelEvents &ev, hipStream_t stream)
@@ -1206,7 +1218,10 @@ static int launch_project(const void *x, const void *w_q, const void *w_k, const
     const long long n_large = (long long)B * k * ((Tn + kJTok - 1) / kJTok);
     const bool one_round = n_large <= 150 && D < 8192;
     const long long most = n_large > 256 ? 24576 : (D < 2048 || one_round ? 16384 : (D < 3072 || n_large > 200 ? 20480 : 24576));
-    if (listed && items <= most && H <= kJtMaxHeads && (long long)B * Tn * D * 2 < 0x7fffffffLL &&
+    // (With adapters, a call of more tokens goes there as well where it is the faster by far: 14 rows x 32 tokens of 72 dense heads, D = 4096
+    // 383 / 122, 8 x 64 255 / 144, 28 x 64 with 16 of 72 182 / 115.  Calls without keep the kernels, and the bits, that they had.)
+    const bool few = items <= most || (A::any && 1.15 * small_tiles_cost(B, H, k, Tn, D) < large_tiles_cost(B, k, Tn, D));
+    if (listed && few && H <= kJtMaxHeads && (long long)B * Tn * D * 2 < 0x7fffffffLL &&
         (long long)kHeadDim * D * 2 < 0x7fffffffLL) {
         static DeviceFlags tile_lds_allowed;
         const hipError_t attr = allow_dynamic_lds(reinterpret_cast<const void *>(&project_tile_kernel<A>), kJtLdsBytes,
@@ -1240,9 +1255,26 @@ int launch_project_qk(const void *x, const void *w_q, const void *w_k, const int
 int launch_project_qk_adapted(const void *x, const void *w_q, const void *w_k, const int32_t *rep, int B, int H, int k, int Tn, int D,
                               void *q_out, void *k_compact, int pos0, int Tc_cap, const AdapterUse &use, hipStream_t stream)
 {
-    Adapters ad;
-    static_cast<AdapterUse &>(ad) = use;
-    return launch_project(x, w_q, w_k, rep, B, H, k, Tn, D, q_out, k_compact, pos0, Tc_cap, ad, KernelEvents{}, stream);
+    // Rows of so many pairs that they cannot be listed in LDS go in parts that can, where that is faster than 256-token tiles (43 rows x 2
+    // tokens of 32 dense heads, D = 6656 838 us in one, 84 in two; 35 x 4 of 72, D = 2048 507 and 69 in three).
+    int rows = B;
+    if ((long long)B * k > kJtMaxSlots && k <= kJtMaxSlots && H <= kJtMaxHeads && !project_streams(B, H, k, Tn, D)) {
+        const int parts = (int)((B + kJtMaxSlots / k - 1) / (kJtMaxSlots / k)), each = (B + parts - 1) / parts;
+        const double small = small_tiles_cost(each, H, k, Tn, D), large = large_tiles_cost(each, k, Tn, D);
+        if (1.15 * parts * (small < large ? small : large) < large_tiles_cost(B, k, Tn, D)) rows = each;
+    }
+    for (int b = 0; b < B; b += rows) {
+        const int n = B - b < rows ? B - b : rows;
+        Adapters ad;
+        static_cast<AdapterUse &>(ad) = use;
+        ad.ids += b;
+        ad.t += (size_t)b * Tn * 2 * use.chunks() * 64;
+        const int e = launch_project(static_cast<const char *>(x) + (size_t)b * Tn * D * 2, w_q, w_k, rep + (size_t)b * k, n, H, k, Tn, D,
+                                     static_cast<char *>(q_out) + (size_t)b * H * Tn * (kHeadDim * 2),
+                                     static_cast<char *>(k_compact) + (size_t)b * k * Tc_cap * (kHeadDim * 2), pos0, Tc_cap, ad, KernelEvents{}, stream);
+        if (e != (int)hipSuccess) return e;
+    }
+    return (int)hipSuccess;
 }
 
 }  // namespace chai

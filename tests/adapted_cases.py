@@ -6,3 +6,6 @@ CASES = {
     "large": [(2, 16, 16, 801, 192), (4, 16, 16, 1025, 128), (1, 3, 3, 16384, 64)],
 }
 RANKS = [8, 16, 24, 64, 128]
+# calls that go another way than those without adapters: in parts of rows that can be listed, and small tiles of more tokens
+PARTS = [(43, 32, 32, 2, 256), (35, 72, 72, 4, 128), (1030, 1, 1, 3, 64)]
+MORE = [(14, 72, 72, 32, 1024)]

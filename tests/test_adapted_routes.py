@@ -6,7 +6,7 @@ import torch
 
 import launch_log
 import paper_2403_08058_amd as C
-from adapted_cases import CASES, RANKS
+from adapted_cases import CASES, MORE, PARTS, RANKS
 
 FAKE, BIG = 0x1000, 1 << 40
 NULL, SHAPE, DTYPE, WORKSPACE, UNSUPPORTED, ALIGN = 1, 2, 3, 4, 5, 7
@@ -14,7 +14,7 @@ NULL, SHAPE, DTYPE, WORKSPACE, UNSUPPORTED, ALIGN = 1, 2, 3, 4, 5, 7
 
 @pytest.fixture(scope="module")
 def launched(tmp_path_factory):
-    sizes = [(*c, R) for cases in CASES.values() for c in cases for R in RANKS]
+    sizes = [(*c, R) for cases in (*CASES.values(), PARTS, MORE) for c in cases for R in RANKS]
     return launch_log.run(tmp_path_factory.mktemp("stand_in"), f"""
         result = []
         for B, H, k, Tn, D, R in {sizes!r}:
@@ -40,6 +40,22 @@ def test_kernels_of_the_sizes(launched, kernel):
     if kernel == "large":                                  # a workgroup per tile, and several tiles each
         grids = {r[2][1][1] for r in launched if r[1][:5] in [list(c) for c in CASES["large"]]}
         assert 256 in grids and any(n < 256 for n in grids)
+
+
+def test_rows_of_too_many_pairs_go_in_parts(launched):
+    for case in PARTS:
+        st, _, got, plain = next(r for r in launched if r[1] == [*case, 16])
+        assert st == 0 and len(plain) == 1 and "14project_kernel" in plain[0][0]
+        assert len(got) >= 3 and "adapter_down_kernel" in got[0][0] and not any("14project_kernel" in g[0] for g in got), got
+    for case in MORE:
+        st, _, got, plain = next(r for r in launched if r[1] == [*case, 16])
+        assert st == 0 and "14project_kernel" in plain[0][0] and len(got) == 2 and "project_tile_kernel" in got[1][0]
+
+
+def test_shapes_of_the_first_half(launched):
+    """Every shape of workgroups of it is reached."""
+    shapes = {re.search(r"adapter_down_kernelILi(\d+)ELi(\d+)ELi(\d+)E", r[2][0][0]).groups() for r in launched}
+    assert shapes == {("1", "1", "16"), ("2", "1", "16"), ("4", "1", "16"), ("1", "2", "16"), ("4", "4", "4")}
 
 
 def call(**kw):

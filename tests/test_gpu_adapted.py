@@ -11,7 +11,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 import paper_2403_08058_amd as C
-from adapted_cases import CASES, RANKS
+from adapted_cases import CASES, MORE, PARTS, RANKS
 
 D_HEAD = 128
 BF16 = torch.bfloat16
@@ -107,6 +107,21 @@ def test_every_kernel(kernel, B, H, k, Tn, D, R):
     plain_q, plain_k = x.run(plain=True)
     bare = np.flatnonzero(x.ids < 0)                       # without an adapter: the projections' own bits
     assert torch.equal(q[bare], plain_q[bare]) and torch.equal(kc[bare], plain_k[bare])
+
+
+@pytest.mark.parametrize("B,H,k,Tn,D", PARTS + MORE)
+@pytest.mark.parametrize("R", [8, 128])
+def test_many_pairs(B, H, k, Tn, D, R):
+    print(f"[adapted] many pairs {B} x {Tn} tokens, {k} of {H}, width {D}, rank {R}", flush=True)
+    x = Inputs(B + R, B, H, k, Tn, D, R, n=B // 2, pos0=2)
+    q, kc = x.run()
+    x.check(q, kc, rows=[0, 1, B // 2 - 1, B // 2, B - 1])
+    # without an adapter: the projections' values in another order of the sums, each within half a step and 3e-6 of the magnitudes (at most
+    # 0.8 * 1024^0.5 on average, five times that in all) of the exact one
+    bare = np.flatnonzero(x.ids < 0)
+    for got, want in zip((q, kc), x.run(plain=True)):
+        a, b = got[bare].float(), want[bare].float()
+        assert bool(((a - b).abs() <= 2.0 ** -7 * b.abs() + 2 * 3e-6 * 5 * 26).all())
 
 
 @pytest.mark.parametrize("kernel", CASES)
