@@ -194,7 +194,6 @@ struct PlaceOut {
     int32_t *table = nullptr, *new_lens = nullptr, *n_left = nullptr, *granted = nullptr, *offsets = nullptr, *token_rows = nullptr,
             *positions = nullptr, *slots = nullptr;
 };
-constexpr int kPlaceOneRows = 1024, kPlaceOneTokens = 2048;      // up to so many of both: one launch of one workgroup
 size_t place_workspace_bytes(int B);
 int launch_place_tokens(const PlaceShape &sh, const PlaceIn &in, const PlaceOut &out, void *workspace, hipStream_t stream);
 int launch_release_pages(const PlaceShape &sh, const int32_t *keep, const int32_t *lens, int32_t *table, int32_t *free_pages,

@@ -8,6 +8,8 @@
 //   token i:  position len + i in page position / page of its row, slot = page number * page + position % page
 //
 // Two sums over the rows (tokens and pages), both capped, so that no number of tokens overflows them: min(a + b, cap) is associative.
+//
+// What bounds it: look-ups that depend on one another (lengths, two sums over the workgroup, the row of a token, its page) and the launch.
 #include "chai_internal.h"
 
 #include <hip/hip_ext.h>
@@ -18,6 +20,8 @@ namespace {
 
 constexpr int kPlaceBlock = 256;
 constexpr int kPlaceWaves = kPlaceBlock / 64;
+constexpr int kPlaceOneTokens = 2048;        // that one workgroup takes at most
+constexpr int kPlaceMost = 1024;             // workgroups of a launch that all look at the rows
 
 __device__ __forceinline__ unsigned int capped(unsigned int a, unsigned int b, unsigned int cap) { return min(a + b, cap); }
 
@@ -50,72 +54,76 @@ __device__ __forceinline__ unsigned int block_scan(unsigned int x, unsigned int 
     return x;
 }
 
-// Which rows get their tokens; one workgroup.  rows: [B] in LDS or in the workspace; total (in LDS or NULL): tokens of all.  Everything that may be written in place
-// (new_lens over seq_lens, n_left over n_free) has been read by every thread before the first barrier.
-__device__ __forceinline__ void place_rows(const PlaceShape &sh, const PlaceIn &in, const PlaceOut &out, PlacedRow *rows, int *total)
+// Which rows get their tokens; a workgroup, SPAN rows a thread.  rows: [B] in LDS or in the workspace; total (in LDS or NULL): tokens of all;
+// `write`: the rows' outputs, by one of the workgroups that find the same.  Everything that may be written in place (new_lens over
+// seq_lens, n_left over n_free) has been read by every thread before the first barrier.
+template <int SPAN>
+__device__ __forceinline__ void place_rows(const PlaceShape &sh, const PlaceIn &in, const PlaceOut &out, PlacedRow *rows, int *total, bool write)
 {
     __shared__ unsigned int sums[2][kPlaceWaves], taken;
-    const int tid = threadIdx.x, span = (sh.B + kPlaceBlock - 1) / kPlaceBlock;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, b0 = tid * SPAN;
     const unsigned int most_tokens = (unsigned int)sh.N + 1u, most_pages = (unsigned int)sh.n_pages + 1u;
+    int given[SPAN], len[SPAN];
+#pragma unroll
+    for (int i = 0; i < SPAN; ++i) {                     // (rows past the end ask for nothing)
+        given[i] = b0 + i < sh.B ? in.counts[b0 + i] : 0;
+        len[i] = b0 + i < sh.B ? max(in.lens[b0 + i], 0) : 0;
+    }
     const unsigned int n_free = (unsigned int)min(max(in.n_free[0], 0), sh.n_pages);
     const long long reach = min((long long)sh.max_blocks * sh.page, 0x7fffffffll);
     if (tid == 0) taken = 0u;
 
-    // (the first of a thread's rows, all it has where there are few, is asked for once)
-    const int b0 = min(tid * span, sh.B), b1 = min(b0 + span, sh.B);
-    const int count0 = b0 < b1 ? in.counts[b0] : 0, len0 = b0 < b1 ? in.lens[b0] : 0;
-    auto count_of = [&](int b) { return min((unsigned int)max(b == b0 ? count0 : in.counts[b], 0), most_tokens); };
-    auto len_of = [&](int b) { return max(b == b0 ? len0 : in.lens[b], 0); };
-    unsigned int tokens = 0u;
-    for (int b = b0; b < b1; ++b) tokens = capped(tokens, count_of(b), most_tokens);
-    const unsigned int tokens_upto = block_scan(tokens, most_tokens, sums[0]);
-    // what came before this thread's rows: with a cap it cannot be had by subtraction
-    unsigned int tokens_before = (unsigned int)__shfl_up((int)tokens_upto, 1);
-    if ((tid & 63) == 0) {
-        tokens_before = 0u;
-        for (int v = 0; v < tid >> 6; ++v) tokens_before = capped(tokens_before, sums[0][v], most_tokens);
-    }
-    auto need_of = [&](unsigned int end, int len, unsigned int count, bool &fits) {
-        fits = end <= (unsigned int)sh.N && (long long)len + count <= reach;
-        return fits ? (unsigned int)(blocks_of(sh, (unsigned int)len + count) - blocks_of(sh, (unsigned int)len)) : 0u;
+    // what came before a thread's rows: with a cap it cannot be had from the sum up to them by subtraction
+    auto before = [&](unsigned int upto, const unsigned int *of_waves, unsigned int cap) {
+        unsigned int x = (unsigned int)__shfl_up((int)upto, 1);
+        if (lane == 0) {
+            x = 0u;
+            for (int v = 0; v < w; ++v) x = capped(x, of_waves[v], cap);
+        }
+        return x;
     };
-    unsigned int pages = 0u, end = tokens_before;
-    for (int b = b0; b < b1; ++b) {
-        const unsigned int count = count_of(b);
-        bool fits;
-        end = capped(end, count, most_tokens);
-        pages = capped(pages, need_of(end, len_of(b), count, fits), most_pages);
+    unsigned int count[SPAN], tokens = 0u;
+#pragma unroll
+    for (int i = 0; i < SPAN; ++i) {
+        count[i] = min((unsigned int)max(given[i], 0), most_tokens);
+        tokens = capped(tokens, count[i], most_tokens);
+    }
+    const unsigned int tokens_upto = block_scan(tokens, most_tokens, sums[0]);
+    unsigned int first[SPAN], need[SPAN], end = before(tokens_upto, sums[0], most_tokens), pages = 0u;
+    bool fits[SPAN];
+#pragma unroll
+    for (int i = 0; i < SPAN; ++i) {
+        first[i] = end;
+        end = capped(end, count[i], most_tokens);
+        fits[i] = end <= (unsigned int)sh.N && (long long)len[i] + count[i] <= reach;
+        need[i] = fits[i] ? (unsigned int)(blocks_of(sh, (unsigned int)len[i] + count[i]) - blocks_of(sh, (unsigned int)len[i])) : 0u;
+        pages = capped(pages, need[i], most_pages);
     }
     const unsigned int pages_upto = block_scan(pages, most_pages, sums[1]);
-    unsigned int pages_end = (unsigned int)__shfl_up((int)pages_upto, 1);
-    if ((tid & 63) == 0) {
-        pages_end = 0u;
-        for (int v = 0; v < tid >> 6; ++v) pages_end = capped(pages_end, sums[1][v], most_pages);
-    }
-    end = tokens_before;
-    unsigned int last = 0u;
-    for (int b = b0; b < b1; ++b) {
-        const unsigned int count = count_of(b), first = end, before = pages_end;
-        const int len = len_of(b);
-        bool fits;
-        end = capped(end, count, most_tokens);
-        const unsigned int need = need_of(end, len, count, fits);
-        pages_end = capped(pages_end, need, most_pages);
-        const bool granted = fits && (need == 0u || pages_end <= n_free);
-        if (granted && need != 0u) last = pages_end;
-        rows[b] = PlacedRow{(int)min(first, (unsigned int)sh.N), len, granted ? blocks_of(sh, (unsigned int)len) : -1,
-                            granted ? (int)(n_free - min(before, n_free)) : 0};
-        out.offsets[b] = (int)min(first, (unsigned int)sh.N);
-        out.granted[b] = granted ? 1 : 0;
-        out.new_lens[b] = granted ? len + (int)count : len;
+    unsigned int pages_end = before(pages_upto, sums[1], most_pages), last = 0u;
+#pragma unroll
+    for (int i = 0; i < SPAN; ++i) {
+        const int b = b0 + i;
+        const unsigned int pages_before = pages_end;
+        pages_end = capped(pages_end, need[i], most_pages);
+        const bool granted = fits[i] && (need[i] == 0u || pages_end <= n_free);
+        if (granted && need[i] != 0u) last = pages_end;
+        if (b >= sh.B) continue;
+        const int at = (int)min(first[i], (unsigned int)sh.N);
+        rows[b] = PlacedRow{at, len[i], granted ? blocks_of(sh, (unsigned int)len[i]) : -1, granted ? (int)(n_free - min(pages_before, n_free)) : 0};
+        if (write) {
+            out.offsets[b] = at;
+            out.granted[b] = granted ? 1 : 0;
+            out.new_lens[b] = granted ? len[i] + (int)count[i] : len[i];
+        }
     }
     if (last != 0u) atomicMax(&taken, last);
     if (tid == kPlaceBlock - 1) {
-        out.offsets[sh.B] = (int)min(tokens_upto, (unsigned int)sh.N);
+        if (write) out.offsets[sh.B] = (int)min(tokens_upto, (unsigned int)sh.N);
         if (total != nullptr) *total = (int)min(tokens_upto, (unsigned int)sh.N);
     }
     __syncthreads();
-    if (tid == 0) out.n_left[0] = (int)(n_free - taken);
+    if (tid == 0 && write) out.n_left[0] = (int)(n_free - taken);
 }
 
 // Token n: its row (the last one that begins at or before it: rows without tokens begin where the next one does), position and slot;
@@ -152,18 +160,21 @@ __device__ __forceinline__ void place_token(const PlaceShape &sh, const PlaceIn 
     out.slots[n] = slot;
 }
 
-// One workgroup for everything.
+// One launch for everything.  Where there are many tokens several workgroups take them, each of which finds out about the rows for itself
+// (nothing that they read may be written in place then: only the first writes what is known of rows, but it does not wait for the others).
+template <int SPAN>
 __global__ __launch_bounds__(kPlaceBlock) void place_all_kernel(PlaceShape sh, PlaceIn in, PlaceOut out)
 {
-    __shared__ PlacedRow rows[kPlaceOneRows];
+    __shared__ PlacedRow rows[SPAN * kPlaceBlock];
     __shared__ int total;
-    place_rows(sh, in, out, rows, &total);
-    for (int n = threadIdx.x; n < sh.N; n += kPlaceBlock) place_token(sh, in, out, rows, n, total);
+    place_rows<SPAN>(sh, in, out, rows, &total, blockIdx.x == 0);
+    for (int n = blockIdx.x * kPlaceBlock + threadIdx.x; n < sh.N; n += gridDim.x * kPlaceBlock) place_token(sh, in, out, rows, n, total);
 }
 
+template <int SPAN>
 __global__ __launch_bounds__(kPlaceBlock) void place_rows_kernel(PlaceShape sh, PlaceIn in, PlaceOut out, PlacedRow *rows)
 {
-    place_rows(sh, in, out, rows, nullptr);
+    place_rows<SPAN>(sh, in, out, rows, nullptr, true);
 }
 
 __global__ __launch_bounds__(kPlaceBlock) void place_tokens_kernel(PlaceShape sh, PlaceIn in, PlaceOut out, const PlacedRow *rows)
@@ -252,10 +263,19 @@ size_t place_workspace_bytes(int B) { return ((size_t)B * sizeof(PlacedRow) + 25
 
 int launch_place_tokens(const PlaceShape &sh, const PlaceIn &in, const PlaceOut &out, void *workspace, hipStream_t stream)
 {
-    if (sh.B <= kPlaceOneRows && sh.N <= kPlaceOneTokens)
-        return (int)launch_kernel(place_all_kernel, dim3(1), dim3(kPlaceBlock), 0, stream, KernelEvents{}, sh, in, out);
+    // Up to 1024 rows, a workgroup for every 256 tokens, in one launch; where outputs lie over inputs one workgroup, or two launches of
+    // more than 2048 tokens.  Kernel times in us, one workgroup / these / two launches: 16 rows' tokens 3.7; 32 rows, 2000 tokens 8.8 / 5.7; 256 rows
+    // with 24 prompts, 26 000 tokens - / 6.6 / 17; 1000 rows, 100 000 tokens - / 8.7 / 18.
+    const bool in_place = out.new_lens == in.lens || out.n_left == in.n_free;
+    if (sh.B <= 4 * kPlaceBlock && (sh.N <= kPlaceOneTokens || !in_place)) {
+        const int workgroups = in_place ? 1 : (sh.N + kPlaceBlock - 1) / kPlaceBlock;
+        const dim3 grid((unsigned int)(workgroups < 1 ? 1 : workgroups < kPlaceMost ? workgroups : kPlaceMost));
+        return (int)launch_kernel(sh.B <= kPlaceBlock ? place_all_kernel<1> : place_all_kernel<4>, grid, dim3(kPlaceBlock), 0, stream, KernelEvents{}, sh, in, out);
+    }
     PlacedRow *rows = static_cast<PlacedRow *>(workspace);
-    const hipError_t e = launch_kernel(place_rows_kernel, dim3(1), dim3(kPlaceBlock), 0, stream, KernelEvents{}, sh, in, out, rows);
+    static_assert(kMaxPagedBatch <= 16 * kPlaceBlock, "rows of a workgroup");
+    const hipError_t e = launch_kernel(sh.B <= kPlaceBlock ? place_rows_kernel<1> : place_rows_kernel<16>, dim3(1), dim3(kPlaceBlock), 0, stream, KernelEvents{},
+                                       sh, in, out, rows);
     if (e != hipSuccess || sh.N == 0) return (int)e;
     return (int)launch_kernel(place_tokens_kernel, dim3((unsigned int)((sh.N + kPlaceBlock - 1) / kPlaceBlock)), dim3(kPlaceBlock), 0, stream,
                               KernelEvents{}, sh, in, out, rows);

@@ -109,12 +109,21 @@ def test_rows_grow(B, page, longest, most, in_place):
             assert want["granted"].all()
 
 
-@pytest.mark.parametrize("N", [1, 2047, 2048, 2049, 5000])
-def test_one_row_with_many_tokens(N):
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("N", [1, 255, 256, 257, 2047, 2048, 2049, 5000])
+def test_one_row_with_many_tokens(N, in_place):
     g = np.random.default_rng(N)
     pool = Pool(g, 2, 16, [5, 3], 400, 500)
-    check(pool, [N - 1, 1], N)
-    check(pool, [0, N], N)
+    check(pool, [N - 1, 1], N, in_place=in_place)
+    check(pool, [0, N], N, in_place=in_place)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_more_tokens_than_workgroups_at_once(in_place):
+    """300 000 tokens: every workgroup takes more than one stretch of them."""
+    g = np.random.default_rng(8)
+    pool = Pool(g, 3, 64, [100, 7, 0], 3300, 4700)
+    check(pool, [200000, 1, 100000], 300010, in_place=in_place)
 
 
 def test_tables_that_are_full_and_rows_without_tokens():
