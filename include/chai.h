@@ -738,7 +738,7 @@ int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new
  *                 need not be initialised.  Two calls that run concurrently
  *                 need separate workspaces.
  * R is a multiple of 8 up to 128 (adapters of a smaller rank: zeros behind it);
- * the other arguments, limits and errors as chai_project_qk.
+ * B = 0 is a no-op (arrays of no rows may be NULL); the other arguments, limits and errors as chai_project_qk.
  */
 size_t chai_project_adapted_workspace_bytes(int B, int Tn, int R);
 int chai_project_qk_adapted(const void *x, const void *w_q, const void *w_k, const int32_t *rep_heads, const int32_t *adapter_ids,

@@ -513,8 +513,11 @@ int chai_project_qk_adapted(const void *x, const void *w_q, const void *w_k, con
                             int n_adapters, int R, int B, int H, int k, int Tn, int D, int d, int dtype, void *q_out,
                             void *k_compact, int pos0, int Tc_cap, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!adapter_ids || !a_q != !b_q || !a_k != !b_k || (!a_q && !a_k)) return CHAI_ERR_NULL;
-    int st = check_project(x, w_q, w_k, rep_heads, B, H, k, Tn, D, d, dtype, q_out, k_compact, pos0, Tc_cap);
+    if ((!adapter_ids && B != 0) || !a_q != !b_q || !a_k != !b_k || (!a_q && !a_k)) return CHAI_ERR_NULL;
+    // (arrays of no rows may be NULL, as an allocator may give them)
+    const bool rows = x && rep_heads && q_out && k_compact;
+    int st = B == 0 && !rows ? check_project(w_q, w_q, w_k, static_cast<const int32_t *>(w_q), B, H, k, Tn, D, d, dtype, w_q, w_q, pos0, Tc_cap)
+                             : check_project(x, w_q, w_k, rep_heads, B, H, k, Tn, D, d, dtype, q_out, k_compact, pos0, Tc_cap);
     if (st != CHAI_OK) return st;
     if (n_adapters < 1 || R < 1) return CHAI_ERR_SHAPE;
     if (R % 8 != 0 || R > kMaxAdapterRank) return CHAI_ERR_UNSUPPORTED;

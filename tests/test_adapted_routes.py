@@ -74,7 +74,7 @@ def test_refusals():
     assert call(dtype=0) == UNSUPPORTED and call(R=12) == UNSUPPORTED and call(R=136) == UNSUPPORTED and call(D=500) == UNSUPPORTED
     assert call(a_q=FAKE + 8) == ALIGN and call(b_k=FAKE + 2) == ALIGN and call(x=FAKE + 8) == ALIGN
     assert call(ws=None) == WORKSPACE and call(ws=FAKE + 16) == WORKSPACE and call(ws_bytes=2 * 4 * 2 * 64 - 1) == WORKSPACE
-    assert call(B=0, ws=None) == 0
+    assert call(B=0, ws=None) == 0 and call(B=0, x=None, rep=None, ids=None, q_out=None, kc=None, ws=None) == 0 and call(B=0, w_k=None) == NULL
 
 
 def test_workspace():

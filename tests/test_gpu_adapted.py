@@ -210,3 +210,42 @@ def test_recorded_and_on_another_stream(kernel):
         call()
         torch.cuda.synchronize()
         assert torch.equal(got[0], q) and torch.equal(got[1], kc)
+
+
+@pytest.mark.parametrize("kernel", CASES)
+def test_adapters_beyond_32_bits(kernel):
+    """The last adapter of tables of more than 2^32 bytes."""
+    B, H, k, Tn, D = CASES[kernel][1]
+    R = 128
+    x = Inputs(90, B, H, k, Tn, D, R, n=2)
+    x.ids[:] = 1
+    small = x.run()
+    n = (1 << 32) // (2 * R * min(D, H * D_HEAD)) + 3
+    tables = {}
+    for p in "qk":
+        for name, t in (("a", x.a[p]), ("b", x.b[p])):
+            tables[name, p] = torch.zeros((n, *t.shape[1:]), dtype=BF16, device="cuda")
+            tables[name, p][-1] = t[1]
+    x.a, x.b = ({p: tables[name, p] for p in "qk"} for name in "ab")
+    x.scale = torch.full((n,), float(x.scale[1]), device="cuda")
+    x.ids[:] = n - 1
+    for a, b in zip(x.run(), small):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kernel", CASES)
+def test_two_calls_at_once(kernel):
+    """On two streams, with a workspace each."""
+    B, H, k, Tn, D = CASES[kernel][1]
+    calls = [Inputs(95 + i, B, H, k, Tn, D, 24, n=3) for i in range(2)]
+    want = [x.run() for x in calls]
+    got = [[torch.full_like(t, float(v)) for t, v in zip(w, (7.0, 9.0))] for w in want]
+    spaces, streams = [C.alloc_adapted_workspace(B, Tn, 24) for _ in calls], [torch.cuda.Stream() for _ in calls]
+    maps = [(dev(x.rep), dev(x.ids)) for x in calls]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, (q, kc), ws, stream, (rep, ids) in zip(calls, got, spaces, streams, maps):
+            C.chai_project_qk_adapted(x.x, x.w["q"], x.w["k"], rep, ids, x.a["q"], x.b["q"], x.a["k"], x.b["k"], x.scale, q, kc, 0, ws, stream=stream)
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])

@@ -334,3 +334,42 @@ def test_packed_recorded_and_on_another_stream():
         call()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (s["q_out"], *s["pages"], *s["scales"])))
+
+
+def test_packed_offsets_beyond_32_bits():
+    """The last page of pools of more than 2^32 bytes."""
+    H, k, page, n_pages, N = 72, 2, 256, 1000, 9
+    g = np.random.default_rng(51)
+    new = lambda *s: torch.from_numpy(g.standard_normal(s).astype(np.float32)).cuda().to(torch.bfloat16)  # noqa: E731
+    v_pages = torch.zeros((n_pages, H, page, D), dtype=torch.bfloat16, device="cuda")
+    k_pages = torch.zeros((n_pages, k, page, D), dtype=torch.bfloat16, device="cuda")
+    q, keys, v, freq = new(N, H, D), new(N, k, D), new(N, H, D), C.chai_rotary_frequencies(128)
+    slots = (n_pages - 1) * page + page - 1 - np.arange(N)
+    pos = np.arange(5, 5 + N)
+    C.chai_paged_append_packed(q, keys, v, dev([[1, 70]]), dev(np.zeros(N)), dev(pos), dev(slots), freq.cuda(), q, k_pages, v_pages, k_by_slot=True)
+    torch.cuda.synchronize()
+    at = torch.from_numpy(slots % page).cuda()
+    assert torch.equal(v_pages[-1][:, at], v.transpose(0, 1))
+    want, mag = turned(keys.transpose(0, 1).double().cpu().numpy(), pos, freq.numpy(), "halves", 1.0)
+    assert_rounded(k_pages[-1][:, at], want, mag, "bf16", "last page")
+    v_pages[-1][:, at] = 0
+    assert not bool(v_pages.view(torch.int64).any())
+
+
+def test_empty_calls():
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    i = lambda *s: z(*s, dt=torch.int32)  # noqa: E731
+    freq = C.chai_rotary_frequencies(128).cuda()
+    for B, Tn in ((0, 3), (2, 0)):
+        q, kc = z(B, 4, Tn, D), torch.full((B, 2, 5, D), 3.0, device="cuda", dtype=torch.bfloat16)
+        C.chai_rotate_qk(q, z(B, 2, Tn, D), i(B, 2), freq, z(B, 4, Tn, D), kc, 1)
+        assert bool((kc == 3.0).all())
+    pages = torch.full((3, 2, 8, D), 3.0, device="cuda", dtype=torch.bfloat16), torch.full((3, 4, 8, D), 3.0, device="cuda", dtype=torch.bfloat16)
+    C.chai_paged_append_packed(z(0, 4, D), z(0, 4, D), z(0, 4, D), i(2, 2), i(0), i(0), i(0), freq, z(0, 4, D), *pages)
+    C.chai_paged_place_tokens(i(0), i(0), i(0, 4), i(9), i(1), 8, i(0), i(1), i(0), i(1), i(6), i(6), i(6), C.alloc_paged_place_workspace(0))
+    C.chai_paged_release_pages(i(0), i(0), i(0, 4), i(9), i(1), 8, i(0), i(1))
+    x = z(0, 3, 64)
+    C.chai_project_qk_adapted(x, z(4 * D, 64), z(4 * D, 64), i(0, 2), i(0), z(1, 8, 64), z(1, 4 * D, 8), None, None, None, z(0, 4, 3, D), z(0, 2, 3, D), 0,
+                              C.alloc_adapted_workspace(0, 3, 8))
+    torch.cuda.synchronize()
+    assert all(bool((p == 3.0).all()) for p in pages)
