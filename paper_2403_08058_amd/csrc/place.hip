@@ -185,7 +185,10 @@ __global__ __launch_bounds__(kPlaceBlock) void place_tokens_kernel(PlaceShape sh
 
 // ---------------------------------------------------------------------------------------------------------
 // Pages of rows that end, or lose their last positions, go back on the list: those behind the kept positions that are pages, rows in
-// order, a row's in order.  One workgroup: rows write behind one another.
+// order, a row's in order.  One workgroup, because rows write behind one another; a wave takes every 16th row, looks at 64 at a time, and
+// goes through those that give pages back, once to count them and once, when all that come before are counted, to move them.  Look-ups
+// that wait for one another bound it: one row of 32 pages among 16 rows 4.2 us, 16 rows of 128 pages among 256 4.5 us, 100 rows of 32
+// pages among 4096 14.6 us (waves that take neighbouring rows 15 and 39.5 us, waves that walk through every row 10.6 and 120).
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kReleaseBlock = 1024;
 
@@ -196,20 +199,30 @@ __global__ __launch_bounds__(kReleaseBlock) void release_kernel(PlaceShape sh, c
     __shared__ int sums[kReleaseBlock / 64];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int top = min(max(n_free[0], 0), sh.n_pages);
-    auto bounds = [&](int b, int &lo, int &hi) {
-        const int len = max(lens[b], 0), kept = min(max(keep[b], 0), len);
-        lo = min(blocks_of(sh, (unsigned int)kept), sh.max_blocks);
-        hi = min(blocks_of(sh, (unsigned int)len), sh.max_blocks);
-        return kept;
-    };
-    for (int b = w; b < sh.B; b += kReleaseBlock / 64) {
-        int lo, hi, n = 0;
-        bounds(b, lo, hi);
-        for (int i = lo; i < hi; i += 64) {
-            const int p = i + lane < hi ? table[(size_t)b * sh.max_blocks + i + lane] : -1;
-            n += __popcll(__ballot((unsigned int)p < (unsigned int)sh.n_pages));
+    constexpr int kWaves = kReleaseBlock / 64;           // a wave's rows are b0 + w, b0 + w + 16, ...: rows that end together are often neighbours
+    // f(row, its lane, first page that goes back, end of them) for the rows that give any, in order
+    auto each_row = [&](int b0, auto f) __attribute__((always_inline)) {
+        const int b = b0 + lane * kWaves + w;
+        const bool row = b < sh.B;
+        const int len = row ? max(lens[b], 0) : 0, kept = row ? min(max(keep[b], 0), len) : 0;
+        const int lo = min(blocks_of(sh, (unsigned int)kept), sh.max_blocks), hi = min(blocks_of(sh, (unsigned int)len), sh.max_blocks);
+        for (unsigned long long left = __ballot(hi > lo); left != 0ull; left &= left - 1ull) {
+            const int r = __ffsll((long long)left) - 1;
+            f(b0 + r * kWaves + w, r, __builtin_amdgcn_readlane(lo, r), __builtin_amdgcn_readlane(hi, r));
         }
-        if (lane == 0) from[b] = n;
+    };
+    for (int b0 = 0; b0 < sh.B; b0 += kReleaseBlock) {
+        int mine = 0;
+        each_row(b0, [&](int b, int r, int lo, int hi) {
+            int n = 0;
+            for (int i = lo; i < hi; i += 64) {
+                const int p = i + lane < hi ? table[(size_t)b * sh.max_blocks + i + lane] : -1;
+                n += __popcll(__ballot((unsigned int)p < (unsigned int)sh.n_pages));
+            }
+            mine = lane == r ? n : mine;
+        });
+        const int b = b0 + lane * kWaves + w;
+        if (b < sh.B) from[b] = mine;
     }
     __syncthreads();
     // (at most n_pages go back in a table of pages that are in use once; a sum that a broken table makes larger is cut there)
@@ -234,26 +247,22 @@ __global__ __launch_bounds__(kReleaseBlock) void release_kernel(PlaceShape sh, c
         before = capped(before, n, cap);
     }
     __syncthreads();
-    for (int b = w; b < sh.B; b += kReleaseBlock / 64) {
-        int lo, hi;
-        bounds(b, lo, hi);
-        long long at = (long long)top + from[b];
-        for (int i = lo; i < hi; i += 64) {
-            int32_t *entry = table + (size_t)b * sh.max_blocks + i + lane;
-            const int p = i + lane < hi ? *entry : -1;
-            const bool page = (unsigned int)p < (unsigned int)sh.n_pages;
-            const unsigned long long votes = __ballot(page);
-            const long long to = at + __popcll(votes & ((1ull << lane) - 1ull));
-            if (page && to < sh.n_pages) free_pages[to] = p;
-            if (i + lane < hi) *entry = -1;
-            at += __popcll(votes);
-        }
-    }
+    for (int c0 = 0; c0 < sh.B; c0 += kReleaseBlock)
+        each_row(c0, [&](int b, int, int lo, int hi) {
+            long long at = (long long)top + from[b];
+            for (int i = lo; i < hi; i += 64) {
+                int32_t *entry = table + (size_t)b * sh.max_blocks + i + lane;
+                const int p = i + lane < hi ? *entry : -1;
+                const bool page = (unsigned int)p < (unsigned int)sh.n_pages;
+                const unsigned long long votes = __ballot(page);
+                const long long to = at + __popcll(votes & ((1ull << lane) - 1ull));
+                if (page && to < sh.n_pages) free_pages[to] = p;
+                if (i + lane < hi) *entry = -1;
+                at += __popcll(votes);
+            }
+        });
     __syncthreads();
-    for (int b = tid; b < sh.B; b += kReleaseBlock) {
-        int lo, hi;
-        new_lens[b] = bounds(b, lo, hi);
-    }
+    for (int b = tid; b < sh.B; b += kReleaseBlock) new_lens[b] = min(max(keep[b], 0), max(lens[b], 0));
     if (tid == kReleaseBlock - 1) n_left[0] = (int)min((long long)top + before, (long long)sh.n_pages);
 }
 
