@@ -675,7 +675,7 @@ int chai_paged_release_pages(const int32_t *keep, const int32_t *seq_lens, int32
  *     (strides in elements, >= Tn*d, multiples of 8; inputs and outputs are
  *     the same rows or do not overlap.)  q and q_out, or k and k_out, may both
  *     be NULL.  rep_heads NULL: every head (k = H).  chai_project_qk leaves
- *   queries and keys in these layouts.  B * Tn < 2^31.
+ *   queries and keys in these layouts.  B * Tn <= 2^26.
  */
 enum { CHAI_ROPE_HALVES = 0, CHAI_ROPE_PAIRS = 1 };
 enum { CHAI_ROPE_PLAIN = 0, CHAI_ROPE_LINEAR = 1, CHAI_ROPE_BASE = 2, CHAI_ROPE_TURNS = 3 };

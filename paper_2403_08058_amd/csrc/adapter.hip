@@ -177,25 +177,33 @@ __global__ __launch_bounds__(WAVES * 64) void adapter_down_kernel(const char *__
     }
 }
 
+size_t adapter_row_bytes(int Tn, int R) { return (size_t)Tn * 2 * ((R + 15) / 16) * 64; }
+
 template <int U, int XT, int WAVES>
 int launch_down(const char *x, const int32_t *ids, const char *a_q, const char *a_k, const float *scales, int n, int R, int B, int Tn, int D,
                 char *t, hipStream_t stream)
 {
     const int total = R / 8 * ((a_q ? 1 : 0) + (a_k ? 1 : 0)), groups = (total + U - 1) / U, tiles = (Tn + 8 * XT - 1) / (8 * XT);
-    const long long n_tiles = (long long)B * tiles, items = n_tiles * groups, grid = (n_tiles + 7) / 8 * 8 * groups;
-    if (grid > 0x7fffffffll) return (int)hipErrorInvalidConfiguration;
     static DeviceFlags lds_allowed;
     const size_t lds = (size_t)WAVES * wave_bytes(WAVES);
     const auto kernel = adapter_down_kernel<U, XT, WAVES>;
-    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds, lds_allowed);
-    if (e != hipSuccess) return (int)e;
-    return (int)launch_kernel(kernel, dim3((unsigned int)grid), dim3(WAVES * 64), lds, stream, KernelEvents{}, x, ids, a_q, a_k, scales, n, R, Tn, D,
-                              tiles, groups, (unsigned int)items, t);
+    const hipError_t attr = allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds, lds_allowed);
+    if (attr != hipSuccess) return (int)attr;
+    // A launch has less than 2^32 threads.  (A row has less than 2^32 bytes of at least 128 a token: less than 2^25 tokens, which fit.)
+    const int most = (int)(0xffffffffll / (WAVES * 64) / groups / 8 * 8 / tiles);
+    for (long long b = 0; b < B; b += most) {
+        const long long n_tiles = (B - b < most ? B - b : most) * tiles, items = n_tiles * groups, grid = (n_tiles + 7) / 8 * 8 * groups;
+        const int e = (int)launch_kernel(kernel, dim3((unsigned int)grid), dim3(WAVES * 64), lds, stream, KernelEvents{}, x + (size_t)b * Tn * D * 2,
+                                         ids + b, a_q, a_k, scales, n, R, Tn, D, tiles, groups, (unsigned int)items,
+                                         t + (size_t)b * adapter_row_bytes(Tn, R));
+        if (e != (int)hipSuccess) return e;
+    }
+    return (int)hipSuccess;
 }
 
 }  // namespace
 
-size_t adapter_workspace_bytes(int B, int Tn, int R) { return ((size_t)B * Tn * 2 * ((R + 15) / 16) * 64 + 255) / 256 * 256; }
+size_t adapter_workspace_bytes(int B, int Tn, int R) { return (B * adapter_row_bytes(Tn, R) + 255) / 256 * 256; }
 
 int launch_adapter_down(const void *x_, const int32_t *ids, const void *a_q_, const void *a_k_, const float *scales, int n, int R, int B, int Tn,
                         int D, void *t_, hipStream_t stream)

@@ -817,6 +817,8 @@ int chai_rotary_frequencies(int rot, double theta, int kind, double factor, doub
     return CHAI_OK;
 }
 
+constexpr int kMaxTurnTokens = 1 << 26;          // of a launch: a workgroup of 256 threads for every eight, less than 2^32 of them in one direction
+
 // What is common to rows that are turned.
 static int check_turn(int rot, int layout, int dtype, int d, const void *freq)
 {
@@ -842,7 +844,7 @@ int chai_rotate_qk(const void *q, const void *k, int64_t q_head_stride, int64_t 
     if (k && static_cast<const char *>(k) == static_cast<char *>(k_out) + (int64_t)pos0 * row_bytes_of(dtype) && k_head_stride != (int64_t)Tc_cap * d &&
         (long long)B * k_slots > 1)
         return CHAI_ERR_SHAPE;
-    if ((long long)B * Tn > 0x7fffffffll || 2ll * k_slots > kMaxGridYZ || (long long)pos0 + Tn > 0x7fffffffll) return CHAI_ERR_UNSUPPORTED;
+    if ((long long)B * Tn > kMaxTurnTokens || 2ll * k_slots > kMaxGridYZ || (long long)pos0 + Tn > 0x7fffffffll) return CHAI_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return CHAI_ERR_ALIGN;
     if (B == 0 || Tn == 0) return CHAI_OK;
     TurnShape sh;

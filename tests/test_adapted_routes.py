@@ -58,6 +58,19 @@ def test_shapes_of_the_first_half(launched):
     assert shapes == {("1", "1", "16"), ("2", "1", "16"), ("4", "1", "16"), ("1", "2", "16"), ("4", "4", "4")}
 
 
+def test_the_first_half_of_more_rows_than_a_launch_has_threads_for(tmp_path):
+    """A launch has less than 2^32 threads in a direction."""
+    got = launch_log.run(tmp_path, """
+        result = []
+        for B, Tn, R, part in ((5_000_000, 1, 8, None), (5_000_000, 3, 128, P), (40_000, 64, 128, P), (20_000, 64, 128, P), (70_000, 1000, 128, P)):
+            st = L.chai_project_qk_adapted(P, P, P, P, P, P, P, part, part, P, 3, R, B, 1, 1, Tn, 256, 128, 1, P, P, 0, Tn, P, N, None)
+            result.append([st, launches()])
+    """)
+    assert [sum("adapter_down_kernel" in n[0] for n in launches) for _, launches in got] == [2, 10, 2, 1, 2]      # rows of a launch: 4194296, 524280, 32766, 65535
+    for st, launches in got:
+        assert st == 0 and all(n[1] * n[2] < 1 << 32 for n in launches)
+
+
 def call(**kw):
     fields = (("x", FAKE), ("w_q", FAKE), ("w_k", FAKE), ("rep", FAKE), ("ids", FAKE), ("a_q", FAKE), ("b_q", FAKE), ("a_k", FAKE), ("b_k", FAKE),
               ("scale", FAKE), ("n", 3), ("R", 16), ("B", 2), ("H", 32), ("k", 8), ("Tn", 4), ("D", 512), ("d", 128), ("dtype", 1), ("q_out", FAKE),

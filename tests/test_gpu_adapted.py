@@ -249,3 +249,32 @@ def test_two_calls_at_once(kernel):
     torch.cuda.synchronize()
     for g, w in zip(got, want):
         assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+
+
+def test_more_rows_than_a_launch_has_threads_for():
+    """4 194 296 rows of one group of ranks are a launch's: rows on both sides of that against 64 bits."""
+    B, D, R, n = 4_194_400, 128, 8, 5
+    print(f"[adapted] {B} rows", flush=True)
+    x = Inputs(97, 1, 1, 1, 1, D, R, n)
+    rows = torch.arange(B, device="cuda")
+    xs = (rows[:, None] * 7 + torch.arange(D, device="cuda") * 3).remainder_(31).sub_(15).to(BF16).view(B, 1, D)
+    ids = rows.remainder(n + 1).sub_(1).to(torch.int32)
+    rep = torch.zeros((B, 1), dtype=torch.int32, device="cuda")
+    q, kc = (torch.zeros((B, 1, 1, D_HEAD), dtype=BF16, device="cuda") for _ in "qk")
+    ws = C.alloc_adapted_workspace(B, 1, R)
+    C.chai_project_qk_adapted(xs, x.w["q"], x.w["k"], rep, ids, x.a["q"], x.b["q"], None, None, x.scale, q, kc, 0, ws)
+    torch.cuda.synchronize()
+    for b in (0, 1, 4_194_294, 4_194_295, 4_194_296, 4_194_297, 4_194_303, 4_194_304, B - 1):
+        one = Inputs(97, 1, 1, 1, 1, D, R, n)
+        one.a["k"] = one.b["k"] = None
+        one.x, one.rep, one.ids = xs[b:b + 1], np.zeros((1, 1), np.int64), np.array([int(ids[b])])
+        one.check(q[b:b + 1], kc[b:b + 1])
+    mine = ids.long()
+    t = sum((mine == a).double()[:, None] * x.scale[a].double() * (xs[:, 0].double() @ x.a["q"][a].double().t().contiguous()) for a in range(n))
+    want = xs[:, 0].double() @ x.w["q"].double().t().contiguous()
+    for a in range(n):
+        want += (mine == a).double()[:, None] * (t @ x.b["q"][a].double().t().contiguous())
+    # a sum's magnitudes: 15 (2 D^-0.5 ...) are bounded by their largest over all rows
+    bound = 15 * (x.w["q"].double().abs().sum(1) + 2 * (x.b["q"].double().abs().max(0)[0] @ x.a["q"].double().abs().max(0)[0].sum(1)))
+    worst = ((q[:, 0, 0].double() - want).abs() - 2.0 ** -8 * want.abs() - (3e-6 + 2.0 ** -17) * bound).max()
+    assert float(worst) <= 0.0

@@ -83,6 +83,7 @@ def test_rotated_blocks():
     assert rotate(rot=0) == SHAPE and rotate(rot=-16) == SHAPE and rotate(rot=144) == SHAPE and rotate(layout=2) == SHAPE
     assert rotate(rot=24) == UNSUPPORTED and rotate(d=64, rot=64) == UNSUPPORTED
     assert rotate(B=1 << 20, Tn=1 << 12, q_stride=1 << 20, k_stride=1 << 20, Tc_cap=1 << 13) == UNSUPPORTED
+    assert rotate(B=1, H=1, k_slots=1, Tn=(1 << 26) + 1, q_stride=1 << 40, k_stride=1 << 40, Tc_cap=1 << 30) == UNSUPPORTED
     assert rotate(q=FAKE + 8) == ALIGN and rotate(k_out=FAKE + 4) == ALIGN and rotate(freq=FAKE + 4) == ALIGN
     assert rotate(B=0) == 0 and rotate(Tn=0) == 0
 
