@@ -626,7 +626,8 @@ int chai_paged_decode_step(const void *q, const void *k_new, const void *v_new, 
  *     free_pages, block_table  changed;  new_lens [B], n_left [1] written (may
  *     be seq_lens, n_free)
  * workspace: chai_paged_place_workspace_bytes(B) (0 on invalid sizes; never
- *   decreases), 256-byte aligned, contents need not be initialised.
+ *   decreases), 256-byte aligned, contents need not be initialised.  Two calls
+ *   that run concurrently need separate workspaces.
  * B = 0: no tokens (token_rows, positions, slots, n_left and offsets are not
  * written).  B <= 4096, N <= 2^24, n_pages * page < 2^31, page a multiple of 8.
  */
