@@ -725,8 +725,8 @@ int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new
  * adapter_ids[b], s_a its factor, slot j with r = rep_heads[b][j] >= 0):
  *   q_out[b][r][i][:]            = x[b][i] . w_q[r]^T + s_a (x[b][i] . a_q[a]^T) . b_q[a][r]^T
  *   k_compact[b][j][pos0 + i][:] = the same with w_k, a_k, b_k
- * Products accumulate in fp32; (s_a x a^T) is held in 16 bits of mantissa (two
- * bf16), their sum in fp32, and that is rounded once to bf16.
+ * Products accumulate in fp32; (s_a x a^T) keeps the 24 bits that it then has
+ * (as three bf16), and the sum of both products is rounded once to bf16.
  *
  *   adapter_ids   [B] int32 on the device; a row whose id is outside
  *                 [0,n_adapters) has no adapter

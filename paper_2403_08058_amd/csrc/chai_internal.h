@@ -137,13 +137,14 @@ int launch_project_qk(const void *x, const void *w_q, const void *w_k, const int
 
 // The same with a low-rank adapter of every row's own: first t = s_a x A_a^T of all tokens, then the projections, which add t B_a^T.
 struct AdapterUse {
-    const char *t = nullptr;             // [B,Tn][2 (queries, keys)][chunks][hi of 16 ranks | lo] bf16
+    const char *t = nullptr;             // [B,Tn][2 (queries, keys)][chunks][upper | middle | lower 8 bits of 16 ranks] bf16
     const char *b_q = nullptr, *b_k = nullptr;           // [n,H*128,R] bf16, or NULL: none of that part
     const int32_t *ids = nullptr;        // [B]
     int n = 0, R = 0;
     __host__ __device__ int chunks() const { return (R + 15) / 16; }
 };
 constexpr int kMaxAdapterRank = 128;
+constexpr int kAdapterChunkBytes = 3 * 16 * 2;           // of t: sixteen ranks, three bf16 each
 size_t adapter_workspace_bytes(int B, int Tn, int R);
 int launch_adapter_down(const void *x, const int32_t *ids, const void *a_q, const void *a_k, const float *scales, int n, int R, int B, int Tn,
                         int D, void *t, hipStream_t stream);

@@ -59,9 +59,9 @@ __device__ __forceinline__ void unroll(F &&f)
 }
 
 // Low-rank adapters of the rows' own (chai_project_qk_adapted): the kernels below add t B_a^T to a token's products, where t = s_a x A_a^T
-// [R] of the token, made before (adapter.hip), is held as two bf16, t = hi + lo to 2^-17 of it (16 bits of 24: the product's sum is
-// rounded to 8), sixteen ranks' hi and their lo one behind the other: a chunk of 32 is a product's depth, and meets the sixteen columns
-// of B_a twice.  NoAdapters: the kernels as they are without.
+// [R] of the token, made before (adapter.hip), is held as three bf16, t = hi + mid + lo with all of its 24 bits, those of sixteen ranks one
+// behind the other.  hi and mid are a product's depth, 32, and meet the sixteen columns of B_a twice; lo is a second product's, half of
+// which is zeros.  NoAdapters: the kernels as they are without.
 struct NoAdapters {
     static constexpr bool any = false;
 };
@@ -74,7 +74,7 @@ struct Adapters : AdapterUse {
     }
     // lane group g's eight ranks of chunk c
     __device__ __forceinline__ bool inside(int c, int g) const { return c * 16 + (g & 1) * 8 < R; }
-    __device__ __forceinline__ const char *token(size_t token, int part) const { return t + (token * 2 + part) * (size_t)(chunks() * 64); }
+    __device__ __forceinline__ const char *token(size_t token, int part) const { return t + (token * 2 + part) * (size_t)(chunks() * kAdapterChunkBytes); }
     __device__ __forceinline__ const char *column(int part, int a, int H, int head, int f) const
     {
         return (part == 0 ? b_q : b_k) + (((size_t)a * H + head) * kHeadDim + f) * (size_t)(R * 2);
@@ -88,7 +88,12 @@ struct Adapters : AdapterUse {
     }
     __device__ __forceinline__ u32x4 token_piece(const char *row, int c, int g) const
     {
-        return only(inside(c, g), *reinterpret_cast<const u32x4 *>(row + c * 64 + g * 16));
+        return only(inside(c, g), *reinterpret_cast<const u32x4 *>(row + c * kAdapterChunkBytes + g * 16));
+    }
+    // lo, for the first two lane groups of a product
+    __device__ __forceinline__ u32x4 token_rest(const char *row, int c, int g) const
+    {
+        return only(g < 2 && inside(c, g), *reinterpret_cast<const u32x4 *>(row + c * kAdapterChunkBytes + 64 + (g & 1) * 16));
     }
     __device__ __forceinline__ u32x4 column_piece(const char *row, int c, int g) const
     {
@@ -140,9 +145,13 @@ __device__ __forceinline__ void add_adapters(const Adapters &ad, f32x4 (&acc)[NB
         for (int c = 0; c < ad.chunks(); ++c) {
             int i = first;
             if (i < n_list) {
-                Frag x[TT];
+                Frag x[TT], rest[TT];
 #pragma unroll
-                for (int t = 0; t < TT; ++t) x[t].raw = ad.token_piece(ad.token((size_t)b[t] * Tn + tok[t], part), c, g);
+                for (int t = 0; t < TT; ++t) {
+                    const char *const row = ad.token((size_t)b[t] * Tn + tok[t], part);
+                    x[t].raw = ad.token_piece(row, c, g);
+                    rest[t].raw = ad.token_rest(row, c, g);
+                }
                 for (; i < n_list; i += WAVES) {
                     const int a = __builtin_amdgcn_readlane(list, i);
                     Frag y[NB];
@@ -153,7 +162,8 @@ __device__ __forceinline__ void add_adapters(const Adapters &ad, f32x4 (&acc)[NB
                     for (int n = 0; n < NB; ++n)
 #pragma unroll
                         for (int t = 0; t < TT; ++t) {
-                            const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n].bf, x[t].bf, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                            f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n].bf, x[t].bf, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[n].bf, rest[t].bf, d, 0, 0, 0);
                             const bool own = id[t] == a && (f0 + n * 16 + g * 4) / kHeadDim == part;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) acc[n][t][e] = own ? acc[n][t][e] + d[e] : acc[n][t][e];
@@ -365,13 +375,16 @@ __global__ __launch_bounds__(kJBlock, 1) void project_kernel(A given, const char
                     const int r2 = l2 & 15, g2 = l2 >> 4;
                     const char *cols = ad.column(wn, id, H, now.head, r2);
                     unroll<8>([&](auto nb) { fa[1][decltype(nb)::value].raw = ad.column_piece(cols + decltype(nb)::value * 16 * (size_t)(ad.R * 2), c, g2); });
+                    Frag rest[8];
                     unroll<8>([&](auto tb) {
                         const int tok = min(now.t0 + wm * 128 + decltype(tb)::value * 16 + r2, Tn - 1);
-                        fb[1][decltype(tb)::value].raw = ad.token_piece(ad.token((size_t)now.b * Tn + tok, wn), c, g2);
+                        const char *const row = ad.token((size_t)now.b * Tn + tok, wn);
+                        fb[1][decltype(tb)::value].raw = ad.token_piece(row, c, g2);
+                        rest[decltype(tb)::value].raw = ad.token_rest(row, c, g2);
                     });
-                    unroll<64>([&](auto nc) {
-                        constexpr int n = decltype(nc)::value, nb = n >> 3, tb = (nb & 1) ? 7 - (n & 7) : n & 7;
-                        acc[nb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][nb].bf, fb[1][tb].bf, acc[nb][tb], 0, 0, 0);
+                    unroll<128>([&](auto nc) {
+                        constexpr int n = decltype(nc)::value & 63, nb = n >> 3, tb = (nb & 1) ? 7 - (n & 7) : n & 7;
+                        acc[nb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][nb].bf, decltype(nc)::value < 64 ? fb[1][tb].bf : rest[tb].bf, acc[nb][tb], 0, 0, 0);
                     });
                 }
             }
@@ -906,7 +919,7 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
     if (my_steps > 0) stage(0, 0);
     if (my_steps > 1) stage(1, 1);
     if constexpr (A::any) {
-        // As add_adapters, with tiles of 32 features x 32 tokens: hi and lo are a product each.  The teams deal (chunk, adapter) out.
+        // As add_adapters, with tiles of 32 features x 32 tokens: hi, mid and lo are a product each.  The teams deal (chunk, adapter) out.
         const int item = min(c0 + wm * 32 + r, n_items - 1), row = slots[item / Tn] / k, tok = item % Tn, part = f0 < kHeadDim ? 0 : 1;
         const int id[1] = {(part == 0 ? ad.b_q : ad.b_k) != nullptr ? ad.of(row) : -1};
         int n_list;
@@ -917,9 +930,10 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
         for (int c = 0; c < ad.chunks(); ++c) {
             int i = first_of;
             if (i < n_list) {
-                Frag t[2];
+                Frag t[3];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) t[e].raw = ad.token_piece(trow, c, 2 * e + hl);
+                t[2].raw = ad.token_rest(trow, c, hl);
                 for (; i < n_list; i += kJtTeams) {
                     const int a = __builtin_amdgcn_readlane(list, i);
                     Frag col[NB];
@@ -931,7 +945,7 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
 #pragma unroll
                         for (int e = 0; e < 16; ++e) d[e] = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col[nb].bf, t[e].bf, d, 0, 0, 0);
+                        for (int e = 0; e < 3; ++e) d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col[nb].bf, t[e].bf, d, 0, 0, 0);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) acc[nb][e] = id[0] == a ? acc[nb][e] + d[e] : acc[nb][e];
                     }
@@ -1268,7 +1282,7 @@ int launch_project_qk_adapted(const void *x, const void *w_q, const void *w_k, c
         Adapters ad;
         static_cast<AdapterUse &>(ad) = use;
         ad.ids += b;
-        ad.t += (size_t)b * Tn * 2 * use.chunks() * 64;
+        ad.t += (size_t)b * Tn * 2 * use.chunks() * kAdapterChunkBytes;
         const int e = launch_project(static_cast<const char *>(x) + (size_t)b * Tn * D * 2, w_q, w_k, rep + (size_t)b * k, n, H, k, Tn, D,
                                      static_cast<char *>(q_out) + (size_t)b * H * Tn * (kHeadDim * 2),
                                      static_cast<char *>(k_compact) + (size_t)b * k * Tc_cap * (kHeadDim * 2), pos0, Tc_cap, ad, KernelEvents{}, stream);
