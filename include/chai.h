@@ -648,7 +648,7 @@ int chai_paged_release_pages(const int32_t *keep, const int32_t *seq_lens, int32
  *     (a, b) -> gain * (a cos - b sin, a sin + b cos)
  *     layout CHAI_ROPE_HALVES: elements i and i + rot / 2
  *            CHAI_ROPE_PAIRS:  elements 2 i and 2 i + 1
- * Elements from rot on stay as they are.  Angles, turns and products are in
+ * Elements from rot on stay as they are.  Angles, turns, gain, products are in
  * 64 bits, rounded once to fp32 and from there to the stored type.  rot is a
  * multiple of 16 up to d; freq [rot/2] is on the device, in 64 bits, radians
  * per position (at most pi); a negative position turns back.
@@ -684,7 +684,7 @@ int chai_rotary_frequencies(int rot, double theta, int kind, double factor, doub
                             double *freq);
 int chai_rotate_qk(const void *q, const void *k, int64_t q_head_stride, int64_t k_head_stride, const int32_t *rep_heads,
                    const int32_t *positions, const double *freq, int B, int H, int k_slots, int Tn, int pos0, int Tc_cap, int d,
-                   int rot, int layout, int dtype, float gain, void *q_out, void *k_out, void *stream);
+                   int rot, int layout, int dtype, double gain, void *q_out, void *k_out, void *stream);
 
 /*
  * chai_paged_append_packed: N tokens one behind the other, of any rows, into
@@ -717,7 +717,7 @@ int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new
                              const int32_t *slots, const double *freq, void *q_out, int64_t out_token_stride,
                              int64_t out_head_stride, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int N,
                              int B, int H, int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype,
-                             float gain, void *stream);
+                             double gain, void *stream);
 
 /*
  * chai_project_qk with a low-rank adapter of every row's own beside the shared

@@ -103,8 +103,8 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.chai_paged_release_pages.argtypes = [vp] * 5 + [ci] * 4 + [vp] * 3
     cd = ctypes.c_double
     L.chai_rotary_frequencies.argtypes = [ci, cd, ci, cd, cd, cd, cd, vp]
-    L.chai_rotate_qk.argtypes = [vp, vp, i64, i64, vp, vp, vp] + [ci] * 10 + [cf, vp, vp, vp]
-    L.chai_paged_append_packed.argtypes = [vp] * 3 + [i64] * 6 + [ci] + [vp] * 6 + [i64] * 2 + [vp] * 4 + [ci] * 11 + [cf, vp]
+    L.chai_rotate_qk.argtypes = [vp, vp, i64, i64, vp, vp, vp] + [ci] * 10 + [cd, vp, vp, vp]
+    L.chai_paged_append_packed.argtypes = [vp] * 3 + [i64] * 6 + [ci] + [vp] * 6 + [i64] * 2 + [vp] * 4 + [ci] * 11 + [cd, vp]
     L.chai_project_adapted_workspace_bytes.restype = sz
     L.chai_project_adapted_workspace_bytes.argtypes = [ci] * 3
     L.chai_project_qk_adapted.argtypes = [vp] * 10 + [ci] * 9 + [vp, vp, ci, ci, vp, sz, vp]

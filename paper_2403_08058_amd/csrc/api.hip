@@ -831,7 +831,7 @@ static int check_turn(int rot, int layout, int dtype, int d, const void *freq)
 
 int chai_rotate_qk(const void *q, const void *k, int64_t q_head_stride, int64_t k_head_stride, const int32_t *rep_heads,
                    const int32_t *positions, const double *freq, int B, int H, int k_slots, int Tn, int pos0, int Tc_cap, int d,
-                   int rot, int layout, int dtype, float gain, void *q_out, void *k_out, void *stream)
+                   int rot, int layout, int dtype, double gain, void *q_out, void *k_out, void *stream)
 {
     if (B != 0 && Tn != 0 && ((!q != !q_out) || (!k != !k_out) || (!q && !k))) return CHAI_ERR_NULL;
     const int st = check_turn(rot, layout, dtype, d, freq);
@@ -855,7 +855,7 @@ int chai_rotate_qk(const void *q, const void *k, int64_t q_head_stride, int64_t 
     sh.H = H;
     sh.k = k_slots;
     sh.rot = rot;
-    sh.gain = (double)gain;
+    sh.gain = gain;
     sh.Tn = Tn;
     sh.pos0 = pos0;
     sh.Tc_cap = Tc_cap;
@@ -876,7 +876,7 @@ int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new
                              const int32_t *slots, const double *freq, void *q_out, int64_t out_token_stride,
                              int64_t out_head_stride, void *k_pages, void *v_pages, float *k_scales, float *v_scales, int N,
                              int B, int H, int k, int n_pages, int page, int d, int rot, int layout, int dtype, int cache_dtype,
-                             float gain, void *stream)
+                             double gain, void *stream)
 {
     if (N != 0 && (!k_new || !v_new || !token_rows || !slots || (rot != 0 && !positions) || (!q != !q_out))) return CHAI_ERR_NULL;
     PagedShape ps;
@@ -909,7 +909,7 @@ int chai_paged_append_packed(const void *q, const void *k_new, const void *v_new
     sh.H = H;
     sh.k = k;
     sh.rot = rot;
-    sh.gain = (double)gain;
+    sh.gain = gain;
     sh.rows = token_rows;
     sh.slots = slots;
     sh.N = N;
