@@ -759,11 +759,11 @@ def _tokens_of(fn, name, t, shape, dtype):
 def chai_paged_append_packed(q, k_new, v_new, rep_heads, token_rows, positions, slots, freq, q_out, k_pages, v_pages, k_scales=None,
                              v_scales=None, layout: int = CHAI_ROPE_HALVES, gain: float = 1.0, k_by_slot: Optional[bool] = None,
                              stream=None):
-    """N tokens one behind the other: keys k_new [N,H,d] (or [N,k,d], k_by_slot: the representatives' alone; None: by the shape) and
-    values v_new [N,H,d] into their slots of the pages, queries q [N,H,d] of the representatives -> q_out [N,H,d] (may be q; both
-    may be None).  Queries and keys are turned by positions times freq [rot/2] (64 bits; None: as they are).  token_rows, positions,
-    slots [N] int32 as chai_paged_place_tokens gives them; rep_heads [B,k], or None for every head (k = H).  Queries, keys and values may
-    be views (parts of wider rows, or a row's block [heads,N,d] transposed)."""
+    """N tokens one behind the other: keys k_new [N,H,d] (or [N,k,d], k_by_slot: the representatives' alone; None: by the shape, which
+    maps of k = H heads leave open: refused) and values v_new [N,H,d] into their slots of the pages, queries q [N,H,d] of the
+    representatives -> q_out [N,H,d] (may be q; both may be None).  Queries and keys are turned by positions times freq [rot/2] (64
+    bits; None: as they are).  token_rows, positions, slots [N] int32 as chai_paged_place_tokens gives them; rep_heads [B,k], or None
+    for every head (k = H).  Queries, keys and values may be views (parts of wider rows, or a row's block [heads,N,d] transposed)."""
     fn = "chai_paged_append_packed"
     n_pages, k, page, d = k_pages.shape
     shape = v_new.shape
@@ -773,6 +773,8 @@ def chai_paged_append_packed(q, k_new, v_new, rep_heads, token_rows, positions, 
     if (q is None) != (q_out is None):
         _misfit(fn, "queries with what they are written to")
     if k_by_slot is None:
+        if k == H > 1 and rep_heads is not None:           # (the other reading would write other heads' keys)
+            _misfit(fn, f"k_by_slot has to say whether the {H} keys of a token are its heads' or its slots'")
         k_by_slot = k_new.shape[1] != H
     B = _MOST_ROWS                                         # (without maps a row is only a number that is not below 0)
     if rep_heads is not None:
