@@ -1,10 +1,11 @@
 // The first half of a low-rank adapter: t = s_a x A_a^T of every token, a = the adapter of the token's row.  The projections add the second
 // half, t B_a^T, to what they sum up (project.hip).
 //
-//   x [B,Tn,D], A [n,R,D] bf16, queries' and keys' apart;  t [B,Tn][2][chunks][3][16] bf16: of sixteen ranks the upper 8 bits of t, the next
-//   8 and the last 8: all of its 24.  (In the upper 16 alone it is the largest error of the call before its rounding: it then decides that of
-//   0.17 % of the outputs, 16 rows x 1 token, width 4096, rank 16, and the order of all sums together that of 0.02 %.  The lower 8 cost
-//   nothing there; 1 x 1777 tokens of 16 heads, rank 64, 160 -> 164 us, 4 x 2043 of 8, rank 128, 180 -> 190.)
+//   x [B,Tn,D], A [n,R,D] bf16, queries' and keys' apart;  t [B,Tn][2][chunks][3][16] bf16: of sixteen ranks the upper 8 bits of t (half
+//   of that number, which is taken twice), the next 8 and the last 8: all of its 24.  (In the upper 16 alone it is the largest error of the
+//   call before its rounding: it then decides that of 0.17 % of the outputs, 16 rows x 1 token, width 4096, rank 16, and the order of all
+//   sums together that of 0.02 %.  The lower 8 cost nothing there; 1 x 1777 tokens of 16 heads, rank 64, 164 -> 168 us, 4 x 2043 of 8, rank
+//   128, 181 -> 194.)
 //
 // A workgroup takes the ranks of U units of 8 (of queries, then of keys) for 8 XT tokens of one row.  As in the projections of few tokens,
 // its waves deal the contraction out in blocks of 64 elements and stream their blocks, ranks and tokens, through rings of their own in LDS,
@@ -47,8 +48,19 @@ __device__ __forceinline__ void unroll(F &&f)
     unroll_seq(f, std::make_integer_sequence<int, N>{});
 }
 
-// the upper 8 bits of a number's mantissa: a bf16
-__device__ __forceinline__ float upper(float y) { return __uint_as_float(__float_as_uint(y) & 0xffff0000u); }
+// y = 2 hi + mid + lo, each of 8 bits of mantissa and of y's sign, none 0 unless y is: cut below the number next to it, so that something
+// is left for the next.  0, infinities and NaN are all three.  (Below 2^-95 what is left is too small for a bf16, and 0.)
+struct Parts {
+    float hi, mid, lo;
+};
+__device__ __forceinline__ Parts parts_of(float y)
+{
+#pragma clang fp contract(off)
+    auto below = [](float x) { return __uint_as_float((__float_as_uint(x) - 1u) & 0xffff0000u); };
+    if (y == 0.f || y - y != 0.f) return Parts{y, y, y};
+    const float hi = below(y), rest = y - hi, mid = below(rest);
+    return Parts{0.5f * hi, mid, rest - mid};
+}
 
 constexpr int wave_bytes(int waves) { return waves > 8 ? 10 * 1024 : 20 * 1024; }      // ring of a wave
 constexpr int kAdMostAhead = 8;
@@ -165,11 +177,10 @@ __global__ __launch_bounds__(WAVES * 64) void adapter_down_kernel(const char *__
         bf16x4 hi, mid, lo;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            // (cut, not rounded: the parts add up to y in any order; what a part of an infinity or NaN leaves is 0)
-            const float y = scale * sum[e], y_hi = upper(y), rest = y - y_hi, y_mid = rest - rest == 0.f ? upper(rest) : 0.f;
-            hi[e] = (__bf16)(rest - rest == 0.f ? y_hi : y);
-            mid[e] = (__bf16)y_mid;
-            lo[e] = (__bf16)(rest - rest == 0.f ? rest - y_mid : 0.f);
+            const Parts y = parts_of(scale * sum[e]);
+            hi[e] = (__bf16)y.hi;
+            mid[e] = (__bf16)y.mid;
+            lo[e] = (__bf16)y.lo;
         }
         char *to = t + (((size_t)b * Tn + tok) * 2 + part) * (size_t)((R + 15) / 16 * kAdapterChunkBytes) + rank / 16 * kAdapterChunkBytes + rank % 16 * 2;
         *reinterpret_cast<bf16x4 *>(to) = hi;

@@ -59,9 +59,10 @@ __device__ __forceinline__ void unroll(F &&f)
 }
 
 // Low-rank adapters of the rows' own (chai_project_qk_adapted): the kernels below add t B_a^T to a token's products, where t = s_a x A_a^T
-// [R] of the token, made before (adapter.hip), is held as three bf16, t = hi + mid + lo with all of its 24 bits, those of sixteen ranks one
-// behind the other.  hi and mid are a product's depth, 32, and meet the sixteen columns of B_a twice; lo is a second product's, half of
-// which is zeros.  NoAdapters: the kernels as they are without.
+// [R] of the token, made before (adapter.hip), is held as three bf16, t = 2 hi + mid + lo with all of its 24 bits, those of sixteen ranks one
+// behind the other.  hi and mid are a product's depth, 32, hi and lo another's, and meet the sixteen columns of B_a twice.  All three have the
+// sign of t, and none is 0 (nor are there zeros beside lo) unless t is: 0 times an infinity in B_a would be NaN where t times it is not.
+// NoAdapters: the kernels as they are without.
 struct NoAdapters {
     static constexpr bool any = false;
 };
@@ -90,10 +91,9 @@ struct Adapters : AdapterUse {
     {
         return only(inside(c, g), *reinterpret_cast<const u32x4 *>(row + c * kAdapterChunkBytes + g * 16));
     }
-    // lo, for the first two lane groups of a product
-    __device__ __forceinline__ u32x4 token_rest(const char *row, int c, int g) const
+    __device__ __forceinline__ u32x4 token_rest(const char *row, int c, int g) const   // the same of the second product: hi and lo
     {
-        return only(g < 2 && inside(c, g), *reinterpret_cast<const u32x4 *>(row + c * kAdapterChunkBytes + 64 + (g & 1) * 16));
+        return only(inside(c, g), *reinterpret_cast<const u32x4 *>(row + c * kAdapterChunkBytes + (g < 2 ? g : g + 2) * 16));
     }
     __device__ __forceinline__ u32x4 column_piece(const char *row, int c, int g) const
     {
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(kJBlock, 1) void project_kernel(A given, const char
                     });
                     unroll<128>([&](auto nc) {
                         constexpr int n = decltype(nc)::value & 63, nb = n >> 3, tb = (nb & 1) ? 7 - (n & 7) : n & 7;
-                        acc[nb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][nb].bf, decltype(nc)::value < 64 ? fb[1][tb].bf : rest[tb].bf, acc[nb][tb], 0, 0, 0);
+                        acc[nb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][nb].bf, decltype(nc)::value == n ? fb[1][tb].bf : rest[tb].bf, acc[nb][tb], 0, 0, 0);
                     });
                 }
             }
@@ -919,7 +919,7 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
     if (my_steps > 0) stage(0, 0);
     if (my_steps > 1) stage(1, 1);
     if constexpr (A::any) {
-        // As add_adapters, with tiles of 32 features x 32 tokens: hi, mid and lo are a product each.  The teams deal (chunk, adapter) out.
+        // As add_adapters, with tiles of 32 features x 32 tokens: hi (twice), mid and lo are a product each.  The teams deal (chunk, adapter) out.
         const int item = min(c0 + wm * 32 + r, n_items - 1), row = slots[item / Tn] / k, tok = item % Tn, part = f0 < kHeadDim ? 0 : 1;
         const int id[1] = {(part == 0 ? ad.b_q : ad.b_k) != nullptr ? ad.of(row) : -1};
         int n_list;
@@ -933,7 +933,7 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
                 Frag t[3];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) t[e].raw = ad.token_piece(trow, c, 2 * e + hl);
-                t[2].raw = ad.token_rest(trow, c, hl);
+                t[2].raw = ad.token_rest(trow, c, 2 + hl);
                 for (; i < n_list; i += kJtTeams) {
                     const int a = __builtin_amdgcn_readlane(list, i);
                     Frag col[NB];
@@ -945,7 +945,7 @@ __device__ __forceinline__ void project_tile(const char *__restrict__ x, const c
 #pragma unroll
                         for (int e = 0; e < 16; ++e) d[e] = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 3; ++e) d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col[nb].bf, t[e].bf, d, 0, 0, 0);
+                        for (int e = 0; e < 4; ++e) d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col[nb].bf, t[e < 2 ? 0 : e - 1].bf, d, 0, 0, 0);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) acc[nb][e] = id[0] == a ? acc[nb][e] + d[e] : acc[nb][e];
                     }

@@ -37,3 +37,35 @@ def test_the_first_half_has_all_its_bits(kernel, B, H, k, Tn, D, R):
         used = x.rep[b][x.rep[b] >= 0]
         assert bool((q[b, used] == 1.5 * 2.0 ** -20).all()), (b, q[b, used].unique())
         assert bool((kc[b, x.rep[b] >= 0] == 1.5 * 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("R", [8, 24])
+@pytest.mark.parametrize("kernel,B,H,k,Tn,D", SIZES)
+def test_infinities_of_adapters_are_the_formulas(kernel, B, H, k, Tn, D, R):
+    """An infinite element of B_a gives infinities of the sign that x A_a^T has there, one of A_a those of x times B_a's, and where they meet NaN
+    (opposite signs, 0 times infinity); columns without are as without."""
+    print(f"[adapted] infinities, {kernel} {B} x {Tn} tokens, {k} of {H}, width {D}, rank {R}", flush=True)
+    x = Inputs(13, B, H, k, Tn, D, R, n=4)
+    x.ids[:] = np.arange(B) % 4
+    inf = float("inf")
+    for p in "qk":
+        up = x.b[p].view(4, H, 128, R)
+        up[0, :, 5, 2], up[0, :, 77, R - 1], up[0, :, 100, 0], up[0, :, 100, 1] = inf, -inf, inf, inf
+        up[1, :, 9, 3], up[1, :, 64, 0] = -inf, float("nan")
+        x.a[p][2, 6, D // 2] = inf
+        up[2, :, 31, 6] = 0.0
+        x.a[p][3, 4] = 0.0
+        up[3, :, 12, 4] = inf
+    q, kc = x.run()
+    for b in sorted({0, 1, 2, 3, B // 2, B - 1} & set(range(B))):
+        a, rows = int(x.ids[b]), x.x[b].double()
+        for p in "qk":
+            t = float(x.scale[a]) * (rows @ x.a[p][a].double().t().contiguous())
+            for j, r in enumerate(x.rep[b]):
+                if r < 0:
+                    continue
+                cols = slice(r * 128, (r + 1) * 128)
+                want = rows @ x.w[p][cols].double().t().contiguous() + t @ x.b[p][a, cols].double().t().contiguous()
+                got = (q[b, r] if p == "q" else kc[b, j]).double()
+                assert torch.equal(torch.isnan(got), torch.isnan(want)), (b, j, p, a)
+                assert torch.equal(torch.where(torch.isinf(got), got, 0.0), torch.where(torch.isinf(want), want, 0.0)), (b, j, p, a)
