@@ -69,3 +69,33 @@ def test_infinities_of_adapters_are_the_formulas(kernel, B, H, k, Tn, D, R):
                 got = (q[b, r] if p == "q" else kc[b, j]).double()
                 assert torch.equal(torch.isnan(got), torch.isnan(want)), (b, j, p, a)
                 assert torch.equal(torch.where(torch.isinf(got), got, 0.0), torch.where(torch.isinf(want), want, 0.0)), (b, j, p, a)
+
+
+@pytest.mark.parametrize("kernel,B,H,k,Tn,D", [(kernel, *c[0]) for kernel, c in CASES.items()])
+@pytest.mark.parametrize("power", [-95, -118, -126, -140])
+def test_small_first_halves(kernel, B, H, k, Tn, D, power):
+    """t of about 2^power, down to where 32 bits are subnormal: the bars of test_gpu_adapted.py, and four parts that may lose what they
+    have below 2^-126."""
+    x = Inputs(15, B, H, k, Tn, D, 16, n=2)
+    x.ids[:] = np.arange(B) % 2
+    for p in "qk":
+        x.w[p].zero_()
+        x.a[p].zero_()
+        x.a[p][:, :, :8] = torch.randn((2, 16, 8), device="cuda").mul_(2.0 ** -20).to(torch.bfloat16)
+        x.b[p].mul_(2.0 ** 100)
+    x.scale.fill_(2.0 ** (power + 20) if power > -140 else 2.0 ** -120)
+    q, kc = x.run()
+    for b in {0, B // 2, B - 1}:
+        a, rows = int(x.ids[b]), x.x[b].double()
+        for p in "qk":
+            down = x.a[p][a].double().t().contiguous()
+            s = float(x.scale[a])
+            t, mag_t = s * (rows @ down), s * (rows.abs() @ down.abs())
+            for j, r in enumerate(x.rep[b]):
+                if r < 0:
+                    continue
+                up = x.b[p][a, r * 128:(r + 1) * 128].double().t().contiguous()
+                want = t @ up
+                allowed = 2.0 ** -8 * want.abs() + (3e-6 * mag_t + (2.0 ** -17 + 2.0 ** -24 + 3e-6) * t.abs() + 4 * 2.0 ** -126) @ up.abs()
+                got = (q[b, r] if p == "q" else kc[b, j]).double()
+                assert bool(((got - want).abs() <= allowed).all()), (b, j, p, float(((got - want).abs() / allowed).max()))
