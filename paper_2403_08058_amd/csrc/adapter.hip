@@ -4,16 +4,16 @@
 //   x [B,Tn,D], A [n,R,D] bf16, queries' and keys' apart;  t [B,Tn][2][chunks][3][16] bf16: of sixteen ranks the upper 8 bits of t (half
 //   of that number, which is taken twice), the next 8 and the last 8: all of its 24.  (In the upper 16 alone it is the largest error of the
 //   call before its rounding: it then decides that of 0.17 % of the outputs, 16 rows x 1 token, width 4096, rank 16, and the order of all
-//   sums together that of 0.02 %.  The lower 8 cost nothing there; 1 x 1777 tokens of 16 heads, rank 64, 164 -> 168 us, 4 x 2043 of 8, rank
+//   sums together that of 0.02 %.  The lower 8 cost nothing there; 1 x 1777 tokens of 16 heads, rank 64, 160 -> 164 us, 4 x 2043 of 8, rank
 //   128, 181 -> 194.)
 //
 // A workgroup takes the ranks of U units of 8 (of queries, then of keys) for 8 XT tokens of one row.  As in the projections of few tokens,
 // its waves deal the contraction out in blocks of 64 elements and stream their blocks, ranks and tokens, through rings of their own in LDS,
 // without a barrier before the sums of all waves are added in wave order.
 //
-// What bounds it: of prompts HBM, which the activations come from once more (16 rows x 2043 tokens, width 4096: 268 MB in 56 us, 4.8 TB/s; a
-// stretch of blocks for each wave, so that a row's neighbouring lines are asked for by one, takes 48 us, but the projections that follow run
-// at the clock that their power leaves and give it back: both 470 together, and few tokens take 0.3 to 1 us longer so).  Making t in the
+// What bounds it: of prompts HBM, which the activations come from once more (16 rows x 2043 tokens, width 4096: 293 MB fetched in 65 us, 4.5
+// TB/s; a stretch of blocks for each wave, so that a row's neighbouring lines are asked for by one, takes a seventh less, but the projections
+// that follow run at the clock that their power leaves and give it back, and few tokens take 0.3 to 1 us longer so).  Making t in the
 // projections' own tiles instead would cost them an eighth more products.  Of few tokens launch, look-up and ramp, 4 to 5 us; rows of one
 // adapter in one workgroup, which reads its ranks once, take 0.8 us more to be found and give nothing back (L2 holds them).
 #include "chai_internal.h"
@@ -225,7 +225,8 @@ int launch_adapter_down(const void *x_, const int32_t *ids, const void *a_q_, co
     // Few tokens of a row: as many workgroups as there are eights of ranks and tokens, of sixteen waves, while that is a round of the chip
     // (8 rows x 37 tokens, width 9216, rank 8 of queries alone, with the projections 84.7 us; eight waves of 16 ranks x 16 tokens 87.4),
     // else two or four eights of ranks each, or sixteen tokens where a row has more (4 x 50 tokens, rank 64, 27.4 us instead of 31.4; 31 rows x 1
-    // token, rank 128, 36.1 instead of 42.2).
+    // token, rank 128, 36.1 instead of 42.2).  Sixteen tokens and one eight of ranks are the faster while they are a round of the chip, width 4096,
+    // rank 128: 4 x 32 tokens 5.0 us, 32 tokens and four eights 6.6; beyond one they are not: 8 x 64 17 and 8, 16 x 64 30 and 9, 64 x 64 115 and 25.
     const long long eights = (long long)B * ((Tn + 7) / 8) * (R / 8) * ((a_q ? 1 : 0) + (a_k ? 1 : 0));
     auto go = [&](auto u, auto xt, auto waves) {
         return launch_down<decltype(u)::value, decltype(xt)::value, decltype(waves)::value>(x, ids, a_q, a_k, scales, n, R, B, Tn, D, t, stream);

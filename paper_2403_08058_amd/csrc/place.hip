@@ -188,7 +188,8 @@ __global__ __launch_bounds__(kPlaceBlock) void place_tokens_kernel(PlaceShape sh
 // order, a row's in order.  One workgroup, because rows write behind one another; a wave takes every 16th row, looks at 64 at a time, and
 // goes through those that give pages back, once to count them and once, when all that come before are counted, to move them.  Look-ups
 // that wait for one another bound it: one row of 32 pages among 16 rows 4.2 us, 16 rows of 128 pages among 256 4.5 us, 100 rows of 32
-// pages among 4096 14.6 us (waves that take neighbouring rows 15 and 39.5 us, waves that walk through every row 10.6 and 120).
+// pages among 4096 14.6 us (waves that take neighbouring rows 15 and 39.5 us, waves that walk through every row 10.6 and 120).  One row
+// of 8192 pages is one wave's: 55 us.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kReleaseBlock = 1024;
 
@@ -274,7 +275,8 @@ int launch_place_tokens(const PlaceShape &sh, const PlaceIn &in, const PlaceOut 
 {
     // Up to 1024 rows, a workgroup for every 256 tokens, in one launch; where outputs lie over inputs one workgroup, or two launches of
     // more than 2048 tokens.  Kernel times in us, one workgroup / these / two launches: 16 rows' tokens 3.7; 32 rows, 2000 tokens 8.8 / 5.7; 256 rows
-    // with 24 prompts, 26 000 tokens - / 6.6 / 17; 1000 rows, 100 000 tokens - / 8.7 / 18.
+    // with 24 prompts, 26 000 tokens - / 6.6 / 17; 1000 rows, 100 000 tokens - / 8.7 / 18.  (Two launches in a recorded graph take less between
+    // them: in place 2.9 and 7.5 us more than one.  One launch would have to wait for all workgroups' reads before the first write.)
     const bool in_place = out.new_lens == in.lens || out.n_left == in.n_free;
     if (sh.B <= 4 * kPlaceBlock && (sh.N <= kPlaceOneTokens || !in_place)) {
         const int workgroups = in_place ? 1 : (sh.N + kPlaceBlock - 1) / kPlaceBlock;

@@ -127,7 +127,7 @@ __device__ __forceinline__ int list_adapters(const int (&id)[TT], int lane, int 
 // of head's 256, of which n_cols are wanted; token tok[t] of row b[t].  The tokens may be of rows with different adapters: every one of
 // those is multiplied with all of them, and kept where it is the token's own (what another's columns or ranks hold, infinities and NaN
 // among it, reaches nobody else).  WAVES waves with sums of their own deal (part, chunk, adapter) out among themselves.  (64 rows x 1 token
-// with 64 adapters of rank 16 26.6 us, 17.2 of them without adapters and 6 their first half; 16 x 1 with rank 64 21.8, 14.1 and 4.5.  The
+// with 64 adapters of rank 16 25.4 us, 17.2 of them without adapters and 5.4 their first half; 16 x 1 with rank 64 21.1, 14.0 and 6.  The
 // columns of two or four adapters asked for at once: 28.1 and 27.9, 23.2 and 26.5.)
 template <int WAVES, int NB, int TT>
 __device__ __forceinline__ void add_adapters(const Adapters &ad, f32x4 (&acc)[NB][TT], const int (&b)[TT], const int (&tok)[TT], int Tn, int H,
@@ -1233,7 +1233,7 @@ static int launch_project(const void *x, const void *w_q, const void *w_k, const
     const bool one_round = n_large <= 150 && D < 8192;
     const long long most = n_large > 256 ? 24576 : (D < 2048 || one_round ? 16384 : (D < 3072 || n_large > 200 ? 20480 : 24576));
     // (With adapters, a call of more tokens goes there as well where it is the faster by far: 14 rows x 32 tokens of 72 dense heads, D = 4096
-    // 383 / 122, 8 x 64 255 / 144, 28 x 64 with 16 of 72 182 / 115.  Calls without keep the kernels, and the bits, that they had.)
+    // 380 / 131, 8 x 64 251 / 152, 28 x 64 with 16 of 72 185 / 128, both halves.  Calls without keep the kernels, and the bits, that they had.)
     const bool few = items <= most || (A::any && 1.15 * small_tiles_cost(B, H, k, Tn, D) < large_tiles_cost(B, k, Tn, D));
     if (listed && few && H <= kJtMaxHeads && (long long)B * Tn * D * 2 < 0x7fffffffLL &&
         (long long)kHeadDim * D * 2 < 0x7fffffffLL) {
@@ -1270,7 +1270,7 @@ int launch_project_qk_adapted(const void *x, const void *w_q, const void *w_k, c
                               void *q_out, void *k_compact, int pos0, int Tc_cap, const AdapterUse &use, hipStream_t stream)
 {
     // Rows of so many pairs that they cannot be listed in LDS go in parts that can, where that is faster than 256-token tiles (43 rows x 2
-    // tokens of 32 dense heads, D = 6656 838 us in one, 84 in two; 35 x 4 of 72, D = 2048 507 and 69 in three).
+    // tokens of 32 dense heads, D = 6656 840 us in one, 65 in two; 35 x 4 of 72, D = 2048 493 and 67 in three).
     int rows = B;
     if ((long long)B * k > kJtMaxSlots && k <= kJtMaxSlots && H <= kJtMaxHeads && !project_streams(B, H, k, Tn, D)) {
         const int parts = (int)((B + kJtMaxSlots / k - 1) / (kJtMaxSlots / k)), each = (B + parts - 1) / parts;

@@ -241,7 +241,9 @@ __global__ __launch_bounds__(kBlock, 7) void turn_kernel(TurnShape sh, TurnRows 
             const int h = rep != nullptr ? min(rep[j], sh.H - 1) : j;
             if (h < 0) return;                           // a slot without a cluster
             if (!key) {
-                if (q_in_place && rep != nullptr) {      // a head that stands in several slots is turned once
+                // A head that stands in several slots is turned once.  (A look at every slot before: 16 x 2043 tokens of 32 heads in 8 clusters
+                // 54.6 us in place, 49.2 elsewhere, of 72 in 16 117 and 100, 4 x 777 of 72 with maps of all 88 and 44.)
+                if (q_in_place && rep != nullptr) {
                     for (int o = 0; o < j; ++o)
                         if (min(rep[o], sh.H - 1) == h) return;
                 }
